@@ -330,6 +330,103 @@ adaspa_status adaspa_block_sparse_attn_noalloc(const adaspa_problem* prob, const
                                                const int32_t* col_idx, int64_t col_count,
                                                void* out, float* lse_out, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The prompt side: attention of queries over keys of another length (cross
+ * attention to an encoder's states), and attention with a learned relative
+ * position bias by buckets (the encoder's own), each with its backward pass.
+ *
+ *   out_i = sum_j exp(S_ij - lse_i) v_j     lse_i = log sum_j exp(S_ij)
+ *   S_ij  = scale * q_i . k_j  (+ table[bucket(j - i - offset), h])
+ *
+ * over the visible keys: j < key_lens[b], key_mask[b, j] != 0 and, with
+ * `causal`, j <= i + offset.  A row that sees no key (a dropped prompt) gives
+ * out = 0, lse = -inf and no gradient.  Whatever masked keys hold, infinities
+ * and NaN too, takes no part.
+ *
+ * Tensors are bf16 or fp16 views [B, heads, tokens, D], D contiguous, with
+ * strides of their own (elements; multiples of 8, the token stride below 2^23;
+ * 16-byte aligned data), so a projection's output is read as it lies and a
+ * batch stride of 0 reads one encoder state for every sample.  Outputs must
+ * not overlap themselves.  H query heads share Hk key heads, H % Hk == 0, in
+ * runs of H / Hk.  Lengths may be 0.  lse: fp32 [B, H, Lq], contiguous.
+ * Scores, softmax, sums and gradients are accumulated in fp32; the weights and
+ * dS are rounded to the inputs' type for the second products, results once.
+ * The workspace is scratch, 256-byte aligned, of the size that the matching
+ * _workspace call names (0: invalid arguments; 16: the call takes none, NULL
+ * will do), not shared by calls that may overlap.  Ownership, streams, errors and determinism are those above: every
+ * sum over more than one workgroup is taken in a fixed order. */
+enum { ADASPA_BF16 = 0, ADASPA_FP16 = 1 };
+
+typedef struct {
+  int32_t batch, heads, kv_heads, q_len, k_len, head_dim;   /* D in {64, 128} */
+  int32_t dtype;                  /* ADASPA_BF16 / ADASPA_FP16, of every tensor */
+  float softmax_scale;            /* <= 0 selects 1/sqrt(D) */
+  /* (batch, head, token) strides in elements; the last four are read by the
+   * backward calls only. */
+  int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
+  int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+  int64_t key_mask_stride;        /* between the mask's rows, in bytes */
+} adaspa_cross_problem;
+
+/* Buckets of the distance between a key and a query.  Bucket m of a direction
+ * holds the distances [bucket_start[m], bucket_start[m+1]), the last one all
+ * from its start on.  Bidirectional: the first half of the table is for keys
+ * at or before the query, the second for keys after it; otherwise keys after
+ * the query have distance 0. */
+typedef struct {
+  int32_t num_buckets;            /* rows of the table, [num_buckets, H]; at most 256 a direction */
+  int32_t bidirectional;
+  const int32_t* bucket_start;    /* HOST array of num_buckets / 2 (bidirectional) or num_buckets
+                                     distances, ascending from 0, the last at most 1024 */
+  int32_t causal;                 /* keys after the query are masked */
+  int32_t q_offset;               /* position of query 0 among the keys, |q_offset| < 2^28 */
+  int32_t queries_at_end;         /* instead: the queries are their sample's last positions,
+                                     offset = key_lens[b] - Lq (decoding with a cache) */
+  int32_t table_fp32;             /* the table and its gradient are fp32 (else the tensors' type) */
+} adaspa_rel_bias;
+
+/* Cross attention.  key_lens: device int32 [B] or NULL (every key), clamped to
+ * [0, Lk]; key_mask: device bytes [B, Lk] (0 = masked) or NULL; lse may be
+ * NULL. */
+size_t adaspa_cross_attn_workspace(const adaspa_cross_problem* prob);
+adaspa_status adaspa_cross_attn(const adaspa_cross_problem* prob, const void* q, const void* k,
+                                const void* v, const int32_t* key_lens,
+                                const uint8_t* key_mask, void* out, float* lse, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* Its backward pass: dq [B, H, Lq, D], dk and dv [B, Hk, Lk, D] (summed over
+ * the query heads that share a key head; 0 for masked keys) from the output's
+ * gradient and the forward call's out and lse. */
+size_t adaspa_cross_attn_bwd_workspace(const adaspa_cross_problem* prob);
+adaspa_status adaspa_cross_attn_bwd(const adaspa_cross_problem* prob, const void* dout,
+                                    const void* q, const void* k, const void* v,
+                                    const int32_t* key_lens, const uint8_t* key_mask,
+                                    const void* out, const float* lse, void* dq, void* dk,
+                                    void* dv, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
+/* Attention with a learned relative position bias: the bias is added from the
+ * table inside the kernels and never written out. */
+size_t adaspa_rel_bias_attn_workspace(const adaspa_cross_problem* prob,
+                                      const adaspa_rel_bias* bias);
+adaspa_status adaspa_rel_bias_attn(const adaspa_cross_problem* prob, const adaspa_rel_bias* bias,
+                                   const void* q, const void* k, const void* v, const void* table,
+                                   const int32_t* key_lens, const uint8_t* key_mask, void* out,
+                                   float* lse, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/* Its backward pass; dtable [num_buckets, H] is the sum of dS over samples and
+ * over the pairs of each bucket, in fp32, rounded once to the table's type. */
+size_t adaspa_rel_bias_attn_bwd_workspace(const adaspa_cross_problem* prob,
+                                          const adaspa_rel_bias* bias);
+adaspa_status adaspa_rel_bias_attn_bwd(const adaspa_cross_problem* prob,
+                                       const adaspa_rel_bias* bias, const void* dout,
+                                       const void* q, const void* k, const void* v,
+                                       const void* table, const int32_t* key_lens,
+                                       const uint8_t* key_mask, const void* out, const float* lse,
+                                       void* dq, void* dk, void* dv, void* dtable,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

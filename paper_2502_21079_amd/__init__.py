@@ -15,6 +15,10 @@ The three calls mirror the C ABI in ``include/adaspa.h``:
                              shape allows it, then the selection (bitwise
                              what the first two give)
 
+The prompt side (cross attention to an encoder's states, attention with a
+learned relative position bias, each with its backward pass) is in
+``prompt.py`` and exported here.
+
 There is no CPU fallback: if the library is missing, every call raises.
 """
 from __future__ import annotations
@@ -33,7 +37,9 @@ __all__ = ["dense_attn_lse", "dense_attn_workspace", "block_search", "block_spar
            "library_path", "load_library", "AdaspaError", "EXPORTED_SYMBOLS",
            "block_search_workspace", "block_search_capacity", "fused_online_search",
            "single_pass_online_search", "single_pass_online_search_workspace",
-           "single_pass_online_search_min_workspace"]
+           "single_pass_online_search_min_workspace", "cross_attn", "cross_attn_workspace", "cross_attn_bwd",
+           "cross_attn_bwd_workspace", "cross_attention", "rel_bias_attn", "rel_bias_attn_workspace",
+           "rel_bias_attn_bwd", "rel_bias_attn_bwd_workspace", "rel_bias_attention", "relative_bucket_starts"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libadaspa.so"
@@ -43,7 +49,10 @@ EXPORTED_SYMBOLS = ("adaspa_status_string", "adaspa_dense_attn_workspace", "adas
                     "adaspa_block_search", "adaspa_block_sparse_attn_workspace",
                     "adaspa_block_sparse_attn", "adaspa_block_sparse_attn_noalloc",
                     "adaspa_fused_online_search", "adaspa_single_pass_online_search_workspace",
-                    "adaspa_single_pass_online_search_min_workspace", "adaspa_single_pass_online_search")
+                    "adaspa_single_pass_online_search_min_workspace", "adaspa_single_pass_online_search",
+                    "adaspa_cross_attn_workspace", "adaspa_cross_attn", "adaspa_cross_attn_bwd_workspace",
+                    "adaspa_cross_attn_bwd", "adaspa_rel_bias_attn_workspace", "adaspa_rel_bias_attn",
+                    "adaspa_rel_bias_attn_bwd_workspace", "adaspa_rel_bias_attn_bwd")
 
 SELECT_TOPK = 0
 SELECT_COVERAGE = 1
@@ -119,6 +128,7 @@ def load_library():
     lib.adaspa_block_sparse_attn_noalloc.restype = ctypes.c_int
     lib.adaspa_block_sparse_attn_noalloc.argtypes = [P, vp, vp, vp, i32p, i32p, ctypes.c_int64,
                                                      vp, f32p, vp]
+    _prompt._declare(lib)
     _lib = lib
     return lib
 
@@ -527,3 +537,9 @@ def block_sparse_attn_noalloc(q, k, v, row_ptr, col_idx, *, block: int, out, lse
                                                 _ptr(out), _ptr(lse), _stream(q.device)))
     return out, lse
 
+
+
+from . import prompt as _prompt  # noqa: E402  (it uses the helpers above)
+from .prompt import (cross_attention, cross_attn, cross_attn_bwd, cross_attn_bwd_workspace,  # noqa: E402
+                     cross_attn_workspace, rel_bias_attention, rel_bias_attn, rel_bias_attn_bwd,
+                     rel_bias_attn_bwd_workspace, rel_bias_attn_workspace, relative_bucket_starts)

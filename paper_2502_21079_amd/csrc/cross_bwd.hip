@@ -1,0 +1,468 @@
+// Backward pass of the attention in cross_fwd.hip (gfx950).
+//
+//   P = exp(S - lse), dP = dO V^T, delta_i = dO_i . O_i, dS = P (dP - delta)
+//   dq = scale dS K, dk = scale dS^T Q, dv = P^T dO   (dk, dv summed over the
+//   query heads that share a key head)
+//   dtable[u, h] = sum of dS over the pairs of bucket u
+//
+// Two kernels, each with its own axis in registers: cross_dq_kernel walks the
+// keys for 128 query rows (and adds up dS by diagonal), cross_dkv_kernel
+// walks the queries for its keys.  Both form S and dP again.  No sum is added
+// to memory by more than one workgroup: partial sums go to the workspace and
+// are added in a fixed order, so results are the same from call to call.
+#include "cross_tile.hpp"
+
+namespace adaspa {
+
+namespace {
+constexpr int kDqRows = 128;           // query rows of a workgroup of cross_dq_kernel
+constexpr int kDkvWaves = 4;           // waves of 32 keys of a workgroup of cross_dkv_kernel
+}  // namespace
+
+template <class T, int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
+  constexpr int NW = 4, KE = 64 * D;
+  __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];
+  extern __shared__ __attribute__((aligned(16))) float bt[];     // the bias, then sums of dS per diagonal
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+
+  const int n_rows = BIAS ? p.Lq : p.G * p.Lq, n_rt = (n_rows + kDqRows - 1) / kDqRows;
+  const int lid = xcd_remap(blockIdx.x, p.n_wg);
+  const int unit = lid / (n_rt * p.splits), split = lid / n_rt % p.splits, r0 = lid % n_rt * kDqRows;
+  const int r = r0 + wave * 32 + c32;
+  const bool row_ok = r < n_rows;
+  const RowOf ro = row_of<BIAS>(p, unit, row_ok ? r : 0);
+  const int b = BIAS ? unit / p.H : unit / p.Hk, hk = BIAS ? (unit % p.H) / p.G : unit % p.Hk;
+  const int n = key_count(p, b), off = query_offset(p, n);
+
+  int kend = n;
+  if (BIAS && p.rb.causal) {
+    const int64_t last = (int64_t)(r0 + kDqRows < n_rows ? r0 + kDqRows : n_rows) + off;
+    kend = last < kend ? (last < 0 ? 0 : (int)last) : kend;
+  }
+  const int nt = (kend + 63) / 64;
+  const int t0 = (int)((int64_t)nt * split / p.splits), t1 = (int)((int64_t)nt * (split + 1) / p.splits);
+
+  // Sums of dS per diagonal: an array of this half-wave's own, so that no two
+  // lanes of one instruction add to the same place and the order of a place's
+  // additions is the program's.
+  const int nd = BIAS ? bias_entries(p.rb.far) : 0;
+  float* diag = bt + nd * (1 + 2 * wave + hw);
+  float far_lo = 0.f, far_hi = 0.f;                       // beyond far on either side
+  if (BIAS) {
+    for (int i = tid; i < 8 * nd; i += 256) bt[nd + i] = 0.f;
+    fill_bias<T, 256>(bt, reinterpret_cast<uint16_t*>(ring), p, unit % p.H, tid);
+    __syncthreads();
+  }
+  const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
+  typename T::x8 qf[D / 16], gf[D / 16];
+  load_row<T, D>(p.q + ro.b * p.sq.b + ro.h * p.sq.h + ro.i * p.sq.t, row_ok, hw, qf);
+  load_row<T, D>(p.dout + ro.b * p.sdo.b + ro.h * p.sdo.h + ro.i * p.sdo.t, row_ok, hw, gf);
+  float lse2 = INFINITY, delta = 0.f;                      // a row without a key: every weight 0
+  {
+    typename T::x8 of[D / 16];
+    load_row<T, D>(p.out + ro.b * p.so.b + ro.h * p.so.h + ro.i * p.so.t, row_ok, hw, of);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
+    delta = both_halves_sum(delta);
+    const float z = row_ok ? p.lse[row] : -INFINITY;
+    if (z != -INFINITY) lse2 = z * kLog2e;
+    if (row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(lse2, delta);
+  }
+
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
+  TileLoad<D, NW> lk, lv;
+  lk.init(wave, lane, p.sk.t);
+  lv.init(wave, lane, p.sv.t);
+  const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+  const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+  int mb = 1;
+  auto issue = [&](int t) {
+    const uint32_t dst = lds_addr(ring[t & 1]);
+    lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
+    lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
+    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, lane);
+  };
+  const int ka = row_lane<D>(c32, hw), ca = col_lane<D>(lane);
+  const int rel0 = 4 * hw - (ro.i + off);
+
+  if (t0 < t1) issue(t0);
+  for (int t = t0; t < t1; ++t) {
+    wait_vmem();
+    const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb != 0) : ~0ull);
+    __syncthreads();
+    if (t + 1 < t1) issue(t + 1);
+    u16* sK = ring[t & 1];
+    u16* sV = sK + KE;
+    if (keep != ~0ull) {
+      if (keep == 0) continue;
+      clear_rows<D, 256>(sK, keep, tid);
+      clear_rows<D, 256>(sV, keep, tid);
+      __syncthreads();
+    }
+    const int far = BIAS ? p.rb.far : 0;
+    const int lo = t * 64 - (r0 + wave * 32 + 31 + off), hi = t * 64 + 63 - (r0 + wave * 32 + off);
+    const int rel = rel0 + t * 64, place = (row_ok ? rel : lo) + far + kPad;
+    const bool beyond = BIAS && (lo >= far || hi <= -far);
+    const float flat = beyond ? bt[lo >= far ? 2 * (far + kPad) : 0] : 0.f;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      f32x16 x = f32x16{}, y = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        x = T::mfma(read_row<T>(sK + (ka ^ (16 * ks)) + 32 * g * D), qf[ks], x);
+        y = T::mfma(read_row<T>(sV + (ka ^ (16 * ks)) + 32 * g * D), gf[ks], y);
+      }
+      if (BIAS) {
+        if (beyond) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, flat);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, bt[place + 32 * g + 8 * (e >> 2) + (e & 3)]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] *= p.sl2;
+      }
+      if (keep != ~0ull) {
+        const uint32_t mine = (uint32_t)(keep >> (32 * g)) >> (4 * hw);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!((mine >> (8 * (e >> 2) + (e & 3))) & 1)) x[e] = -INFINITY;
+      }
+      if (BIAS && p.rb.causal && t * 64 + 63 > r0 + wave * 32 + off) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (rel + 32 * g + 8 * (e >> 2) + (e & 3) > 0) x[e] = -INFINITY;
+      }
+      u32x4 w[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] = fast_exp2(x[e] - lse2) * (y[e] - delta);
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+      if (BIAS) {
+        if (beyond) {
+          float s = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s += y[e];
+          if (lo >= far) far_hi += s;
+          else far_lo += s;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            __hip_atomic_fetch_add(diag + place + 32 * g + 8 * (e >> 2) + (e & 3), y[e], __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const typename T::x8 ds = __builtin_bit_cast(typename T::x8, w[s]);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+          acc[d] = T::mfma(read_col<T, D>(sK, ca, d, 32 * g + 16 * s), ds, acc[d]);
+      }
+    }
+  }
+
+  if (p.splits > 1) {
+    const int64_t at = (int64_t)split * p.B * p.H * p.Lq + row;
+    store_tile_f32<D>(acc, p.part_o + at * D, row_ok, hw);
+  } else {
+    store_tile<T, D>(acc, p.scale, p.dq + ro.b * p.sdq.b + ro.h * p.sdq.h + ro.i * p.sdq.t, row_ok, hw);
+  }
+  if (!BIAS) return;
+
+  // This workgroup's share of the table's gradient: diagonals added over the
+  // eight half-waves, then each bucket its run of diagonals.
+  far_lo = wave_sum(far_lo);
+  far_hi = wave_sum(far_hi);
+  __syncthreads();                                        // every wave's additions are done, the ring is free
+  float* far_sum = reinterpret_cast<float*>(ring);
+  if (lane == 0) {
+    far_sum[wave] = far_lo;
+    far_sum[4 + wave] = far_hi;
+  }
+  for (int i = tid; i < nd; i += 256) {
+    float s = 0.f;
+    for (int a = 1; a <= 8; ++a) s += bt[nd * a + i];
+    bt[i] = s;
+  }
+  __syncthreads();
+  const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side, mid = p.rb.far + kPad;
+  for (int u = tid; u < buckets; u += 256) {
+    const bool ahead = u >= p.rb.side;
+    const int m = ahead ? u - p.rb.side : u;
+    const bool last = m == p.rb.side - 1;
+    int i0 = p.rb.start[m];
+    const int i1 = last ? mid + 1 : p.rb.start[m + 1];
+    if (ahead && i0 == 0) i0 = 1;
+    float s = 0.f;
+    for (int i = i0; i < i1; ++i) s += bt[ahead ? mid + i : mid - i];
+    const float* fs = far_sum + (ahead ? 4 : 0);
+    if (last) s += (fs[0] + fs[1]) + (fs[2] + fs[3]);
+    if (!p.rb.both && u == 0) {                            // one direction: every key after the query
+      for (int i = mid + 1; i < nd; ++i) s += bt[i];
+      s += (far_sum[4] + far_sum[5]) + (far_sum[6] + far_sum[7]);
+    }
+    p.part_t[(((int64_t)unit * n_rt + r0 / kDqRows) * p.splits + split) * buckets + u] = s;
+  }
+}
+
+// dk and dv of 32 keys per wave, over one range of the (query head, 64-row
+// query tile) items that see them.
+template <class T, int D, bool BIAS>
+__global__ __launch_bounds__(64 * kDkvWaves, 1) void cross_dkv_kernel(const CrossParams p) {
+  constexpr int NW = kDkvWaves, NT = 64 * NW, KE = 64 * D;
+  __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];      // slots [Q | dO]
+  __shared__ __attribute__((aligned(16))) float2 ld[2][64];           // log2-LSE and delta of their rows
+  extern __shared__ __attribute__((aligned(16))) float bt[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+
+  const int n_kt = (p.Lk + 32 * NW - 1) / (32 * NW);
+  const int lid = xcd_remap(blockIdx.x, p.n_wg);
+  const int unit = lid / (n_kt * p.kv_splits), split = lid / n_kt % p.kv_splits, j0 = lid % n_kt * 32 * NW;
+  const int b = unit / p.Hk, hk = unit % p.Hk;
+  const int n = key_count(p, b), off = query_offset(p, n);
+  const int key = j0 + wave * 32 + c32;
+  const bool key_ok = key < n && !(p.key_mask && p.key_mask[b * p.mask_stride + key] == 0);
+
+  const int nqt = (p.Lq + 63) / 64;
+  int q_first = 0;                                        // first query tile that sees a key of this tile
+  if (BIAS && p.rb.causal) q_first = j0 - off <= 0 ? 0 : (j0 - off) / 64;
+  const int per_head = j0 >= n || q_first >= nqt ? 0 : nqt - q_first;
+  const int64_t items = (int64_t)per_head * p.G;
+  const int i0 = (int)(items * split / p.kv_splits), i1 = (int)(items * (split + 1) / p.kv_splits);
+
+  typename T::x8 kf[D / 16], vf[D / 16];
+  load_row<T, D>(p.k + b * p.sk.b + hk * p.sk.h + (int64_t)key * p.sk.t, key_ok, hw, kf);
+  load_row<T, D>(p.v + b * p.sv.b + hk * p.sv.h + (int64_t)key * p.sv.t, key_ok, hw, vf);
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f32x16{};
+
+  TileLoad<D, NW> lq, lg;
+  lq.init(wave, lane, p.sq.t);
+  lg.init(wave, lane, p.sdo.t);
+  const int ra = row_lane<D>(c32, hw), ca = col_lane<D>(lane);
+  float2 mine = make_float2(0.f, 0.f);
+  auto issue = [&](int it) {
+    const int h = hk * p.G + it / per_head, q0 = (q_first + it % per_head) * 64;
+    const uint32_t dst = lds_addr(ring[it & 1]);
+    lq.issue(dst, p.q + b * p.sq.b + h * p.sq.h + q0 * p.sq.t, p.sq.t, p.Lq - q0);
+    lg.issue(dst + KE * 2, p.dout + b * p.sdo.b + h * p.sdo.h + q0 * p.sdo.t, p.sdo.t, p.Lq - q0);
+    if (tid < 64) {
+      mine = make_float2(INFINITY, 0.f);                  // past the last row: weight 0
+      if (q0 + tid < p.Lq) mine = p.row_ld[((int64_t)b * p.H + h) * p.Lq + q0 + tid];
+    }
+  };
+  // A tile that ends past the last row leaves those rows of its slot as they
+  // were: they have to be numbers, since they meet weights of zero.
+  for (int c = tid; c < 2 * 2 * KE / 8; c += NT) *reinterpret_cast<u32x4*>(&ring[0][0] + c * 8) = u32x4{0, 0, 0, 0};
+  __syncthreads();
+  int head = -1;
+  if (i0 < i1) {
+    issue(i0);
+    if (tid < 64) ld[i0 & 1][tid] = mine;
+  }
+  for (int it = i0; it < i1; ++it) {
+    wait_vmem();
+    __syncthreads();
+    const int g_head = it / per_head, q0 = (q_first + it % per_head) * 64;
+    if (BIAS && g_head != head) {                         // another query head: its own bias
+      __shared__ uint16_t start[kMaxBucketSide];
+      fill_bias<T, NT>(bt, start, p, hk * p.G + g_head, tid);
+      head = g_head;
+      __syncthreads();
+    }
+    if (it + 1 < i1) issue(it + 1);
+    const u16* sQ = ring[it & 1];
+    const u16* sG = sQ + KE;
+    const int far = BIAS ? p.rb.far : 0;
+    const int jw = j0 + wave * 32, lo = jw - (q0 + 63 + off), hi = jw + 31 - (q0 + off);
+    const int rel = key - (q0 + 4 * hw + off);            // of this lane's first query of the tile
+    const bool beyond = BIAS && (lo >= far || hi <= -far);
+    const float flat = beyond ? bt[lo >= far ? 2 * (far + kPad) : 0] : 0.f;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      f32x16 x = f32x16{}, y = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        x = T::mfma(read_row<T>(sQ + (ra ^ (16 * ks)) + 32 * g * D), kf[ks], x);
+        y = T::mfma(read_row<T>(sG + (ra ^ (16 * ks)) + 32 * g * D), vf[ks], y);
+      }
+      if (BIAS) {
+        if (beyond) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, flat);
+        } else {
+          const float* at = bt + rel + far + kPad;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[-(32 * g + 8 * (e >> 2) + (e & 3))]);
+        }
+        if (p.rb.causal && hi > 0) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (rel - (32 * g + 8 * (e >> 2) + (e & 3)) > 0) x[e] = -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] *= p.sl2;
+      }
+      u32x4 wp[2], ws[2];
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const f32x4 s = *reinterpret_cast<const f32x4*>(&ld[it & 1][32 * g + 8 * (e >> 2) + 4 * hw + (e & 3)]);
+        const float a = fast_exp2(x[e] - s[0]), c = fast_exp2(x[e + 1] - s[2]);
+        wp[e >> 3][(e & 7) >> 1] = T::pack(a, c);
+        ws[e >> 3][(e & 7) >> 1] = T::pack(a * (y[e] - s[1]), c * (y[e + 1] - s[3]));
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const typename T::x8 pf = __builtin_bit_cast(typename T::x8, wp[s]), sf = __builtin_bit_cast(typename T::x8, ws[s]);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+          dv[d] = T::mfma(read_col<T, D>(sG, ca, d, 32 * g + 16 * s), pf, dv[d]);
+          dk[d] = T::mfma(read_col<T, D>(sQ, ca, d, 32 * g + 16 * s), sf, dk[d]);
+        }
+      }
+    }
+    if (it + 1 < i1 && tid < 64) ld[(it + 1) & 1][tid] = mine;
+  }
+  // A masked key took part with a row of zeros: its sums are dropped.
+  if (!key_ok) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f32x16{};
+  }
+  const bool ok = key < p.Lk;
+  if (p.kv_splits > 1) {
+    const int64_t all = (int64_t)p.B * p.Hk * p.Lk, at = (int64_t)unit * p.Lk + key;
+    store_tile_f32<D>(dk, p.part_kv + ((2 * split) * all + at) * D, ok, hw);
+    store_tile_f32<D>(dv, p.part_kv + ((2 * split + 1) * all + at) * D, ok, hw);
+    return;
+  }
+  store_tile<T, D>(dk, p.scale, p.dk + b * p.sdk.b + hk * p.sdk.h + (int64_t)key * p.sdk.t, ok, hw);
+  store_tile<T, D>(dv, 1.f, p.dv + b * p.sdv.b + hk * p.sdv.h + (int64_t)key * p.sdv.t, ok, hw);
+}
+
+// out row = scale * sum over the splits of its partial rows, in order.
+template <class T, int D>
+__global__ __launch_bounds__(256) void cross_sum_kernel(const float* part, int64_t stride, int splits, int64_t rows,
+                                                        int heads, int len, u16* out, Strides so, float scale) {
+  constexpr int TPR = D / 4;
+  const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (row >= rows) return;
+  const int c = threadIdx.x % TPR * 4;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(part + s * stride + row * D + c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += v[j];
+  }
+  const int i = (int)(row % len), h = (int)(row / len % heads), b = (int)(row / len / heads);
+  uint2 w;
+  w.x = T::pack(o[0] * scale, o[1] * scale);
+  w.y = T::pack(o[2] * scale, o[3] * scale);
+  *reinterpret_cast<uint2*>(out + b * so.b + h * so.h + i * so.t + c) = w;
+}
+
+// dtable[u, h]: the workgroups' shares of head h, over samples and row tiles,
+// four runs of them at a time, each in order.
+template <class T>
+__global__ __launch_bounds__(256) void cross_dtable_kernel(const CrossParams p, int tiles) {
+  __shared__ float sum[4][64];
+  const int h = blockIdx.x, buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
+  const int u = blockIdx.y * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6, n = p.B * tiles;
+  float s = 0.f;
+  if (u < buckets) {
+    const int a0 = (int)((int64_t)n * part / 4), a1 = (int)((int64_t)n * (part + 1) / 4);
+    for (int a = a0; a < a1; ++a)
+      s += p.part_t[(((int64_t)(a / tiles) * p.H + h) * tiles + a % tiles) * buckets + u];
+  }
+  sum[part][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (part != 0 || u >= buckets) return;
+  s = (sum[0][threadIdx.x] + sum[1][threadIdx.x]) + (sum[2][threadIdx.x] + sum[3][threadIdx.x]);
+  const int64_t at = (int64_t)u * p.H + h;
+  if (p.rb.table_f32) ((float*)p.rb.dtable)[at] = s;
+  else T::store(p.rb.dtable, at, s);
+}
+
+namespace {
+int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
+int64_t row_tiles(const CrossParams& p, bool bias) {
+  return ((bias ? p.Lq : (int64_t)p.G * p.Lq) + kDqRows - 1) / kDqRows;
+}
+int clamp_splits(int64_t s, int64_t most) {
+  s = s < most ? s : most;
+  return s < 1 ? 1 : (s > 128 ? 128 : (int)s);
+}
+}  // namespace
+
+CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
+  CrossPlan c{};
+  const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), tiles = units * row_tiles(p, bias);
+  const int64_t nt = (p.Lk + 63) / 64;
+  c.splits = tiles > 0 && tiles < 256 ? clamp_splits(512 / tiles, nt / 4) : 1;
+  const int64_t ktiles = (int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves));
+  const int64_t items = (int64_t)p.G * ((p.Lq + 63) / 64);
+  c.kv_splits = ktiles > 0 && ktiles < 256 ? clamp_splits(512 / ktiles, items / 4) : 1;
+  const int64_t rows = (int64_t)p.B * p.H * p.Lq;
+  int64_t off = up256(rows * 8);                     // row_ld at 0
+  c.part_o = off;
+  if (c.splits > 1) off += up256(c.splits * rows * D * 4);
+  c.part_kv = off;
+  if (c.kv_splits > 1) off += up256((int64_t)c.kv_splits * 2 * p.B * p.Hk * p.Lk * D * 4);
+  c.part_t = off;
+  if (bias) off += up256(tiles * c.splits * (p.rb.both ? 2 : 1) * p.rb.side * 4);
+  c.bytes = off;
+  return c;
+}
+
+template <class T, int D>
+static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStream_t st) {
+  p.splits = c.splits;
+  p.kv_splits = c.kv_splits;
+  const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rt = row_tiles(p, bias);
+  const int64_t rows = (int64_t)p.B * p.H * p.Lq, keys = (int64_t)p.B * p.Hk * p.Lk;
+  const uint32_t lds = bias ? bias_entries(p.rb.far) * 4 : 0, per = 256 / (D / 4);
+  p.n_wg = (int)(units * rt * p.splits);
+  if (p.n_wg > 0) {
+    if (bias) hipLaunchKernelGGL((cross_dq_kernel<T, D, true>), dim3(p.n_wg), dim3(256), 9 * lds, st, p);
+    else hipLaunchKernelGGL((cross_dq_kernel<T, D, false>), dim3(p.n_wg), dim3(256), 0, st, p);
+    if (p.splits > 1)
+      hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, st,
+                         p.part_o, rows * D, p.splits, rows, p.H, p.Lq, p.dq, p.sdq, p.scale);
+  }
+  p.n_wg = (int)((int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves)) * p.kv_splits);
+  if (p.n_wg > 0) {
+    if (bias) hipLaunchKernelGGL((cross_dkv_kernel<T, D, true>), dim3(p.n_wg), dim3(64 * kDkvWaves), lds, st, p);
+    else hipLaunchKernelGGL((cross_dkv_kernel<T, D, false>), dim3(p.n_wg), dim3(64 * kDkvWaves), 0, st, p);
+    if (p.kv_splits > 1) {
+      const dim3 grid((uint32_t)((keys + per - 1) / per));
+      hipLaunchKernelGGL((cross_sum_kernel<T, D>), grid, dim3(256), 0, st, p.part_kv, 2 * keys * D, p.kv_splits, keys,
+                         p.Hk, p.Lk, p.dk, p.sdk, p.scale);
+      hipLaunchKernelGGL((cross_sum_kernel<T, D>), grid, dim3(256), 0, st, p.part_kv + keys * D, 2 * keys * D,
+                         p.kv_splits, keys, p.Hk, p.Lk, p.dv, p.sdv, 1.f);
+    }
+  }
+  if (bias) {
+    const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
+    hipLaunchKernelGGL((cross_dtable_kernel<T>), dim3(p.H, (buckets + 63) / 64), dim3(256), 0, st, p,
+                       (int)(rt * p.splits));
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_cross_bwd(CrossParams p, int D, bool f16, bool bias, const CrossPlan& c, hipStream_t st) {
+  if (D == 64) return f16 ? run_bwd<FP16, 64>(p, bias, c, st) : run_bwd<BF16, 64>(p, bias, c, st);
+  return f16 ? run_bwd<FP16, 128>(p, bias, c, st) : run_bwd<BF16, 128>(p, bias, c, st);
+}
+
+}  // namespace adaspa

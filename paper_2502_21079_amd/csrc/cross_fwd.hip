@@ -1,0 +1,276 @@
+// Forward attention of queries over keys of another length, with an optional
+// learned relative position bias (gfx950).
+//
+//   out_i = sum_j exp(S_ij - lse_i) v_j,  lse_i = log sum_j exp(S_ij),
+//   S_ij = scale q_i . k_j (+ bias[bucket(j - i - offset), h])
+//
+// over the visible keys of the sample; a row without any gives 0 and -inf.
+#include "cross_tile.hpp"
+
+namespace adaspa {
+
+namespace {
+
+constexpr int kRows = 128;             // query rows of a workgroup: four waves of 32
+constexpr float kMaxRise = 8.f;        // log2 units a row's maximum may rise before its sums are rescaled
+
+// Running softmax of the rows of a wave (lane = row c32, the two half-waves
+// hold its keys between them).  The reference m (log2 units) follows the
+// maximum, but stays where it is while the maximum is less than kMaxRise above
+// it: no weight then exceeds 2^8, which fp16 holds as well, and the output
+// accumulator is rescaled a few times per row instead of at every tile.
+template <class T, int D>
+struct Rows {
+  f32x16 o[D / 32];
+  float m, l;
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
+    m = -INFINITY;
+    l = 0.f;
+  }
+  // Scores of 64 keys in x (log2 units): weights into pb, their fp32 sum into
+  // l, the accumulator rescaled where the reference moved.
+  __device__ __forceinline__ void weigh(f32x16 (&x)[2], typename T::x8 (&pb)[2][2]) {
+    float mt = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) mt = vmax(mt, vmax(x[g][e], x[g][e + 1]));
+    mt = both_halves_max(mt);
+    // Also where the maximum is NaN: the row becomes NaN.
+    const bool move = !(mt <= m + kMaxRise) && mt != -INFINITY;
+    if (__any(move)) {
+      const float mn = move ? mt : m;
+      const float a = move ? fast_exp2(m - mn) : 1.f;
+      m = mn;
+      l *= a;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] *= a;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      u32x4 w[2];
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float a = fast_exp2(x[g][e] - ref), b = fast_exp2(x[g][e + 1] - ref);
+        s0 += a;
+        s1 += b;
+        w[e >> 3][(e & 7) >> 1] = T::pack(a, b);
+      }
+      pb[g][0] = __builtin_bit_cast(typename T::x8, w[0]);
+      pb[g][1] = __builtin_bit_cast(typename T::x8, w[1]);
+    }
+    l += s0 + s1;
+  }
+};
+
+}  // namespace
+
+// Workgroup: 128 query rows of one unit over one range of its keys, 64-key
+// tiles through a ring of two in LDS, the next one loaded while one is used.
+template <class T, int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) {
+  constexpr int NW = 4, KE = 64 * D;
+  __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];
+  extern __shared__ __attribute__((aligned(16))) float bt[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+
+  const int n_rows = BIAS ? p.Lq : p.G * p.Lq, n_rt = (n_rows + kRows - 1) / kRows;
+  const int lid = xcd_remap(blockIdx.x, p.n_wg);
+  const int unit = lid / (n_rt * p.splits), split = lid / n_rt % p.splits, r0 = lid % n_rt * kRows;
+  const int r = r0 + wave * 32 + c32;
+  const bool row_ok = r < n_rows;
+  const RowOf ro = row_of<BIAS>(p, unit, row_ok ? r : 0);
+  const int b = BIAS ? unit / p.H : unit / p.Hk, hk = BIAS ? (unit % p.H) / p.G : unit % p.Hk;
+  const int n = key_count(p, b), off = query_offset(p, n);
+
+  int kend = n;
+  if (BIAS && p.rb.causal) {
+    const int64_t last = (int64_t)(r0 + kRows < n_rows ? r0 + kRows : n_rows) + off;   // past the last visible key
+    kend = last < kend ? (last < 0 ? 0 : (int)last) : kend;
+  }
+  const int nt = (kend + 63) / 64;
+  const int t0 = (int)((int64_t)nt * split / p.splits), t1 = (int)((int64_t)nt * (split + 1) / p.splits);
+
+  if (BIAS) {
+    uint16_t* start = reinterpret_cast<uint16_t*>(ring);
+    fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
+    __syncthreads();
+  }
+  typename T::x8 qf[D / 16];
+  load_row<T, D>(p.q + ro.b * p.sq.b + ro.h * p.sq.h + ro.i * p.sq.t, row_ok, hw, qf);
+
+  Rows<T, D> acc;
+  acc.init();
+  TileLoad<D, NW> lk, lv;
+  lk.init(wave, lane, p.sk.t);
+  lv.init(wave, lane, p.sv.t);
+  const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+  const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+  int mb = 1;
+  auto issue = [&](int t) {
+    const uint32_t dst = lds_addr(ring[t & 1]);
+    lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
+    lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
+    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, lane);
+  };
+  const int ka = row_lane<D>(c32, hw), ca = col_lane<D>(lane);
+  // Key minus query position of this lane's first key of tile 0.
+  const int rel0 = 4 * hw - (ro.i + off);
+
+  if (t0 < t1) issue(t0);
+  for (int t = t0; t < t1; ++t) {
+    wait_vmem();
+    const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb != 0) : ~0ull);
+    __syncthreads();
+    if (t + 1 < t1) issue(t + 1);
+    u16* sK = ring[t & 1];
+    u16* sV = sK + KE;
+    if (keep != ~0ull) {
+      if (keep == 0) continue;
+      clear_rows<D, 256>(sV, keep, tid);
+      __syncthreads();
+    }
+    f32x16 x[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      x[g] = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+        x[g] = T::mfma(read_row<T>(sK + (ka ^ (16 * ks)) + 32 * g * D), qf[ks], x[g]);
+    }
+    const int rel = rel0 + t * 64;                       // of this lane's first key of the tile
+    if (BIAS) {
+      const int far = p.rb.far, lo = t * 64 - (r0 + wave * 32 + 31 + off), hi = t * 64 + 63 - (r0 + wave * 32 + off);
+      if (lo >= far || hi <= -far) {
+        const float c = bt[lo >= far ? 2 * (far + kPad) : 0];
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[g][e] = fmaf(x[g][e], p.sl2, c);
+      } else {
+        const float* at = bt + (row_ok ? rel : lo) + far + kPad;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[g][e] = fmaf(x[g][e], p.sl2, at[32 * g + 8 * (e >> 2) + (e & 3)]);
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[g][e] *= p.sl2;
+    }
+    if (keep != ~0ull) {
+      const uint64_t mine = keep >> (4 * hw);
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!((mine >> (32 * g + 8 * (e >> 2) + (e & 3))) & 1)) x[g][e] = -INFINITY;
+    }
+    if (BIAS && p.rb.causal && t * 64 + 63 > r0 + wave * 32 + off) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (rel + 32 * g + 8 * (e >> 2) + (e & 3) > 0) x[g][e] = -INFINITY;
+    }
+    typename T::x8 pb[2][2];
+    acc.weigh(x, pb);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        acc.o[d] = T::mfma(read_col<T, D>(sV, ca, d, 16 * s), pb[s >> 1][s & 1], acc.o[d]);
+  }
+
+  const float l = both_halves_sum(acc.l);
+  const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
+  if (p.splits > 1) {
+    const int64_t at = (int64_t)split * p.B * p.H * p.Lq + row;
+    store_tile_f32<D>(acc.o, p.part_o + at * D, row_ok, hw);
+    if (row_ok && hw == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(acc.m, l);
+    return;
+  }
+  store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, p.out + ro.b * p.so.b + ro.h * p.so.h + ro.i * p.so.t, row_ok, hw);
+  if (p.lse && row_ok && hw == 0) p.lse[row] = l == 0.f ? -INFINITY : (acc.m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Joins the ranges of a split call: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+template <class T, int D>
+__global__ __launch_bounds__(256) void cross_join_kernel(const CrossParams p) {
+  constexpr int TPR = D / 4;                             // threads per row
+  const int64_t rows = (int64_t)p.B * p.H * p.Lq, row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (row >= rows) return;
+  const int c = threadIdx.x % TPR * 4;
+  float m = -INFINITY;
+  for (int s = 0; s < p.splits; ++s) m = vmax(m, p.part_ml[2 * (s * rows + row)]);
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < p.splits; ++s) {
+    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * (s * rows + row));
+    const float w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (s * rows + row) * D + c);
+    l += w * ml.y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += w * v[j];
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int i = (int)(row % p.Lq), h = (int)(row / p.Lq % p.H), b = (int)(row / p.Lq / p.H);
+  uint2 w;
+  w.x = T::pack(o[0] * inv, o[1] * inv);
+  w.y = T::pack(o[2] * inv, o[3] * inv);
+  *reinterpret_cast<uint2*>(p.out + b * p.so.b + h * p.so.h + i * p.so.t + c) = w;
+  if (p.lse && c == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+namespace {
+int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
+}  // namespace
+
+CrossPlan plan_fwd(const CrossParams& p, int D, bool bias) {
+  CrossPlan c{};
+  const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rows = bias ? p.Lq : (int64_t)p.G * p.Lq;
+  const int64_t tiles = units * ((rows + kRows - 1) / kRows), nt = (p.Lk + 63) / 64;
+  // Keys are split where the row tiles alone leave CUs without work, into
+  // ranges of no less than four tiles.
+  int64_t s = tiles > 0 && tiles < 256 ? 512 / tiles : 1;
+  s = s < nt / 4 ? s : nt / 4;
+  c.splits = s < 1 ? 1 : (s > 128 ? 128 : (int)s);
+  if (c.splits > 1) {
+    const int64_t all = (int64_t)c.splits * p.B * p.H * p.Lq;
+    c.part_ml = up256(all * D * 4);
+    c.bytes = c.part_ml + up256(all * 8);
+  }
+  return c;
+}
+
+template <class T, int D>
+static hipError_t run_fwd(CrossParams p, bool bias, const CrossPlan& c, hipStream_t st) {
+  p.splits = c.splits;
+  const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rows = bias ? p.Lq : (int64_t)p.G * p.Lq;
+  p.n_wg = (int)(units * ((rows + kRows - 1) / kRows) * p.splits);
+  if (p.n_wg == 0) return hipSuccess;
+  if (bias)
+    hipLaunchKernelGGL((cross_fwd_kernel<T, D, true>), dim3(p.n_wg), dim3(256), bias_entries(p.rb.far) * 4, st, p);
+  else hipLaunchKernelGGL((cross_fwd_kernel<T, D, false>), dim3(p.n_wg), dim3(256), 0, st, p);
+  if (p.splits > 1) {
+    const int64_t all = (int64_t)p.B * p.H * p.Lq, per = 256 / (D / 4);
+    hipLaunchKernelGGL((cross_join_kernel<T, D>), dim3((uint32_t)((all + per - 1) / per)), dim3(256), 0, st, p);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_cross_fwd(CrossParams p, int D, bool f16, bool bias, const CrossPlan& c, hipStream_t st) {
+  if (D == 64) return f16 ? run_fwd<FP16, 64>(p, bias, c, st) : run_fwd<BF16, 64>(p, bias, c, st);
+  return f16 ? run_fwd<FP16, 128>(p, bias, c, st) : run_fwd<BF16, 128>(p, bias, c, st);
+}
+
+}  // namespace adaspa

@@ -1,0 +1,246 @@
+// Building blocks of the cross-attention kernels (gfx950): element types,
+// strided tiles in LDS that are read by rows and transposed alike, key
+// visibility, the table of a relative position bias.
+#pragma once
+
+#include "attn_tile.hpp"
+#include "cross.hpp"
+
+namespace adaspa {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Element types: eight values of an MFMA operand, the product, rounding.
+struct BF16 {
+  typedef bf16x8 x8;
+  static constexpr bool kHalf = false;
+  __device__ __forceinline__ static f32x16 mfma(x8 a, x8 b, f32x16 c) { return mfma32(a, b, c); }
+  __device__ __forceinline__ static uint32_t pack(float a, float b) {
+    const bf16x2 r = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, r);
+  }
+  __device__ __forceinline__ static float load(const void* p, int64_t i) {
+    return __uint_as_float((uint32_t)((const u16*)p)[i] << 16);
+  }
+  __device__ __forceinline__ static void store(void* p, int64_t i, float v) {
+    ((__bf16*)p)[i] = (__bf16)v;
+  }
+};
+struct FP16 {
+  typedef f16x8 x8;
+  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+  static constexpr bool kHalf = true;
+  __device__ __forceinline__ static f32x16 mfma(x8 a, x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+  __device__ __forceinline__ static uint32_t pack(float a, float b) {
+    const x2 r = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, r);
+  }
+  __device__ __forceinline__ static float load(const void* p, int64_t i) { return (float)((const _Float16*)p)[i]; }
+  __device__ __forceinline__ static void store(void* p, int64_t i, float v) { ((_Float16*)p)[i] = (_Float16)v; }
+};
+
+// A [rows, D] tile of 16-bit elements in LDS, rows back to back, the 16-byte
+// chunks of a row in an order of the row's own: chunk c of row r is at place
+// c ^ order(r).  One order serves both ways a tile is read here: 16 rows at
+// one column (operands along the row) fall in distinct banks, and so do the
+// four rows of 64 bytes that 32 lanes of a transposed read take.
+template <int D>
+__device__ __forceinline__ int row_order(int r) {
+  return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+// Lane address (elements) of a read along rows: row c32, chunk hw; chunk
+// 2 ks + hw of row 32 g + c32 is at (row_lane ^ 16 ks) + 32 g D.
+template <int D>
+__device__ __forceinline__ int row_lane(int c32, int hw) {
+  return c32 * D + (hw ^ row_order<D>(c32)) * 8;
+}
+// Lane address of a transposed read; output block d of rows 16 s further down
+// begins at (col_lane ^ 32 d) + 16 s D, and its second half at
+// (col_lane ^ 16 ^ 32 d) + (16 s + 8) D.
+template <int D>
+__device__ __forceinline__ int col_lane(int lane) {
+  const int gi = lane & 15, grp = lane >> 4, row = 4 * (lane >> 5) + (gi >> 2);
+  return row * D + ((2 * (grp & 1) + ((gi & 3) >> 1)) ^ row_order<D>(row)) * 8 + 4 * (gi & 1);
+}
+template <class T>
+__device__ __forceinline__ typename T::x8 read_row(const u16* p) {
+  return *reinterpret_cast<const typename T::x8*>(p);
+}
+// Transposed operand: 16 rows from `r16` on of output block d.
+template <class T, int D>
+__device__ __forceinline__ typename T::x8 read_col(const u16* tile, int ca, int d, int r16) {
+  const s16x4 lo = lds_read_tr16(tile + (ca ^ (32 * d)) + r16 * D);
+  const s16x4 hi = lds_read_tr16(tile + (ca ^ 16 ^ (32 * d)) + (r16 + 8) * D);
+  typename T::x8 v;
+  __builtin_memcpy(&v, &lo, 8);
+  __builtin_memcpy(reinterpret_cast<char*>(&v) + 8, &hi, 8);
+  return v;
+}
+
+// Loads of ROWS-row tiles straight into LDS by NW waves.  The source is the
+// tile's first row (a 64-bit address: a long cache passes 32 bits) and offsets
+// inside the tile; rows from `valid` on are left out by the buffer's bounds.
+template <int D, int NW, int ROWS = 64>
+struct TileLoad {
+  static constexpr int CPR = D / 8, RPI = 64 / CPR, NINST = ROWS / RPI, PER = NINST / NW;
+  static_assert(NINST % NW == 0 && (NW * RPI) % 16 == 0, "every wave loads alike, whole periods of the row order apart");
+  uint32_t rel, step, wbase;
+  __device__ __forceinline__ void init(int wave, int lane, int64_t row_stride) {
+    const int p = wave * 64 + lane, row = p / CPR;
+    rel = (uint32_t)(row * row_stride + ((p % CPR) ^ row_order<D>(row)) * 8) * 2u;
+    step = (uint32_t)(NW * RPI * row_stride) * 2u;
+    wbase = (uint32_t)wave * 1024u;
+  }
+  template <int J = 0>
+  __device__ __forceinline__ void go(u32x4 r, uint32_t dst, uint32_t off) const {
+    if constexpr (J < PER) {
+      dma16<J * NW * 1024>(r, dst + wbase, off, 0u);
+      go<J + 1>(r, dst, off + step);
+    }
+  }
+  __device__ __forceinline__ void issue(uint32_t dst, const u16* first, int64_t row_stride, int valid) const {
+    const int n = valid < ROWS ? valid : ROWS;
+    const uint32_t bytes = n <= 0 ? 0u : (uint32_t)((n - 1) * row_stride + D) * 2u;
+    go(rsrc_words(first, bytes), dst, rel);
+  }
+};
+
+// Clears rows of a tile whose bit in `keep` is 0 (rows below n), so that
+// whatever a masked row holds, infinities and NaN too, meets a weight of zero
+// as zero.
+template <int D, int NT>
+__device__ __forceinline__ void clear_rows(u16* tile, uint64_t keep, int tid) {
+  for (int c = tid; c < 64 * (D / 8); c += NT)
+    if (!((keep >> (c / (D / 8))) & 1)) *reinterpret_cast<u32x4*>(tile + c * 8) = u32x4{0, 0, 0, 0};
+}
+
+// Keys of sample b: the count of its own, within [0, Lk].
+__device__ __forceinline__ int key_count(const CrossParams& p, int b) {
+  if (!p.key_lens) return p.Lk;
+  const int n = __builtin_amdgcn_readfirstlane(p.key_lens[b]);
+  return n < 0 ? 0 : (n < p.Lk ? n : p.Lk);
+}
+// Bits of the 64 keys from j0 on that lie below n.
+__device__ __forceinline__ uint64_t below(int j0, int n) {
+  const int left = n - j0;
+  return left >= 64 ? ~0ull : (left <= 0 ? 0ull : (1ull << left) - 1);
+}
+// One mask byte per lane of the 64 keys from j0 on (1 past n).
+__device__ __forceinline__ int mask_byte(const CrossParams& p, int b, int j0, int n, int lane) {
+  return j0 + lane < n ? p.key_mask[b * p.mask_stride + j0 + lane] : 1;
+}
+
+// --- relative position bias --------------------------------------------------
+// The value added to a score depends on the head and on key position minus
+// query position alone, and is constant beyond +-far.  Each workgroup keeps
+// one head's values, times log2(e), in LDS: rel = -far - kPad .. far + kPad.
+// A wave's tile of 32 x 64 scores spans 95 diagonals, so one that is not
+// wholly beyond far never leaves the table.
+constexpr int kPad = 96;
+__host__ __device__ __forceinline__ int bias_entries(int far) { return 2 * (far + kPad) + 1; }
+
+// Table row of a relative position.
+__device__ __forceinline__ int bucket_of(const uint16_t* start, const RelBias& rb, int rel) {
+  int n = rb.both ? (rel < 0 ? -rel : rel) : (rel < 0 ? -rel : 0);
+  n = n < rb.far ? n : rb.far;
+  int lo = 0, hi = rb.side;                  // start[lo] <= n < start[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start[mid] <= n) lo = mid;
+    else hi = mid;
+  }
+  return lo + (rb.both && rel > 0 ? rb.side : 0);
+}
+template <class T>
+__device__ __forceinline__ float table_value(const RelBias& rb, int64_t i) {
+  return rb.table_f32 ? ((const float*)rb.table)[i] : T::load(rb.table, i);
+}
+// Fills bt (bias_entries floats) for head h; start: LDS room of side entries.
+// The caller has a barrier between this and the first read.
+template <class T, int NT>
+__device__ __forceinline__ void fill_bias(float* bt, uint16_t* start, const CrossParams& p, int h, int tid) {
+  for (int i = tid; i < p.rb.side; i += NT) start[i] = p.rb.start[i];
+  __syncthreads();
+  const int n = bias_entries(p.rb.far);
+  for (int i = tid; i < n; i += NT)
+    bt[i] = table_value<T>(p.rb, (int64_t)bucket_of(start, p.rb, i - p.rb.far - kPad) * p.H + h) * kLog2e;
+}
+__device__ __forceinline__ int query_offset(const CrossParams& p, int n) { return p.rb.at_end ? n - p.Lq : p.rb.q_offset; }
+
+// Writes a 32 x D tile held transposed (lane = row c32, columns 32 d + 8 i +
+// 4 hw + j), scaled by inv, to this lane's row: the half-waves exchange so
+// that each lane stores 16 contiguous bytes.
+template <class T, int D>
+__device__ __forceinline__ void store_tile(const f32x16 (&o)[D / 32], float inv, u16* row, bool ok, int hw) {
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t a = T::pack(o[d][4 * i + 2 * j] * inv, o[d][4 * i + 2 * j + 1] * inv);
+        const uint32_t b = T::pack(o[d][4 * i + 4 + 2 * j] * inv, o[d][4 * i + 5 + 2 * j] * inv);
+        const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+        w[j] = r[0];
+        w[2 + j] = r[1];
+      }
+      if (ok) *reinterpret_cast<u32x4*>(row + 32 * d + 8 * (i + hw)) = w;
+    }
+}
+// The same in fp32, 16 bytes per lane as they lie.
+template <int D>
+__device__ __forceinline__ void store_tile_f32(const f32x16 (&o)[D / 32], float* row, bool ok, int hw) {
+  if (!ok) return;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(row + 32 * d + 8 * i + 4 * hw) =
+          f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+}
+template <class T, int D>
+__device__ __forceinline__ void load_row(const u16* row, bool ok, int hw, typename T::x8 (&f)[D / 16]) {
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) {
+    u32x4 w = {0, 0, 0, 0};
+    if (ok) w = *reinterpret_cast<const u32x4*>(row + 16 * ks + 8 * hw);
+    f[ks] = __builtin_bit_cast(typename T::x8, w);
+  }
+}
+__device__ __forceinline__ float both_halves_max(float v) {
+  float a, b;
+  half_pair(v, a, b);
+  return vmax(a, b);
+}
+__device__ __forceinline__ float both_halves_sum(float v) {
+  float a, b;
+  half_pair(v, a, b);
+  return a + b;
+}
+
+// Which query row a lane works on.  Without a bias the query heads that share
+// a key head are rows of one problem (unit = (sample, key head), G * Lq rows);
+// with one a unit is a (sample, query head).
+struct RowOf {
+  int b, h, i;
+};
+template <bool BIAS>
+__device__ __forceinline__ RowOf row_of(const CrossParams& p, int unit, int r) {
+  RowOf o;
+  if (BIAS) {
+    o.b = unit / p.H;
+    o.h = unit % p.H;
+    o.i = r;
+  } else {
+    o.b = unit / p.Hk;
+    const int g = p.G == 1 ? 0 : r / p.Lq;
+    o.h = (unit % p.Hk) * p.G + g;
+    o.i = r - g * p.Lq;
+  }
+  return o;
+}
+
+}  // namespace adaspa
