@@ -26,6 +26,7 @@ adaspa_status check_strides(const int64_t* s) {
 
 // An output's rows must not overlap (an expanded tensor's would).
 bool overlaps(const int64_t* s, int B, int H, int L, int D) {
+  if (B == 0 || L == 0) return false;
   return (B > 1 && s[0] < D) || (H > 1 && s[1] < D) || (L > 1 && s[2] < D);
 }
 
@@ -186,6 +187,7 @@ adaspa_status backward(const adaspa_cross_problem* prob, const adaspa_rel_bias* 
   c.part_o = (float*)(ws + plan.part_o);
   c.part_kv = (float*)(ws + plan.part_kv);
   c.part_t = (float*)(ws + plan.part_t);
+  c.part_f = (float*)(ws + plan.part_f);
   return launch_cross_bwd(c, prob->head_dim, prob->dtype == ADASPA_FP16, with_bias, plan, (hipStream_t)stream) ==
                  hipSuccess
              ? ADASPA_OK

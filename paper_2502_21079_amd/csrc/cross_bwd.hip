@@ -6,8 +6,9 @@
 //   dtable[u, h] = sum of dS over the pairs of bucket u
 //
 // Two kernels, each with its own axis in registers: cross_dq_kernel walks the
-// keys for 128 query rows (and adds up dS by diagonal), cross_dkv_kernel
-// walks the queries for its keys.  Both form S and dP again.  No sum is added
+// keys for 128 query rows, cross_dkv_kernel the queries for its keys.  Both
+// form S and dP again.  The table's gradient comes from cross_band_kernel near
+// the diagonal and from cross_dq_kernel beyond the last bucket's start.  No sum is added
 // to memory by more than one workgroup: partial sums go to the workspace and
 // are added in a fixed order, so results are the same from call to call.
 #include "cross_tile.hpp"
@@ -44,14 +45,9 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   const int nt = (kend + 63) / 64;
   const int t0 = (int)((int64_t)nt * split / p.splits), t1 = (int)((int64_t)nt * (split + 1) / p.splits);
 
-  // Sums of dS per diagonal: an array of this half-wave's own, so that no two
-  // lanes of one instruction add to the same place and the order of a place's
-  // additions is the program's.
-  const int nd = BIAS ? bias_entries(p.rb.far) : 0;
-  float* diag = bt + nd * (1 + 2 * wave + hw);
-  float far_lo = 0.f, far_hi = 0.f;                       // beyond far on either side
+  // Sums of dS and P over the blocks of 32 keys beyond far on either side.
+  float below_ds = 0.f, below_p = 0.f, above_ds = 0.f, above_p = 0.f;
   if (BIAS) {
-    for (int i = tid; i < 8 * nd; i += 256) bt[nd + i] = 0.f;
     fill_bias<T, 256>(bt, reinterpret_cast<uint16_t*>(ring), p, unit % p.H, tid);
     __syncthreads();
   }
@@ -70,8 +66,9 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     delta = both_halves_sum(delta);
     const float z = row_ok ? p.lse[row] : -INFINITY;
     if (z != -INFINITY) lse2 = z * kLog2e;
-    if (row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(lse2, delta);
+    if (p.splits > 1 && row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(lse2, delta);
   }
+  float exact = 0.f;                                       // delta again, as the sum of P dP in fp32
 
   f32x16 acc[D / 32];
 #pragma unroll
@@ -105,11 +102,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
       clear_rows<D, 256>(sV, keep, tid);
       __syncthreads();
     }
-    const int far = BIAS ? p.rb.far : 0;
-    const int lo = t * 64 - (r0 + wave * 32 + 31 + off), hi = t * 64 + 63 - (r0 + wave * 32 + off);
-    const int rel = rel0 + t * 64, place = (row_ok ? rel : lo) + far + kPad;
-    const bool beyond = BIAS && (lo >= far || hi <= -far);
-    const float flat = beyond ? bt[lo >= far ? 2 * (far + kPad) : 0] : 0.f;
+    const int far = BIAS ? p.rb.far : 0, rel = rel0 + t * 64;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       f32x16 x = f32x16{}, y = f32x16{};
@@ -118,17 +111,22 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
         x = T::mfma(read_row<T>(sK + (ka ^ (16 * ks)) + 32 * g * D), qf[ks], x);
         y = T::mfma(read_row<T>(sV + (ka ^ (16 * ks)) + 32 * g * D), gf[ks], y);
       }
+      // The 32 x 32 block's smallest and largest key minus query position.
+      const int lo = t * 64 + 32 * g - (r0 + wave * 32 + 31 + off), hi = lo + 62;
+      const bool above = lo >= far, beyond = BIAS && (above || hi <= -far);
       if (BIAS) {
         if (beyond) {
+          const float c = bt[above ? 2 * (far + kPad) : 0] - lse2;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, flat);
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, c);
         } else {
+          const float* at = bt + (row_ok ? rel + 32 * g : lo) + far + kPad;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, bt[place + 32 * g + 8 * (e >> 2) + (e & 3)]);
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[8 * (e >> 2) + (e & 3)] - lse2);
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] *= p.sl2;
+        for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, -lse2);
       }
       if (keep != ~0ull) {
         const uint32_t mine = (uint32_t)(keep >> (32 * g)) >> (4 * hw);
@@ -136,28 +134,33 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
         for (int e = 0; e < 16; ++e)
           if (!((mine >> (8 * (e >> 2) + (e & 3))) & 1)) x[e] = -INFINITY;
       }
-      if (BIAS && p.rb.causal && t * 64 + 63 > r0 + wave * 32 + off) {
+      if (BIAS && p.rb.causal && hi > 0) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (rel + 32 * g + 8 * (e >> 2) + (e & 3) > 0) x[e] = -INFINITY;
       }
       u32x4 w[2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = fast_exp2(x[e] - lse2) * (y[e] - delta);
+      for (int e = 0; e < 16; ++e) {
+        x[e] = fast_exp2(x[e]);
+        exact = fmaf(x[e], y[e], exact);
+        y[e] = x[e] * (y[e] - delta);
+      }
 #pragma unroll
       for (int e = 0; e < 16; e += 2) w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
-      if (BIAS) {
-        if (beyond) {
-          float s = 0.f;
+      if (beyond) {
+        float sd = 0.f, sp = 0.f;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s += y[e];
-          if (lo >= far) far_hi += s;
-          else far_lo += s;
+        for (int e = 0; e < 16; ++e) {
+          sd += y[e];
+          sp += x[e];
+        }
+        if (above) {
+          above_ds += sd;
+          above_p += sp;
         } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            __hip_atomic_fetch_add(diag + place + 32 * g + 8 * (e >> 2) + (e & 3), y[e], __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_WORKGROUP);
+          below_ds += sd;
+          below_p += sp;
         }
       }
 #pragma unroll
@@ -176,41 +179,111 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   } else {
     store_tile<T, D>(acc, p.scale, p.dq + ro.b * p.sdq.b + ro.h * p.sdq.h + ro.i * p.sdq.t, row_ok, hw);
   }
+  // What the other kernels take as delta: the sum of P dP, free of the output's
+  // rounding; where the keys are split, the one from the rounded output.
+  const float change = p.splits > 1 ? 0.f : both_halves_sum(exact) - delta;
+  if (p.splits == 1 && row_ok && hw == 0) p.row_ld[row] = make_float2(lse2, delta + change);
   if (!BIAS) return;
 
-  // This workgroup's share of the table's gradient: diagonals added over the
-  // eight half-waves, then each bucket its run of diagonals.
-  far_lo = wave_sum(far_lo);
-  far_hi = wave_sum(far_hi);
-  __syncthreads();                                        // every wave's additions are done, the ring is free
-  float* far_sum = reinterpret_cast<float*>(ring);
+  // This workgroup's share of the table's last buckets.
+  float* sums = reinterpret_cast<float*>(ring);
+  __syncthreads();                                        // the ring is free
+  const float below = wave_sum(below_ds - change * below_p), above = wave_sum(above_ds - change * above_p);
   if (lane == 0) {
-    far_sum[wave] = far_lo;
-    far_sum[4 + wave] = far_hi;
-  }
-  for (int i = tid; i < nd; i += 256) {
-    float s = 0.f;
-    for (int a = 1; a <= 8; ++a) s += bt[nd * a + i];
-    bt[i] = s;
+    sums[wave] = below;
+    sums[4 + wave] = above;
   }
   __syncthreads();
-  const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side, mid = p.rb.far + kPad;
-  for (int u = tid; u < buckets; u += 256) {
-    const bool ahead = u >= p.rb.side;
-    const int m = ahead ? u - p.rb.side : u;
-    const bool last = m == p.rb.side - 1;
-    int i0 = p.rb.start[m];
-    const int i1 = last ? mid + 1 : p.rb.start[m + 1];
-    if (ahead && i0 == 0) i0 = 1;
-    float s = 0.f;
-    for (int i = i0; i < i1; ++i) s += bt[ahead ? mid + i : mid - i];
-    const float* fs = far_sum + (ahead ? 4 : 0);
-    if (last) s += (fs[0] + fs[1]) + (fs[2] + fs[3]);
-    if (!p.rb.both && u == 0) {                            // one direction: every key after the query
-      for (int i = mid + 1; i < nd; ++i) s += bt[i];
-      s += (far_sum[4] + far_sum[5]) + (far_sum[6] + far_sum[7]);
+  if (tid < 2)
+    p.part_f[(((int64_t)unit * n_rt + r0 / kDqRows) * p.splits + split) * 2 + tid] =
+        (sums[4 * tid] + sums[4 * tid + 1]) + (sums[4 * tid + 2] + sums[4 * tid + 3]);
+}
+
+// Sums of dS by bucket near the diagonal: a workgroup takes the 32 x 32 blocks
+// of one diagonal of blocks, o = first key - first query (or every
+// band_splits-th four of them), each wave every fourth.  Blocks of one
+// diagonal meet element by element, so their dS are added up in registers, and
+// only the sum is folded: 63 diagonals, then their buckets.  (Adding each
+// block's dS to sums per diagonal in LDS instead took 3/4 of cross_dq_kernel's
+// time: 439 us of 580 at 12 heads x 4,095 tokens, d 128.)  S and dP are formed
+// once more, but for these blocks alone, operands straight from memory.
+template <class T, int D>
+__global__ __launch_bounds__(256) void cross_band_kernel(const CrossParams p) {
+  constexpr int PITCH = 36;                               // floats per row of a folded block
+  __shared__ __attribute__((aligned(16))) float fold[4][32 * PITCH];
+  __shared__ float diag[4][64];
+  __shared__ int of[64];
+  __shared__ uint16_t start[kMaxBucketSide];
+  extern __shared__ __attribute__((aligned(16))) float bt[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+  const int part = blockIdx.x % p.band_splits, band = blockIdx.x / p.band_splits % p.bands;
+  const int unit = blockIdx.x / (p.band_splits * p.bands), b = unit / p.H, h = unit % p.H, hk = h / p.G;
+  const int n = key_count(p, b), off = query_offset(p, n), far = p.rb.far;
+
+  // Diagonals of blocks with a pair nearer than far: off - far - 31 < o < off + far + 31.
+  const int lowest = off - far - 30;
+  const int o = (lowest >= 0 ? (lowest + 31) / 32 : -(-lowest / 32)) * 32 + band * 32;
+  const bool used = o < off + far + 31 && !(p.rb.causal && o - 31 - off > 0);
+  f32x16 acc = f32x16{};
+  if (used) {
+    fill_bias<T, 256>(bt, start, p, h, tid);
+    __syncthreads();
+    // Query blocks i whose key block i + o / 32 has keys.
+    const int first = o < 0 ? -o / 32 : 0, nq = (p.Lq + 31) / 32, nk = (n + 31) / 32 - o / 32;
+    const int last = nq < nk ? nq : nk;
+    const u16* qh = p.q + b * p.sq.b + h * p.sq.h;
+    const u16* gh = p.dout + b * p.sdo.b + h * p.sdo.h;
+    const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+    const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+    const float* at = bt + 4 * hw - c32 + o - off + far + kPad;
+    for (int ib = first + part * 4 + wave; ib < last; ib += 4 * p.band_splits) {
+      const int i = ib * 32 + c32, j0 = ib * 32 + o, key = j0 + c32;
+      const bool row_ok = i < p.Lq, key_ok = key < n && !(p.key_mask && p.key_mask[b * p.mask_stride + key] == 0);
+      const uint32_t keep = (uint32_t)__ballot(key_ok) >> (4 * hw);
+      typename T::x8 a[D / 16], c[D / 16];
+      float2 ld = make_float2(INFINITY, 0.f);
+      if (row_ok) ld = p.row_ld[((int64_t)b * p.H + h) * p.Lq + i];
+      f32x16 x = f32x16{}, y = f32x16{};
+      load_row<T, D>(kh + key * p.sk.t, key_ok, hw, a);
+      load_row<T, D>(qh + i * p.sq.t, row_ok, hw, c);
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) x = T::mfma(a[ks], c[ks], x);
+      load_row<T, D>(vh + key * p.sv.t, key_ok, hw, a);
+      load_row<T, D>(gh + i * p.sdo.t, row_ok, hw, c);
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) y = T::mfma(a[ks], c[ks], y);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int kk = 8 * (e >> 2) + (e & 3);
+        float s = fmaf(x[e], p.sl2, at[kk] - ld.x);
+        if (!((keep >> kk) & 1) || (p.rb.causal && o - off + kk + 4 * hw - c32 > 0)) s = -INFINITY;
+        acc[e] += fast_exp2(s) * (y[e] - ld.y);
+      }
     }
-    p.part_t[(((int64_t)unit * n_rt + r0 / kDqRows) * p.splits + split) * buckets + u] = s;
+  }
+#pragma unroll
+  for (int e = 0; e < 16; e += 4)
+    *reinterpret_cast<f32x4*>(&fold[wave][c32 * PITCH + 2 * e + 4 * hw]) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+  __syncthreads();
+  {
+    // Diagonal d: key = query + d - 31 within the block.
+    const int d = lane;
+    float s = 0.f;
+    for (int r = 0; r < 32; ++r) {
+      const int c = r + d - 31;
+      if (c >= 0 && c < 32) s += fold[wave][r * PITCH + c];
+    }
+    diag[wave][d] = s;
+    if (wave == 0) of[d] = used && d < 63 ? bucket_of(start, p.rb, o - off + d - 31) : -1;
+  }
+  __syncthreads();
+  const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
+  for (int u = tid; u < buckets; u += 256) {
+    float s = 0.f;
+    for (int d = 0; d < 63; ++d)
+      if (of[d] == u) s += (diag[0][d] + diag[1][d]) + (diag[2][d] + diag[3][d]);
+    p.part_t[(int64_t)blockIdx.x * buckets + u] = s;
   }
 }
 
@@ -372,23 +445,31 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(const float* part, int64
   *reinterpret_cast<uint2*>(out + b * so.b + h * so.h + i * so.t + c) = w;
 }
 
-// dtable[u, h]: the workgroups' shares of head h, over samples and row tiles,
-// four runs of them at a time, each in order.
+// dtable[u, h]: the shares of head h over samples and workgroups, eight runs of
+// them at a time, each in order; the last buckets also take what lies beyond far.
 template <class T>
 __global__ __launch_bounds__(256) void cross_dtable_kernel(const CrossParams p, int tiles) {
-  __shared__ float sum[4][64];
+  __shared__ float sum[8][32];
   const int h = blockIdx.x, buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
-  const int u = blockIdx.y * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6, n = p.B * tiles;
+  const int t = threadIdx.x & 31, u = blockIdx.y * 32 + t, part = threadIdx.x >> 5;
   float s = 0.f;
   if (u < buckets) {
-    const int a0 = (int)((int64_t)n * part / 4), a1 = (int)((int64_t)n * (part + 1) / 4);
-    for (int a = a0; a < a1; ++a)
-      s += p.part_t[(((int64_t)(a / tiles) * p.H + h) * tiles + a % tiles) * buckets + u];
+    const int per = p.bands * p.band_splits, n = p.B * per;
+#pragma unroll 8
+    for (int a = n * part / 8; a < n * (part + 1) / 8; ++a)
+      s += p.part_t[(((int64_t)(a / per) * p.H + h) * per + a % per) * buckets + u];
+    const int m = p.B * tiles;
+    for (int side = 0; side < 2; ++side)
+      if (u == (side == 0 ? p.rb.side - 1 : p.rb.both ? buckets - 1 : 0)) {
+#pragma unroll 8
+        for (int a = (int)((int64_t)m * part / 8); a < (int)((int64_t)m * (part + 1) / 8); ++a)
+          s += p.part_f[(((int64_t)(a / tiles) * p.H + h) * tiles + a % tiles) * 2 + side];
+      }
   }
-  sum[part][threadIdx.x & 63] = s;
+  sum[part][t] = s;
   __syncthreads();
   if (part != 0 || u >= buckets) return;
-  s = (sum[0][threadIdx.x] + sum[1][threadIdx.x]) + (sum[2][threadIdx.x] + sum[3][threadIdx.x]);
+  s = ((sum[0][t] + sum[1][t]) + (sum[2][t] + sum[3][t])) + ((sum[4][t] + sum[5][t]) + (sum[6][t] + sum[7][t]));
   const int64_t at = (int64_t)u * p.H + h;
   if (p.rb.table_f32) ((float*)p.rb.dtable)[at] = s;
   else T::store(p.rb.dtable, at, s);
@@ -420,7 +501,16 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   c.part_kv = off;
   if (c.kv_splits > 1) off += up256((int64_t)c.kv_splits * 2 * p.B * p.Hk * p.Lk * D * 4);
   c.part_t = off;
-  if (bias) off += up256(tiles * c.splits * (p.rb.both ? 2 : 1) * p.rb.side * 4);
+  if (bias) {
+    // Multiples of 32 in an open interval of 2 far + 62; as many workgroups for
+    // each as leave a wave eight blocks.
+    const int64_t blocks = (p.Lq < p.Lk ? p.Lq : p.Lk) / 32 + 1;
+    c.bands = (2 * p.rb.far + 61) / 32 + 1;
+    c.band_splits = clamp_splits(blocks / 32, 128);
+    off += up256((int64_t)p.B * p.H * c.bands * c.band_splits * (p.rb.both ? 2 : 1) * p.rb.side * 4);
+    c.part_f = off;
+    off += up256(tiles * c.splits * 8);
+  }
   c.bytes = off;
   return c;
 }
@@ -434,7 +524,7 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   const uint32_t lds = bias ? bias_entries(p.rb.far) * 4 : 0, per = 256 / (D / 4);
   p.n_wg = (int)(units * rt * p.splits);
   if (p.n_wg > 0) {
-    if (bias) hipLaunchKernelGGL((cross_dq_kernel<T, D, true>), dim3(p.n_wg), dim3(256), 9 * lds, st, p);
+    if (bias) hipLaunchKernelGGL((cross_dq_kernel<T, D, true>), dim3(p.n_wg), dim3(256), lds, st, p);
     else hipLaunchKernelGGL((cross_dq_kernel<T, D, false>), dim3(p.n_wg), dim3(256), 0, st, p);
     if (p.splits > 1)
       hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, st,
@@ -454,7 +544,11 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   }
   if (bias) {
     const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
-    hipLaunchKernelGGL((cross_dtable_kernel<T>), dim3(p.H, (buckets + 63) / 64), dim3(256), 0, st, p,
+    p.bands = c.bands;
+    p.band_splits = c.band_splits;
+    if (p.B > 0)
+      hipLaunchKernelGGL((cross_band_kernel<T, D>), dim3(p.B * p.H * p.bands * p.band_splits), dim3(256), lds, st, p);
+    hipLaunchKernelGGL((cross_dtable_kernel<T>), dim3(p.H, (buckets + 31) / 32), dim3(256), 0, st, p,
                        (int)(rt * p.splits));
   }
   return hipGetLastError();

@@ -204,21 +204,41 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 }
 
 // Joins the ranges of a split call: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+// A workgroup per row: groups of D / 4 threads take every NG-th range each,
+// then join their sums, all in a fixed order.
 template <class T, int D>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossParams p) {
-  constexpr int TPR = D / 4;                             // threads per row
-  const int64_t rows = (int64_t)p.B * p.H * p.Lq, row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  if (row >= rows) return;
-  const int c = threadIdx.x % TPR * 4;
-  float m = -INFINITY;
-  for (int s = 0; s < p.splits; ++s) m = vmax(m, p.part_ml[2 * (s * rows + row)]);
-  float l = 0.f;
+  constexpr int TPR = D / 4, NG = 256 / TPR;
+  __shared__ f32x4 so[NG][TPR];
+  __shared__ float sm[NG], sl[NG];
+  const int64_t rows = (int64_t)p.B * p.H * p.Lq, row = blockIdx.x;
+  const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+  float m = -INFINITY, l = 0.f;
+  for (int s = grp; s < p.splits; s += NG) m = vmax(m, p.part_ml[2 * (s * rows + row)]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < p.splits; ++s) {
+#pragma unroll 4
+  for (int s = grp; s < p.splits; s += NG) {
     const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * (s * rows + row));
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (s * rows + row) * D + 4 * t);
     const float w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (s * rows + row) * D + c);
     l += w * ml.y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += w * v[j];
+  }
+  so[grp][t] = o;
+  if (t == 0) {
+    sm[grp] = m;
+    sl[grp] = l;
+  }
+  __syncthreads();
+  if (grp != 0) return;
+  for (int g = 1; g < NG; ++g) m = vmax(m, sm[g]);
+  l = 0.f;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int g = 0; g < NG; ++g) {
+    const float w = sm[g] == -INFINITY ? 0.f : fast_exp2(sm[g] - m);
+    const f32x4 v = so[g][t];
+    l += w * sl[g];
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] += w * v[j];
   }
@@ -227,8 +247,8 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossParams p) {
   uint2 w;
   w.x = T::pack(o[0] * inv, o[1] * inv);
   w.y = T::pack(o[2] * inv, o[3] * inv);
-  *reinterpret_cast<uint2*>(p.out + b * p.so.b + h * p.so.h + i * p.so.t + c) = w;
-  if (p.lse && c == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  *reinterpret_cast<uint2*>(p.out + b * p.so.b + h * p.so.h + i * p.so.t + 4 * t) = w;
+  if (p.lse && t == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 namespace {
@@ -262,8 +282,8 @@ static hipError_t run_fwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
     hipLaunchKernelGGL((cross_fwd_kernel<T, D, true>), dim3(p.n_wg), dim3(256), bias_entries(p.rb.far) * 4, st, p);
   else hipLaunchKernelGGL((cross_fwd_kernel<T, D, false>), dim3(p.n_wg), dim3(256), 0, st, p);
   if (p.splits > 1) {
-    const int64_t all = (int64_t)p.B * p.H * p.Lq, per = 256 / (D / 4);
-    hipLaunchKernelGGL((cross_join_kernel<T, D>), dim3((uint32_t)((all + per - 1) / per)), dim3(256), 0, st, p);
+    const int64_t all = (int64_t)p.B * p.H * p.Lq;
+    hipLaunchKernelGGL((cross_join_kernel<T, D>), dim3((uint32_t)all), dim3(256), 0, st, p);
   }
   return hipGetLastError();
 }

@@ -34,6 +34,7 @@ __all__ = ["cross_attn", "cross_attn_workspace", "cross_attn_bwd", "cross_attn_b
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 _I64x3 = ctypes.c_int64 * 3
+_NO_OUTPUTS = (None,) * 4
 _NO_WORKSPACE = 16                        # the size of a call that takes none
 
 
@@ -86,58 +87,93 @@ def _bias_ref(num_buckets, max_distance, bidirectional, causal, q_offset, table_
     return ctypes.byref(r)
 
 
-@functools.lru_cache(maxsize=512, typed=True)
-def _plan(bwd, dtype, qs, ks, scale, strides, mask_stride, bias):
-    """(problem, bias or None, workspace bytes) of a call."""
+class _Plan:
+    """What calls on tensors of one set of shapes and strides share."""
+    __slots__ = ("prob", "bias", "need", "rows")
+
+
+@functools.lru_cache(maxsize=512)
+def _plan(bwd, dtype, shapes, strides, outs, scale, mask_stride, bias) -> _Plan:
+    """Checks the shapes and strides of q, k, v (and dout) and the strides of
+    the outputs (None: new ones of the inputs' layout) and sets up the call's
+    structures and workspace size."""
     lib = load_library()
+    qs, ks, vs = shapes[:3]
+    if len(qs) != 4 or len(ks) != 4:
+        raise AdaspaError(f"q, k, v must be [B, heads, tokens, D], got {tuple(qs)} and {tuple(ks)}")
+    if vs != ks or ks[0] != qs[0] or ks[3] != qs[3] or ks[1] == 0 or qs[1] % ks[1]:
+        raise AdaspaError(f"shapes do not fit: q {tuple(qs)}, k {tuple(ks)}, v {tuple(vs)}")
+    ins = [_steps(s, t) for s, t in zip(shapes, strides)]
+    # Results in the order out, dq, dk, dv.
+    like = ((qs, strides[0]), (qs, strides[0]), (ks, strides[1]), (ks, strides[2]))
+    res = [_steps(n, _new_strides(n, t) if o is None else o) for (n, t), o in zip(like, outs)]
     B, H, Lq, D = qs
-    _, Hk, Lk, _ = ks
-    p = _CrossProblem(B, H, Hk, Lq, Lk, D, dtype, scale)
-    for name, s in zip(("q", "k", "v", "out", "dout", "dq", "dk", "dv"), strides):
-        setattr(p, name + "_stride", _I64x3(*s[:3]))
+    p = _CrossProblem(B, H, ks[1], Lq, ks[2], D, dtype, scale)
+    for name, s in zip(("q", "k", "v", "dout", "out", "dq", "dk", "dv"), ins + [ins[0]] * (4 - len(ins)) + res):
+        setattr(p, name + "_stride", _I64x3(*s))
     p.key_mask_stride = mask_stride
-    prob = ctypes.byref(p)
-    if bias is None:
-        fn = lib.adaspa_cross_attn_bwd_workspace if bwd else lib.adaspa_cross_attn_workspace
-        return prob, None, int(fn(prob))
-    ref = _bias_ref(*bias)
-    fn = lib.adaspa_rel_bias_attn_bwd_workspace if bwd else lib.adaspa_rel_bias_attn_workspace
-    return prob, ref, int(fn(prob, ref))
+    plan = _Plan()
+    plan.prob, plan.rows = ctypes.byref(p), (B, H, Lq)
+    plan.bias = None if bias is None else _bias_ref(*bias)
+    name = "adaspa_%s_attn%s_workspace" % ("cross" if bias is None else "rel_bias", "_bwd" if bwd else "")
+    plan.need = int(getattr(lib, name)(plan.prob, *([] if bias is None else [plan.bias])))
+    return plan
+
+
+def _steps(shape, stride):
+    """(batch, head, token) strides of a tensor the kernels can read, 0 in
+    place of those that nothing steps along."""
+    s = tuple(a if n > 1 else 0 for a, n in zip(stride[:3], shape))
+    if stride[3] != 1 and shape[3] > 1 or (s[0] | s[1] | s[2]) & 7:
+        raise AdaspaError("tensors need D contiguous and (batch, head, token) strides that are multiples of 8, got "
+                          f"strides {tuple(stride)}")
+    return s
+
+
+@functools.lru_cache(maxsize=512)
+def _keeps_layout(shape, stride):
+    """Whether a new tensor like one of this shape gets these strides: no two
+    elements in one place and no gaps."""
+    n = 1
+    for a, m in sorted((a, m) for a, m in zip(stride, shape) if m > 1):
+        if a != n:
+            return False
+        n *= m
+    return 0 not in shape
+
+
+def _new_strides(shape, stride):
+    return stride if _keeps_layout(shape, stride) else _contiguous(shape)
+
+
+def _new(t):
+    """A new tensor of t's shape, in its layout where that is kept."""
+    return torch.empty_like(t) if _keeps_layout(t.shape, t.stride()) else \
+        torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _contiguous(shape):
+    B, H, L, D = shape
+    return (H * L * D, L * D, D, 1)
 
 
 # --- argument checks -----------------------------------------------------------
 
 def _check_tensors(q, k, v):
-    if q.dtype not in _DTYPES or not q.is_cuda:
+    """The device index of q, k, v, after checks of type and device."""
+    dev = q.get_device()
+    if dev < 0 or q.dtype not in _DTYPES:
         raise AdaspaError("q, k, v must be bf16 or fp16 CUDA tensors [B, heads, tokens, D]")
-    qs, ks = q.shape, k.shape
-    if len(qs) != 4 or len(ks) != 4:
-        raise AdaspaError(f"q, k, v must be [B, heads, tokens, D], got {tuple(qs)} and {tuple(ks)}")
-    if k.dtype is not q.dtype or v.dtype is not q.dtype or k.device != q.device or v.device != q.device:
+    if k.dtype is not q.dtype or v.dtype is not q.dtype or k.get_device() != dev or v.get_device() != dev:
         raise AdaspaError("q, k, v must share one type and device")
-    if v.shape != ks or ks[0] != qs[0] or ks[3] != qs[3] or ks[1] == 0 or qs[1] % ks[1]:
-        raise AdaspaError(f"shapes do not fit: q {tuple(qs)}, k {tuple(ks)}, v {tuple(v.shape)}")
-    for t in (q, k, v):
-        _check_rows(t)
+    return dev
 
 
-def _check_rows(t):
-    s = _strides(t)
-    if s[3] != 1 or (s[0] | s[1] | s[2]) & 7:
-        raise AdaspaError("tensors need D contiguous and (batch, head, token) strides that are multiples of 8, got "
-                          f"strides {s}")
-
-
-def _strides(t):
-    """Strides, 0 in place of those that nothing steps along."""
-    s = t.stride()
-    return tuple(a if n > 1 else 0 for a, n in zip(s[:3], t.shape)) + s[3:] if 1 in t.shape[:3] else s
-
-
-def _check_like(t, shape, like, name):
-    if t.dtype is not like.dtype or tuple(t.shape) != tuple(shape) or t.device != like.device:
-        raise AdaspaError(f"{name} must be a {like.dtype} tensor of shape {tuple(shape)} on q's device")
-    _check_rows(t)
+def _check_like(t, like, name):
+    """Strides of a tensor that the caller gives for a result, or with one."""
+    if t.dtype is not like.dtype or t.shape != like.shape or t.device != like.device:
+        raise AdaspaError(f"{name} must be a {like.dtype} tensor of shape {tuple(like.shape)} on q's device")
+    return t.stride()
 
 
 def _check_lse(lse, q):
@@ -145,18 +181,18 @@ def _check_lse(lse, q):
         raise AdaspaError(f"lse must be a contiguous fp32 [B, H, Lq] = {tuple(q.shape[:3])} tensor on q's device")
 
 
-def _check_keys(key_lens, key_mask, q, k):
-    """The mask as bytes, after checks of both."""
-    if key_lens is not None and (key_lens.dtype is not torch.int32 or key_lens.shape != (q.shape[0],)
-                                 or not key_lens.is_contiguous() or key_lens.device != q.device):
-        raise AdaspaError(f"key_lens must be a contiguous int32 [B] = [{q.shape[0]}] tensor on q's device")
+def _check_keys(key_lens, key_mask, q, k, dev):
+    """Bytes between the mask's rows, after checks of lengths and mask."""
+    if key_lens is not None and (key_lens.dtype is not torch.int32 or key_lens.shape != q.shape[:1]
+                                 or not key_lens.is_contiguous() or key_lens.get_device() != dev):
+        raise AdaspaError(f"key_lens must be a contiguous int32 [B] = {tuple(q.shape[:1])} tensor on q's device")
     if key_mask is None:
-        return None
-    if key_mask.dtype not in (torch.bool, torch.uint8) or key_mask.shape != (q.shape[0], k.shape[2]) \
-            or key_mask.device != q.device or (key_mask.stride(1) != 1 and key_mask.shape[1] > 1):
-        raise AdaspaError(f"key_mask must be a bool or uint8 [B, Lk] = [{q.shape[0]}, {k.shape[2]}] tensor with "
+        return 0
+    if key_mask.dtype not in (torch.bool, torch.uint8) or key_mask.shape != q.shape[:1] + k.shape[2:3] \
+            or key_mask.get_device() != dev or (key_mask.stride(1) != 1 and key_mask.shape[1] > 1):
+        raise AdaspaError(f"key_mask must be a bool or uint8 [B, Lk] = {tuple(q.shape[:1] + k.shape[2:3])} tensor with "
                           "contiguous rows on q's device")
-    return key_mask
+    return key_mask.stride(0)
 
 
 def _bias_key(q, k, table, max_distance, bidirectional, causal, q_offset):
@@ -170,55 +206,46 @@ def _bias_key(q, k, table, max_distance, bidirectional, causal, q_offset):
             table.dtype is torch.float32)
 
 
-def _scratch(workspace, need, dev):
+def _scratch(workspace, need, q):
     """(workspace, bytes): the caller's, checked, or a new one; None where a
     call needs none."""
     if workspace is not None:
-        if workspace.device != dev or not workspace.is_contiguous():
+        if workspace.device != q.device or not workspace.is_contiguous():
             raise AdaspaError("workspace must be a contiguous tensor on q's device")
         return workspace, workspace.numel() * workspace.element_size()
     if need <= _NO_WORKSPACE:
         return None, 0
-    return torch.empty(need, dtype=torch.uint8, device=dev), need
+    return torch.empty(need, dtype=torch.uint8, device=q.device), need
 
 
 # --- forward -------------------------------------------------------------------
 
 def _forward(q, k, v, table, bias, key_lens, key_mask, scale, out, lse, want_lse, workspace):
-    key_mask = _check_keys(key_lens, key_mask, q, k)
+    dev = _check_tensors(q, k, v)
+    mask_stride = 0
+    if key_lens is not None or key_mask is not None:
+        mask_stride = _check_keys(key_lens, key_mask, q, k, dev)
+    given = _NO_OUTPUTS if out is None else (_check_like(out, q, "out"), None, None, None)
+    plan = _plan(False, _DTYPES[q.dtype], (q.shape, k.shape, v.shape), (q.stride(), k.stride(), v.stride()), given,
+                 0.0 if scale is None else float(scale), mask_stride, bias)
     if out is None:
-        out = _like(q)
-    else:
-        _check_like(out, q.shape, q, "out")
+        out = _new(q)
     if lse is not None:
         _check_lse(lse, q)
     elif want_lse:
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
-    prob, ref, need = _plan(False, _DTYPES[q.dtype], tuple(q.shape), tuple(k.shape),
-                            0.0 if scale is None else float(scale), (_strides(q), _strides(k), _strides(v), _strides(out)),
-                            0 if key_mask is None else key_mask.stride(0), bias)
-    workspace, ws_bytes = _scratch(workspace, need, q.device)
+        lse = q.new_empty(plan.rows, dtype=torch.float32)
+    workspace, ws_bytes = _scratch(workspace, plan.need, q)
     lib = load_library()
     if bias is None:
-        _check(lib.adaspa_cross_attn(prob, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(key_lens), _ptr(key_mask),
-                                     out.data_ptr(), _ptr(lse), _ptr(workspace), ws_bytes, _stream(q.device)))
+        status = lib.adaspa_cross_attn(plan.prob, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(key_lens),
+                                       _ptr(key_mask), out.data_ptr(), _ptr(lse), _ptr(workspace), ws_bytes,
+                                       _stream(q.device))
     else:
-        _check(lib.adaspa_rel_bias_attn(prob, ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
-                                        _ptr(key_lens), _ptr(key_mask), out.data_ptr(), _ptr(lse), _ptr(workspace),
-                                        ws_bytes, _stream(q.device)))
+        status = lib.adaspa_rel_bias_attn(plan.prob, plan.bias, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                          table.data_ptr(), _ptr(key_lens), _ptr(key_mask), out.data_ptr(), _ptr(lse),
+                                          _ptr(workspace), ws_bytes, _stream(q.device))
+    _check(status)
     return out, lse
-
-
-def _dense(t):
-    """Whether t's rows can be written as they lie: D contiguous, no two
-    elements in one place (as in an expanded tensor)."""
-    s = t.stride()
-    return s[3] == 1 and not (s[0] | s[1] | s[2]) & 7 and all(a >= t.shape[3] or n <= 1 for a, n in zip(s[:3], t.shape))
-
-
-def _like(t):
-    """A new tensor of t's shape, and of its layout where that is dense."""
-    return torch.empty_like(t) if _dense(t) else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def cross_attn(q, k, v, *, key_lens=None, key_mask=None, scale: Optional[float] = None, out=None, lse=None,
@@ -232,7 +259,6 @@ def cross_attn(q, k, v, *, key_lens=None, key_mask=None, scale: Optional[float] 
     takes no part.  ``workspace`` (at least :func:`cross_attn_workspace` bytes,
     any type) is allocated here when not given and needed: few query rows
     split their keys over workgroups."""
-    _check_tensors(q, k, v)
     return _forward(q, k, v, None, None, key_lens, key_mask, scale, out, lse, want_lse, workspace)
 
 
@@ -247,7 +273,6 @@ def rel_bias_attn(q, k, v, table, *, max_distance: int = 128, bidirectional: boo
     them.  Query i stands at position i + ``q_offset`` among the keys; "end"
     puts a sample's queries at its last positions (decoding with a cache: one
     query over key_lens[b] keys).  Returns (out, lse)."""
-    _check_tensors(q, k, v)
     bias = _bias_key(q, k, table, max_distance, bidirectional, causal, q_offset)
     return _forward(q, k, v, table, bias, key_lens, key_mask, scale, out, lse, want_lse, workspace)
 
@@ -255,29 +280,29 @@ def rel_bias_attn(q, k, v, table, *, max_distance: int = 128, bidirectional: boo
 # --- backward ------------------------------------------------------------------
 
 def _backward(dout, q, k, v, table, bias, out, lse, key_lens, key_mask, scale, dq, dk, dv, workspace):
-    key_mask = _check_keys(key_lens, key_mask, q, k)
-    _check_like(out, q.shape, q, "out")
-    _check_like(dout, q.shape, q, "dout")
+    dev = _check_tensors(q, k, v)
+    mask_stride = 0
+    if key_lens is not None or key_mask is not None:
+        mask_stride = _check_keys(key_lens, key_mask, q, k, dev)
     _check_lse(lse, q)
-    given = (("dq", dq, q), ("dk", dk, k), ("dv", dv, v))
-    for name, g, t in given:
-        if g is not None:
-            _check_like(g, t.shape, q, name)
-    dq, dk, dv = (_like(t) if g is None else g for _, g, t in given)
-    prob, ref, need = _plan(True, _DTYPES[q.dtype], tuple(q.shape), tuple(k.shape),
-                            0.0 if scale is None else float(scale),
-                            tuple(map(_strides, (q, k, v, out, dout, dq, dk, dv))),
-                            0 if key_mask is None else key_mask.stride(0), bias)
-    workspace, ws_bytes = _scratch(workspace, need, q.device)
+    g = _check_like(dout, q, "dout")
+    given = (_check_like(out, q, "out"),) + tuple(
+        None if x is None else _check_like(x, t, n) for x, t, n in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
+    plan = _plan(True, _DTYPES[q.dtype], (q.shape, k.shape, v.shape, q.shape), (q.stride(), k.stride(), v.stride(), g),
+                 given, 0.0 if scale is None else float(scale), mask_stride, bias)
+    dq = _new(q) if dq is None else dq
+    dk = _new(k) if dk is None else dk
+    dv = _new(v) if dv is None else dv
+    workspace, ws_bytes = _scratch(workspace, plan.need, q)
     lib = load_library()
     if bias is None:
-        _check(lib.adaspa_cross_attn_bwd(prob, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        _check(lib.adaspa_cross_attn_bwd(plan.prob, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                          _ptr(key_lens), _ptr(key_mask), out.data_ptr(), lse.data_ptr(), dq.data_ptr(),
                                          dk.data_ptr(), dv.data_ptr(), _ptr(workspace), ws_bytes, _stream(q.device)))
         return dq, dk, dv
     dtable = torch.empty_like(table)
-    _check(lib.adaspa_rel_bias_attn_bwd(prob, ref, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                        table.data_ptr(), _ptr(key_lens), _ptr(key_mask), out.data_ptr(),
+    _check(lib.adaspa_rel_bias_attn_bwd(plan.prob, plan.bias, dout.data_ptr(), q.data_ptr(), k.data_ptr(),
+                                        v.data_ptr(), table.data_ptr(), _ptr(key_lens), _ptr(key_mask), out.data_ptr(),
                                         lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dtable.data_ptr(),
                                         _ptr(workspace), ws_bytes, _stream(q.device)))
     return dq, dk, dv, dtable
@@ -289,7 +314,6 @@ def cross_attn_bwd(dout, q, k, v, out, lse, *, key_lens=None, key_mask=None, sca
     output; ``out`` and ``lse`` are what it returned, the other arguments what
     it was given.  dk and dv are sums over the query heads that share a key
     head, and 0 for masked keys."""
-    _check_tensors(q, k, v)
     return _backward(dout, q, k, v, None, None, out, lse, key_lens, key_mask, scale, dq, dk, dv, workspace)
 
 
@@ -299,22 +323,16 @@ def rel_bias_attn_bwd(dout, q, k, v, table, out, lse, *, max_distance: int = 128
     """Gradients (dq, dk, dv, dtable) of :func:`rel_bias_attn`; dtable, of the
     table's shape and type, is the sum over samples and over the pairs of each
     bucket."""
-    _check_tensors(q, k, v)
     bias = _bias_key(q, k, table, max_distance, bidirectional, causal, q_offset)
     return _backward(dout, q, k, v, table, bias, out, lse, key_lens, key_mask, scale, dq, dk, dv, workspace)
 
 
 # --- workspaces ----------------------------------------------------------------
 
-def _contiguous(shape):
-    B, H, L, D = shape
-    return (H * L * D, L * D, D, 1)
-
-
 def _workspace(bwd, q_shape, k_shape, bias):
     qs, ks = tuple(map(index, q_shape)), tuple(map(index, k_shape))
     a, c = _contiguous(qs), _contiguous(ks)
-    return _plan(bwd, 0, qs, ks, 0.0, (a, c, c, a, a, a, c, c), 0, bias)[2]
+    return _plan(bwd, 0, (qs, ks, ks), (a, c, c), _NO_OUTPUTS, 0.0, 0, bias).need
 
 
 def cross_attn_workspace(q_shape, k_shape) -> int:
@@ -345,8 +363,11 @@ def rel_bias_attn_bwd_workspace(q_shape, k_shape, num_buckets: int, *, max_dista
 
 def _rows(t):
     """t itself where the kernels can read it as it lies, else a copy."""
-    s = _strides(t)
-    return t if s[3] == 1 and not (s[0] | s[1] | s[2]) & 7 and t.data_ptr() % 16 == 0 else t.contiguous()
+    try:
+        _steps(t.shape, t.stride())
+    except AdaspaError:
+        return t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.contiguous()
 
 
 class _CrossAttention(torch.autograd.Function):
