@@ -48,9 +48,7 @@ struct CrossParams {
   float2* row_ld;                      // backward: [B*H*Lq] log2-LSE (+inf for an empty row) and delta
   float* part_kv;                      // backward: [splits, 2, B*Hk*Lk, D]
   int kv_splits;
-  float* part_t;                       // backward: [B*H, bands * band_splits, buckets] sums of dS near the diagonal
-  float* part_f;                       // backward: [B*H, row tiles * splits, 2] sums of dS beyond far on either side
-  int bands, band_splits;
+  float* part_t;                       // backward: [B*H, key tiles * kv_splits, buckets] sums of dS
   int n_wg;                            // workgroups (set by the launcher)
   RelBias rb;
 };
@@ -58,11 +56,9 @@ struct CrossParams {
 // Row tiles, splits and scratch of a call: by its shape alone, so that a
 // workspace size, the launches and the results follow the shape.
 struct CrossPlan {
-  bool resident;                       // forward: the keys of a head stay in LDS
-  int chunks;                          // resident: workgroups per (sample, key head)
+  bool resident;                       // forward: the keys of a head stay in LDS, splits workgroups share its rows
   int splits, kv_splits;
-  int64_t part_o, part_ml, row_ld, part_kv, part_t, part_f;   // byte offsets into the workspace
-  int bands, band_splits;              // backward: diagonals of 32 x 32 blocks within far, workgroups of each
+  int64_t part_o, part_ml, row_ld, part_kv, part_t;   // byte offsets into the workspace
   int64_t bytes;
 };
 CrossPlan plan_fwd(const CrossParams& p, int D, bool bias);

@@ -187,7 +187,6 @@ adaspa_status backward(const adaspa_cross_problem* prob, const adaspa_rel_bias* 
   c.part_o = (float*)(ws + plan.part_o);
   c.part_kv = (float*)(ws + plan.part_kv);
   c.part_t = (float*)(ws + plan.part_t);
-  c.part_f = (float*)(ws + plan.part_f);
   return launch_cross_bwd(c, prob->head_dim, prob->dtype == ADASPA_FP16, with_bias, plan, (hipStream_t)stream) ==
                  hipSuccess
              ? ADASPA_OK

@@ -7,8 +7,8 @@
 //
 // Two kernels, each with its own axis in registers: cross_dq_kernel walks the
 // keys for 128 query rows, cross_dkv_kernel the queries for its keys.  Both
-// form S and dP again.  The table's gradient comes from cross_band_kernel near
-// the diagonal and from cross_dq_kernel beyond the last bucket's start.  No sum is added
+// form S and dP again.  The table's gradient is added up in cross_dkv_kernel:
+// its delta is the exact one.  No sum is added
 // to memory by more than one workgroup: partial sums go to the workspace and
 // are added in a fixed order, so results are the same from call to call.
 #include "cross_tile.hpp"
@@ -45,8 +45,6 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   const int nt = (kend + 63) / 64;
   const int t0 = (int)((int64_t)nt * split / p.splits), t1 = (int)((int64_t)nt * (split + 1) / p.splits);
 
-  // Sums of dS and P over the blocks of 32 keys beyond far on either side.
-  float below_ds = 0.f, below_p = 0.f, above_ds = 0.f, above_p = 0.f;
   if (BIAS) {
     fill_bias<T, 256>(bt, reinterpret_cast<uint16_t*>(ring), p, unit % p.H, tid);
     __syncthreads();
@@ -83,9 +81,9 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     const uint32_t dst = lds_addr(ring[t & 1]);
     lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
     lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
-    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, lane);
+    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, fresh(lane));
   };
-  const int ka = row_lane<D>(c32, hw), ca = col_lane<D>(lane);
+  const int ka0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
   const int rel0 = 4 * hw - (ro.i + off);
 
   if (t0 < t1) issue(t0);
@@ -94,12 +92,13 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb != 0) : ~0ull);
     __syncthreads();
     if (t + 1 < t1) issue(t + 1);
+    const int ka = fresh(ka0), ca = fresh(ca0);
     u16* sK = ring[t & 1];
     u16* sV = sK + KE;
     if (keep != ~0ull) {
       if (keep == 0) continue;
-      clear_rows<D, 256>(sK, keep, tid);
-      clear_rows<D, 256>(sV, keep, tid);
+      clear_rows<D, 256>(sK, keep, fresh(tid));
+      clear_rows<D, 256>(sV, keep, fresh(tid));
       __syncthreads();
     }
     const int far = BIAS ? p.rb.far : 0, rel = rel0 + t * 64;
@@ -148,21 +147,6 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
       }
 #pragma unroll
       for (int e = 0; e < 16; e += 2) w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
-      if (beyond) {
-        float sd = 0.f, sp = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          sd += y[e];
-          sp += x[e];
-        }
-        if (above) {
-          above_ds += sd;
-          above_p += sp;
-        } else {
-          below_ds += sd;
-          below_p += sp;
-        }
-      }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const typename T::x8 ds = __builtin_bit_cast(typename T::x8, w[s]);
@@ -179,122 +163,55 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   } else {
     store_tile<T, D>(acc, p.scale, p.dq + ro.b * p.sdq.b + ro.h * p.sdq.h + ro.i * p.sdq.t, row_ok, hw);
   }
-  // What the other kernels take as delta: the sum of P dP, free of the output's
+  // What cross_dkv_kernel takes as delta: the sum of P dP, free of the output's
   // rounding; where the keys are split, the one from the rounded output.
-  const float change = p.splits > 1 ? 0.f : both_halves_sum(exact) - delta;
-  if (p.splits == 1 && row_ok && hw == 0) p.row_ld[row] = make_float2(lse2, delta + change);
-  if (!BIAS) return;
-
-  // This workgroup's share of the table's last buckets.
-  float* sums = reinterpret_cast<float*>(ring);
-  __syncthreads();                                        // the ring is free
-  const float below = wave_sum(below_ds - change * below_p), above = wave_sum(above_ds - change * above_p);
-  if (lane == 0) {
-    sums[wave] = below;
-    sums[4 + wave] = above;
-  }
-  __syncthreads();
-  if (tid < 2)
-    p.part_f[(((int64_t)unit * n_rt + r0 / kDqRows) * p.splits + split) * 2 + tid] =
-        (sums[4 * tid] + sums[4 * tid + 1]) + (sums[4 * tid + 2] + sums[4 * tid + 3]);
+  exact = both_halves_sum(exact);
+  if (p.splits == 1 && row_ok && hw == 0) p.row_ld[row] = make_float2(lse2, exact);
 }
 
-// Sums of dS by bucket near the diagonal: a workgroup takes the 32 x 32 blocks
-// of one diagonal of blocks, o = first key - first query (or every
-// band_splits-th four of them), each wave every fourth.  Blocks of one
-// diagonal meet element by element, so their dS are added up in registers, and
-// only the sum is folded: 63 diagonals, then their buckets.  (Adding each
-// block's dS to sums per diagonal in LDS instead took 3/4 of cross_dq_kernel's
-// time: 439 us of 580 at 12 heads x 4,095 tokens, d 128.)  S and dP are formed
-// once more, but for these blocks alone, operands straight from memory.
-template <class T, int D>
-__global__ __launch_bounds__(256) void cross_band_kernel(const CrossParams p) {
-  constexpr int PITCH = 36;                               // floats per row of a folded block
-  __shared__ __attribute__((aligned(16))) float fold[4][32 * PITCH];
-  __shared__ float diag[4][64];
-  __shared__ int of[64];
-  __shared__ uint16_t start[kMaxBucketSide];
-  extern __shared__ __attribute__((aligned(16))) float bt[];
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int hw = lane >> 5, c32 = lane & 31;
-  const int part = blockIdx.x % p.band_splits, band = blockIdx.x / p.band_splits % p.bands;
-  const int unit = blockIdx.x / (p.band_splits * p.bands), b = unit / p.H, h = unit % p.H, hk = h / p.G;
-  const int n = key_count(p, b), off = query_offset(p, n), far = p.rb.far;
-
-  // Diagonals of blocks with a pair nearer than far: off - far - 31 < o < off + far + 31.
-  const int lowest = off - far - 30;
-  const int o = (lowest >= 0 ? (lowest + 31) / 32 : -(-lowest / 32)) * 32 + band * 32;
-  const bool used = o < off + far + 31 && !(p.rb.causal && o - 31 - off > 0);
-  f32x16 acc = f32x16{};
-  if (used) {
-    fill_bias<T, 256>(bt, start, p, h, tid);
-    __syncthreads();
-    // Query blocks i whose key block i + o / 32 has keys.
-    const int first = o < 0 ? -o / 32 : 0, nq = (p.Lq + 31) / 32, nk = (n + 31) / 32 - o / 32;
-    const int last = nq < nk ? nq : nk;
-    const u16* qh = p.q + b * p.sq.b + h * p.sq.h;
-    const u16* gh = p.dout + b * p.sdo.b + h * p.sdo.h;
-    const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
-    const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
-    const float* at = bt + 4 * hw - c32 + o - off + far + kPad;
-    for (int ib = first + part * 4 + wave; ib < last; ib += 4 * p.band_splits) {
-      const int i = ib * 32 + c32, j0 = ib * 32 + o, key = j0 + c32;
-      const bool row_ok = i < p.Lq, key_ok = key < n && !(p.key_mask && p.key_mask[b * p.mask_stride + key] == 0);
-      const uint32_t keep = (uint32_t)__ballot(key_ok) >> (4 * hw);
-      typename T::x8 a[D / 16], c[D / 16];
-      float2 ld = make_float2(INFINITY, 0.f);
-      if (row_ok) ld = p.row_ld[((int64_t)b * p.H + h) * p.Lq + i];
-      f32x16 x = f32x16{}, y = f32x16{};
-      load_row<T, D>(kh + key * p.sk.t, key_ok, hw, a);
-      load_row<T, D>(qh + i * p.sq.t, row_ok, hw, c);
+// Diagonal sums of a 32 x 32 block held as lane (hw, c32) = column c32, element
+// e = row 8 (e / 4) + 4 hw + e % 4, added to `at` (place 31 + column - row).  Row
+// by row, the sum so far moves up one lane and the next row is added, so a
+// diagonal's sum gathers in one lane; four chains of eight rows, since one of
+// 32 would wait for itself.  No two lanes of an addition share a place.
+__device__ __forceinline__ void add_diagonals(const f32x16& x, float* at, int lane) {
+#ifndef CHAIN
+#define CHAIN 32
+#endif
+  float s = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) x = T::mfma(a[ks], c[ks], x);
-      load_row<T, D>(vh + key * p.sv.t, key_ok, hw, a);
-      load_row<T, D>(gh + i * p.sdo.t, row_ok, hw, c);
+  for (int i = 0; i < 4; ++i) {
+    uint32_t row[8];
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) y = T::mfma(a[ks], c[ks], y);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int kk = 8 * (e >> 2) + (e & 3);
-        float s = fmaf(x[e], p.sl2, at[kk] - ld.x);
-        if (!((keep >> kk) & 1) || (p.rb.causal && o - off + kk + 4 * hw - c32 > 0)) s = -INFINITY;
-        acc[e] += fast_exp2(s) * (y[e] - ld.y);
-      }
+    for (int j = 0; j < 4; ++j) {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[4 * i + j]), 0u, false, false);
+      row[j] = r[0];                                      // the lower half's row, nothing above it
+      row[4 + j] = r[1];
     }
-  }
+    if (8 * i % CHAIN == 0) s = 0.f;
 #pragma unroll
-  for (int e = 0; e < 16; e += 4)
-    *reinterpret_cast<f32x4*>(&fold[wave][c32 * PITCH + 2 * e + 4 * hw]) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-  __syncthreads();
-  {
-    // Diagonal d: key = query + d - 31 within the block.
-    const int d = lane;
-    float s = 0.f;
-    for (int r = 0; r < 32; ++r) {
-      const int c = r + d - 31;
-      if (c >= 0 && c < 32) s += fold[wave][r * PITCH + c];
+    for (int j = 0; j < 8; ++j) {
+      const int moved = __builtin_amdgcn_update_dpp(0, __float_as_int(s), 0x138, 0xF, 0xF, true);   // wave_shr:1
+      s = __int_as_float(moved) + __uint_as_float(row[j]);
     }
-    diag[wave][d] = s;
-    if (wave == 0) of[d] = used && d < 63 ? bucket_of(start, p.rb, o - off + d - 31) : -1;
-  }
-  __syncthreads();
-  const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
-  for (int u = tid; u < buckets; u += 256) {
-    float s = 0.f;
-    for (int d = 0; d < 63; ++d)
-      if (of[d] == u) s += (diag[0][d] + diag[1][d]) + (diag[2][d] + diag[3][d]);
-    p.part_t[(int64_t)blockIdx.x * buckets + u] = s;
+    // Lane CHAIN - 1 + column - (row - first row of the chain).
+    if (8 * (i + 1) % CHAIN == 0 && lane < 31 + CHAIN)
+      __hip_atomic_fetch_add(at + 24 - 8 * i + lane, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   }
 }
+constexpr int kDiagPad = 62;           // diagonals of a block near the diagonal that lie beyond far
+__host__ __device__ __forceinline__ int diag_entries(int far) { return 2 * (far + kDiagPad) + 1; }
 
 // dk and dv of 32 keys per wave, over one range of the (query head, 64-row
 // query tile) items that see them.
 template <class T, int D, bool BIAS>
-__global__ __launch_bounds__(64 * kDkvWaves, 1) void cross_dkv_kernel(const CrossParams p) {
+__global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_kernel(const CrossParams p) {
   constexpr int NW = kDkvWaves, NT = 64 * NW, KE = 64 * D;
   __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];      // slots [Q | dO]
   __shared__ __attribute__((aligned(16))) float2 ld[2][64];           // log2-LSE and delta of their rows
-  extern __shared__ __attribute__((aligned(16))) float bt[];
+  __shared__ uint16_t start[kMaxBucketSide];
+  __shared__ float far_sum[2][NW];
+  extern __shared__ __attribute__((aligned(16))) float bt[];          // the bias, then the sums per diagonal
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
 
@@ -323,7 +240,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, 1) void cross_dkv_kernel(const Cros
   TileLoad<D, NW> lq, lg;
   lq.init(wave, lane, p.sq.t);
   lg.init(wave, lane, p.sdo.t);
-  const int ra = row_lane<D>(c32, hw), ca = col_lane<D>(lane);
+  const int ra0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
   float2 mine = make_float2(0.f, 0.f);
   auto issue = [&](int it) {
     const int h = hk * p.G + it / per_head, q0 = (q_first + it % per_head) * 64;
@@ -339,29 +256,74 @@ __global__ __launch_bounds__(64 * kDkvWaves, 1) void cross_dkv_kernel(const Cros
   // were: they have to be numbers, since they meet weights of zero.
   for (int c = tid; c < 2 * 2 * KE / 8; c += NT) *reinterpret_cast<u32x4*>(&ring[0][0] + c * 8) = u32x4{0, 0, 0, 0};
   __syncthreads();
-  int head = -1;
-  if (i0 < i1) {
-    issue(i0);
-    if (tid < 64) ld[i0 & 1][tid] = mine;
+  // Bias: sums of dS by diagonal (each wave its own, so that their order is the
+  // program's) and, beyond far, on either side of it.
+  const int far = BIAS ? p.rb.far : 0, nd = diag_entries(far);
+  float* dg = bt + bias_entries(far) + wave * nd;
+  float below = 0.f, above = 0.f;
+  int head = 0;
+  // The sums of the head that the workgroup leaves become its share of dtable.
+  auto flush = [&]() {
+    const float lo = wave_sum(below), hi = wave_sum(above);
+    below = above = 0.f;
+    if (lane == 0) {
+      far_sum[0][wave] = lo;
+      far_sum[1][wave] = hi;
+    }
+    __syncthreads();
+    float* all = bt + bias_entries(far);
+    for (int i = tid; i < nd; i += NT) {
+      float s = 0.f;
+      for (int w = 0; w < NW; ++w) {
+        s += all[w * nd + i];
+        all[w * nd + i] = 0.f;
+      }
+      bt[i] = s;                                          // the bias is loaded again for the next head
+    }
+    __syncthreads();
+    const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side, mid = far + kDiagPad;
+    float* share = p.part_t + ((((int64_t)b * p.H + hk * p.G + head) * n_kt + j0 / (32 * NW)) * p.kv_splits + split) * buckets;
+    for (int u = wave; u < buckets; u += NW) {
+      const bool ahead = u >= p.rb.side;
+      const int m = ahead ? u - p.rb.side : u;
+      const bool last = m == p.rb.side - 1;
+      int d = start[m];
+      const int d1 = last ? mid + 1 : start[m + 1];
+      if (ahead && d == 0) d = 1;
+      float s = 0.f;
+      for (d += lane; d < d1; d += 64) s += bt[ahead ? mid + d : mid - d];
+      if (!p.rb.both && u == 0)                           // one direction: every key after the query
+        for (int i = mid + 1 + lane; i < nd; i += 64) s += bt[i];
+      s = wave_sum(s);
+      if (last)
+        for (int w = 0; w < NW; ++w) s += far_sum[ahead][w];
+      if (!p.rb.both && u == 0)
+        for (int w = 0; w < NW; ++w) s += far_sum[1][w];
+      if (lane == 0) share[u] = s;
+    }
+    __syncthreads();
+    ++head;
+  };
+  if (i0 < i1) issue(i0);
+  if (BIAS) {
+    for (int i = tid; i < NW * nd; i += NT) bt[bias_entries(far) + i] = 0.f;
+    fill_bias<T, NT>(bt, start, p, hk * p.G, tid);
   }
+  if (i0 < i1 && tid < 64) ld[i0 & 1][tid] = mine;
   for (int it = i0; it < i1; ++it) {
     wait_vmem();
     __syncthreads();
     const int g_head = it / per_head, q0 = (q_first + it % per_head) * 64;
     if (BIAS && g_head != head) {                         // another query head: its own bias
-      __shared__ uint16_t start[kMaxBucketSide];
+      while (head < g_head) flush();
       fill_bias<T, NT>(bt, start, p, hk * p.G + g_head, tid);
-      head = g_head;
       __syncthreads();
     }
     if (it + 1 < i1) issue(it + 1);
+    const int ra = fresh(ra0), ca = fresh(ca0);
     const u16* sQ = ring[it & 1];
     const u16* sG = sQ + KE;
-    const int far = BIAS ? p.rb.far : 0;
-    const int jw = j0 + wave * 32, lo = jw - (q0 + 63 + off), hi = jw + 31 - (q0 + off);
     const int rel = key - (q0 + 4 * hw + off);            // of this lane's first query of the tile
-    const bool beyond = BIAS && (lo >= far || hi <= -far);
-    const float flat = beyond ? bt[lo >= far ? 2 * (far + kPad) : 0] : 0.f;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       f32x16 x = f32x16{}, y = f32x16{};
@@ -370,14 +332,18 @@ __global__ __launch_bounds__(64 * kDkvWaves, 1) void cross_dkv_kernel(const Cros
         x = T::mfma(read_row<T>(sQ + (ra ^ (16 * ks)) + 32 * g * D), kf[ks], x);
         y = T::mfma(read_row<T>(sG + (ra ^ (16 * ks)) + 32 * g * D), vf[ks], y);
       }
+      // The block's smallest and largest key minus query position.
+      const int lo = j0 + wave * 32 - (q0 + 32 * g + 31 + off), hi = lo + 62;
+      const bool right = lo >= far, beyond = right || hi <= -far;
       if (BIAS) {
         if (beyond) {
+          const float c = bt[right ? 2 * (far + kPad) : 0];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, flat);
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, c);
         } else {
-          const float* at = bt + rel + far + kPad;
+          const float* at = bt + rel - 32 * g + far + kPad;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[-(32 * g + 8 * (e >> 2) + (e & 3))]);
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[-(8 * (e >> 2) + (e & 3))]);
         }
         if (p.rb.causal && hi > 0) {
 #pragma unroll
@@ -393,8 +359,22 @@ __global__ __launch_bounds__(64 * kDkvWaves, 1) void cross_dkv_kernel(const Cros
       for (int e = 0; e < 16; e += 2) {
         const f32x4 s = *reinterpret_cast<const f32x4*>(&ld[it & 1][32 * g + 8 * (e >> 2) + 4 * hw + (e & 3)]);
         const float a = fast_exp2(x[e] - s[0]), c = fast_exp2(x[e + 1] - s[2]);
+        y[e] = a * (y[e] - s[1]);
+        y[e + 1] = c * (y[e + 1] - s[3]);
         wp[e >> 3][(e & 7) >> 1] = T::pack(a, c);
-        ws[e >> 3][(e & 7) >> 1] = T::pack(a * (y[e] - s[1]), c * (y[e + 1] - s[3]));
+        ws[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+      }
+      if (BIAS) {
+        if (!key_ok) y = f32x16{};                        // its row of zeros is no key
+        if (beyond) {
+          float s = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s += y[e];
+          if (right) above += s;
+          else below += s;
+        } else {
+          add_diagonals(y, dg + lo + far + kDiagPad, lane);
+        }
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -407,6 +387,10 @@ __global__ __launch_bounds__(64 * kDkvWaves, 1) void cross_dkv_kernel(const Cros
       }
     }
     if (it + 1 < i1 && tid < 64) ld[(it + 1) & 1][tid] = mine;
+  }
+  if (BIAS) {
+    __syncthreads();
+    while (head < p.G) flush();
   }
   // A masked key took part with a row of zeros: its sums are dropped.
   if (!key_ok) {
@@ -446,25 +430,18 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(const float* part, int64
 }
 
 // dtable[u, h]: the shares of head h over samples and workgroups, eight runs of
-// them at a time, each in order; the last buckets also take what lies beyond far.
+// them at a time, each in order.
 template <class T>
-__global__ __launch_bounds__(256) void cross_dtable_kernel(const CrossParams p, int tiles) {
+__global__ __launch_bounds__(256) void cross_dtable_kernel(const CrossParams p, int per) {
   __shared__ float sum[8][32];
   const int h = blockIdx.x, buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
   const int t = threadIdx.x & 31, u = blockIdx.y * 32 + t, part = threadIdx.x >> 5;
   float s = 0.f;
   if (u < buckets) {
-    const int per = p.bands * p.band_splits, n = p.B * per;
+    const int64_t n = (int64_t)p.B * per;
 #pragma unroll 8
-    for (int a = n * part / 8; a < n * (part + 1) / 8; ++a)
-      s += p.part_t[(((int64_t)(a / per) * p.H + h) * per + a % per) * buckets + u];
-    const int m = p.B * tiles;
-    for (int side = 0; side < 2; ++side)
-      if (u == (side == 0 ? p.rb.side - 1 : p.rb.both ? buckets - 1 : 0)) {
-#pragma unroll 8
-        for (int a = (int)((int64_t)m * part / 8); a < (int)((int64_t)m * (part + 1) / 8); ++a)
-          s += p.part_f[(((int64_t)(a / tiles) * p.H + h) * tiles + a % tiles) * 2 + side];
-      }
+    for (int64_t a = n * part / 8; a < n * (part + 1) / 8; ++a)
+      s += p.part_t[((a / per * p.H + h) * per + a % per) * buckets + u];
   }
   sum[part][t] = s;
   __syncthreads();
@@ -501,16 +478,7 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   c.part_kv = off;
   if (c.kv_splits > 1) off += up256((int64_t)c.kv_splits * 2 * p.B * p.Hk * p.Lk * D * 4);
   c.part_t = off;
-  if (bias) {
-    // Multiples of 32 in an open interval of 2 far + 62; as many workgroups for
-    // each as leave a wave eight blocks.
-    const int64_t blocks = (p.Lq < p.Lk ? p.Lq : p.Lk) / 32 + 1;
-    c.bands = (2 * p.rb.far + 61) / 32 + 1;
-    c.band_splits = clamp_splits(blocks / 32, 128);
-    off += up256((int64_t)p.B * p.H * c.bands * c.band_splits * (p.rb.both ? 2 : 1) * p.rb.side * 4);
-    c.part_f = off;
-    off += up256(tiles * c.splits * 8);
-  }
+  if (bias) off += up256(ktiles * p.G * c.kv_splits * (p.rb.both ? 2 : 1) * p.rb.side * 4);
   c.bytes = off;
   return c;
 }
@@ -532,7 +500,8 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   }
   p.n_wg = (int)((int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves)) * p.kv_splits);
   if (p.n_wg > 0) {
-    if (bias) hipLaunchKernelGGL((cross_dkv_kernel<T, D, true>), dim3(p.n_wg), dim3(64 * kDkvWaves), lds, st, p);
+    if (bias) hipLaunchKernelGGL((cross_dkv_kernel<T, D, true>), dim3(p.n_wg), dim3(64 * kDkvWaves),
+                                 lds + kDkvWaves * diag_entries(p.rb.far) * 4, st, p);
     else hipLaunchKernelGGL((cross_dkv_kernel<T, D, false>), dim3(p.n_wg), dim3(64 * kDkvWaves), 0, st, p);
     if (p.kv_splits > 1) {
       const dim3 grid((uint32_t)((keys + per - 1) / per));
@@ -544,12 +513,8 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   }
   if (bias) {
     const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
-    p.bands = c.bands;
-    p.band_splits = c.band_splits;
-    if (p.B > 0)
-      hipLaunchKernelGGL((cross_band_kernel<T, D>), dim3(p.B * p.H * p.bands * p.band_splits), dim3(256), lds, st, p);
     hipLaunchKernelGGL((cross_dtable_kernel<T>), dim3(p.H, (buckets + 31) / 32), dim3(256), 0, st, p,
-                       (int)(rt * p.splits));
+                       (int)((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves) * p.kv_splits));
   }
   return hipGetLastError();
 }

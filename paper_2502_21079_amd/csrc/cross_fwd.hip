@@ -29,15 +29,15 @@ struct Rows {
     m = -INFINITY;
     l = 0.f;
   }
-  // Scores of 64 keys in x (log2 units): weights into pb, their fp32 sum into
-  // l, the accumulator rescaled where the reference moved.
-  __device__ __forceinline__ void weigh(f32x16 (&x)[2], typename T::x8 (&pb)[2][2]) {
+  // Scores of 64 keys in x (sl2 x in log2 units): weights into pb, their fp32
+  // sum into l, the accumulator rescaled where the reference moved.
+  __device__ __forceinline__ void weigh(const f32x16 (&x)[2], float sl2, typename T::x8 (&pb)[2][2]) {
     float mt = -INFINITY;
 #pragma unroll
     for (int g = 0; g < 2; ++g)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) mt = vmax(mt, vmax(x[g][e], x[g][e + 1]));
-    mt = both_halves_max(mt);
+    mt = both_halves_max(mt) * sl2;
     // Also where the maximum is NaN: the row becomes NaN.
     const bool move = !(mt <= m + kMaxRise) && mt != -INFINITY;
     if (__any(move)) {
@@ -50,14 +50,14 @@ struct Rows {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] *= a;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+    const float ref = m == -INFINITY ? 0.f : -m;
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       u32x4 w[2];
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const float a = fast_exp2(x[g][e] - ref), b = fast_exp2(x[g][e + 1] - ref);
+        const float a = fast_exp2(fmaf(x[g][e], sl2, ref)), b = fast_exp2(fmaf(x[g][e + 1], sl2, ref));
         s0 += a;
         s1 += b;
         w[e >> 3][(e & 7) >> 1] = T::pack(a, b);
@@ -118,9 +118,9 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
     const uint32_t dst = lds_addr(ring[t & 1]);
     lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
     lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
-    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, lane);
+    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, fresh(lane));
   };
-  const int ka = row_lane<D>(c32, hw), ca = col_lane<D>(lane);
+  const int ka0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
   // Key minus query position of this lane's first key of tile 0.
   const int rel0 = 4 * hw - (ro.i + off);
 
@@ -130,11 +130,12 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
     const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb != 0) : ~0ull);
     __syncthreads();
     if (t + 1 < t1) issue(t + 1);
+    const int ka = fresh(ka0), ca = fresh(ca0);
     u16* sK = ring[t & 1];
     u16* sV = sK + KE;
     if (keep != ~0ull) {
       if (keep == 0) continue;
-      clear_rows<D, 256>(sV, keep, tid);
+      clear_rows<D, 256>(sV, keep, fresh(tid));
       __syncthreads();
     }
     f32x16 x[2];
@@ -161,11 +162,6 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[g][e] = fmaf(x[g][e], p.sl2, at[32 * g + 8 * (e >> 2) + (e & 3)]);
       }
-    } else {
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[g][e] *= p.sl2;
     }
     if (keep != ~0ull) {
       const uint64_t mine = keep >> (4 * hw);
@@ -183,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
           if (rel + 32 * g + 8 * (e >> 2) + (e & 3) > 0) x[g][e] = -INFINITY;
     }
     typename T::x8 pb[2][2];
-    acc.weigh(x, pb);
+    acc.weigh(x, BIAS ? 1.f : p.sl2, pb);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -201,6 +197,105 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
   }
   store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, p.out + ro.b * p.so.b + ro.h * p.so.h + ro.i * p.so.t, row_ok, hw);
   if (p.lse && row_ok && hw == 0) p.lse[row] = l == 0.f ? -INFINITY : (acc.m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Few keys, many rows: the keys and values of one (sample, key head) stay in
+// LDS, and each wave walks row tiles of 32 on its own, without barriers; the
+// next tile's queries are loaded while one is worked on.
+constexpr int kKeepBytes = 131072;     // of K and V
+template <int D>
+constexpr int kKeepWaves = D == 64 ? 16 : 8;
+
+template <class T, int D>
+__global__ __launch_bounds__(64 * kKeepWaves<D>, kKeepWaves<D> / 4) void cross_keep_kernel(const CrossParams p) {
+  constexpr int NW = kKeepWaves<D>, NT = 64 * NW, CPR = D / 8, RPI = 64 / CPR;
+  extern __shared__ __attribute__((aligned(1024))) u16 keep_lds[];     // [K | V | 0 or -inf per key]
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+  const int lid = xcd_remap(blockIdx.x, p.n_wg);
+  const int unit = lid / p.splits, chunk = lid % p.splits;
+  const int b = unit / p.Hk, hk = unit % p.Hk, n = key_count(p, b), nt = (n + 63) / 64;
+  const int n_rows = p.G * p.Lq, n_rt = (n_rows + 31) / 32;
+  const int rt1 = (int)((int64_t)n_rt * (chunk + 1) / p.splits);
+  int rt = (int)((int64_t)n_rt * chunk / p.splits) + wave;
+
+  u16* sK = keep_lds;
+  u16* sV = sK + nt * 64 * D;
+  float* sB = reinterpret_cast<float*>(sV + nt * 64 * D);
+  const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+  const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+  // Rows past n and masked rows become zeros; the others come straight in.
+  for (int i = wave; i < nt * 64 / RPI; i += NW) {
+    const int row = i * RPI + lane / CPR, chunk16 = (lane % CPR) ^ row_order<D>(row);
+    const bool ok = row < n && !(p.key_mask && p.key_mask[b * p.mask_stride + row] == 0);
+    u32x4 wk = {0, 0, 0, 0}, wv = {0, 0, 0, 0};
+    if (ok) {
+      wk = *reinterpret_cast<const u32x4*>(kh + row * p.sk.t + chunk16 * 8);
+      wv = *reinterpret_cast<const u32x4*>(vh + row * p.sv.t + chunk16 * 8);
+    }
+    *reinterpret_cast<u32x4*>(sK + i * 512 + lane * 8) = wk;
+    *reinterpret_cast<u32x4*>(sV + i * 512 + lane * 8) = wv;
+  }
+  uint32_t whole = 0;                                    // tiles whose 64 keys are all visible
+  for (int t = 0; t < nt; ++t) {
+    const int key = t * 64 + lane;
+    const bool ok = key < n && !(p.key_mask && p.key_mask[b * p.mask_stride + key] == 0);
+    if (__ballot(ok) == ~0ull) whole |= 1u << t;
+    else if (wave == 0) sB[key] = ok ? 0.f : -INFINITY;
+  }
+  __syncthreads();
+
+  const int ka0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
+  typename T::x8 qf[D / 16], qn[D / 16];
+  auto fetch = [&](int rt, RowOf& ro, bool& ok) {
+    const int r = rt * 32 + c32;
+    ok = r < n_rows;
+    ro = row_of<false>(p, unit, ok ? r : 0);
+    load_row<T, D>(p.q + ro.b * p.sq.b + ro.h * p.sq.h + ro.i * p.sq.t, ok, hw, qn);
+  };
+  RowOf ro_n;
+  bool ok_n = false;
+  if (rt < rt1) fetch(rt, ro_n, ok_n);
+  for (; rt < rt1; rt += NW) {
+    const RowOf ro = ro_n;
+    const bool row_ok = ok_n;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = qn[ks];
+    if (rt + NW < rt1) fetch(rt + NW, ro_n, ok_n);
+    Rows<T, D> acc;
+    acc.init();
+    for (int t = 0; t < nt; ++t) {
+      const int ka = fresh(ka0), ca = fresh(ca0);
+      const u16* tK = sK + t * 64 * D;
+      const u16* tV = sV + t * 64 * D;
+      f32x16 x[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        x[g] = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+          x[g] = T::mfma(read_row<T>(tK + (ka ^ (16 * ks)) + 32 * g * D), qf[ks], x[g]);
+      }
+      if (!((whole >> t) & 1)) {
+        const float* at = sB + t * 64 + 4 * hw;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[g][e] += at[32 * g + 8 * (e >> 2) + (e & 3)];
+      }
+      typename T::x8 pb[2][2];
+      acc.weigh(x, p.sl2, pb);
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          acc.o[d] = T::mfma(read_col<T, D>(tV, ca, d, 16 * s), pb[s >> 1][s & 1], acc.o[d]);
+    }
+    const float l = both_halves_sum(acc.l);
+    store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, p.out + ro.b * p.so.b + ro.h * p.so.h + ro.i * p.so.t, row_ok, hw);
+    if (p.lse && row_ok && hw == 0)
+      p.lse[((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i] = l == 0.f ? -INFINITY : (acc.m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
 }
 
 // Joins the ranges of a split call: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
@@ -259,6 +354,22 @@ CrossPlan plan_fwd(const CrossParams& p, int D, bool bias) {
   CrossPlan c{};
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rows = bias ? p.Lq : (int64_t)p.G * p.Lq;
   const int64_t tiles = units * ((rows + kRows - 1) / kRows), nt = (p.Lk + 63) / 64;
+  // Rows enough for two tiles a wave on every CU, keys few enough for LDS: the
+  // keys stay there, and a unit's rows are shared among as many workgroups as
+  // fill the rounds of 256 best (one workgroup's loading counts as three tiles).
+  const int64_t waves = D == 64 ? kKeepWaves<64> : kKeepWaves<128>, rt = (rows + 31) / 32;
+  c.resident = !bias && nt * 64 * D * 4 <= kKeepBytes && units * rt >= 512 * waves;
+  if (c.resident) {
+    int64_t best = -1;
+    for (int64_t n = 1; n <= 256 && n * waves <= rt + waves; ++n) {
+      const int64_t cost = (units * n + 255) / 256 * ((rt + n * waves - 1) / (n * waves) + 3);
+      if (best < 0 || cost < best) {
+        best = cost;
+        c.splits = (int)n;
+      }
+    }
+    return c;
+  }
   // Keys are split where the row tiles alone leave CUs without work, into
   // ranges of no less than four tiles.
   int64_t s = tiles > 0 && tiles < 256 ? 512 / tiles : 1;
@@ -276,6 +387,12 @@ template <class T, int D>
 static hipError_t run_fwd(CrossParams p, bool bias, const CrossPlan& c, hipStream_t st) {
   p.splits = c.splits;
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rows = bias ? p.Lq : (int64_t)p.G * p.Lq;
+  if (c.resident) {
+    p.n_wg = (int)(units * p.splits);
+    const uint32_t lds = (uint32_t)((p.Lk + 63) / 64 * 64 * (D * 4 + 4));
+    hipLaunchKernelGGL((cross_keep_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves<D>), lds, st, p);
+    return hipGetLastError();
+  }
   p.n_wg = (int)(units * ((rows + kRows - 1) / kRows) * p.splits);
   if (p.n_wg == 0) return hipSuccess;
   if (bias)

@@ -107,6 +107,14 @@ struct TileLoad {
   }
 };
 
+// A value that the compiler takes as new at this point: what is derived from it
+// inside a loop is formed there (a few VALU operations) instead of being kept
+// in registers, or spilled, over the whole loop.
+__device__ __forceinline__ int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 // Clears rows of a tile whose bit in `keep` is 0 (rows below n), so that
 // whatever a masked row holds, infinities and NaN too, meets a weight of zero
 // as zero.
