@@ -45,7 +45,7 @@ struct CrossParams {
   int splits;                          // ranges that an axis is divided into
   float* part_o;                       // forward: [splits, B*H*Lq, D]; backward dq: the same
   float* part_ml;                      // forward: [splits, B*H*Lq, 2] reference and sum
-  float2* row_ld;                      // backward: [B*H*Lq] log2-LSE (+inf for an empty row) and delta
+  float2* row_ld;                      // backward: [B*H*Lq] -LSE / scale (-inf for an empty row) and -delta
   float* part_kv;                      // backward: [splits, 2, B*Hk*Lk, D]
   int kv_splits;
   float* part_t;                       // backward: [B*H, key tiles * kv_splits, buckets] sums of dS

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     delta = both_halves_sum(delta);
     const float z = row_ok ? p.lse[row] : -INFINITY;
     if (z != -INFINITY) lse2 = z * kLog2e;
-    if (p.splits > 1 && row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(lse2, delta);
+    if (p.splits > 1 && row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(-lse2 / p.sl2, -delta);
   }
   float exact = 0.f;                                       // delta again, as the sum of P dP in fp32
 
@@ -133,11 +133,6 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
         for (int e = 0; e < 16; ++e)
           if (!((mine >> (8 * (e >> 2) + (e & 3))) & 1)) x[e] = -INFINITY;
       }
-      if (BIAS && p.rb.causal && hi > 0) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (rel + 32 * g + 8 * (e >> 2) + (e & 3) > 0) x[e] = -INFINITY;
-      }
       u32x4 w[2];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -166,49 +161,56 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   // What cross_dkv_kernel takes as delta: the sum of P dP, free of the output's
   // rounding; where the keys are split, the one from the rounded output.
   exact = both_halves_sum(exact);
-  if (p.splits == 1 && row_ok && hw == 0) p.row_ld[row] = make_float2(lse2, exact);
+  if (p.splits == 1 && row_ok && hw == 0) p.row_ld[row] = make_float2(-lse2 / p.sl2, -exact);
 }
 
 // Diagonal sums of a 32 x 32 block held as lane (hw, c32) = column c32, element
-// e = row 8 (e / 4) + 4 hw + e % 4, added to `at` (place 31 + column - row).  Row
-// by row, the sum so far moves up one lane and the next row is added, so a
-// diagonal's sum gathers in one lane; four chains of eight rows, since one of
-// 32 would wait for itself.  No two lanes of an addition share a place.
+// e = row 8 (e / 4) + 4 hw + e % 4, added to at[31 + column - row].  Row by row,
+// the sum so far moves up one lane and the next row is added, so a diagonal's
+// sum gathers in one lane: two chains of 16 rows side by side, the first one's
+// then moved up by 16 lanes.
 __device__ __forceinline__ void add_diagonals(const f32x16& x, float* at, int lane) {
-#ifndef CHAIN
-#define CHAIN 32
-#endif
-  float s = 0.f;
+  uint32_t row[32];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t row[8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[4 * i + j]), 0u, false, false);
-      row[j] = r[0];                                      // the lower half's row, nothing above it
-      row[4 + j] = r[1];
-    }
-    if (8 * i % CHAIN == 0) s = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int moved = __builtin_amdgcn_update_dpp(0, __float_as_int(s), 0x138, 0xF, 0xF, true);   // wave_shr:1
-      s = __int_as_float(moved) + __uint_as_float(row[j]);
-    }
-    // Lane CHAIN - 1 + column - (row - first row of the chain).
-    if (8 * (i + 1) % CHAIN == 0 && lane < 31 + CHAIN)
-      __hip_atomic_fetch_add(at + 24 - 8 * i + lane, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  for (int e = 0; e < 16; ++e) {
+    const int r = 8 * (e >> 2) + (e & 3);
+    const auto v = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[e]), 0u, false, false);
+    row[r] = v[0];                                        // the lower half's row, nothing above it
+    row[r + 4] = v[1];
   }
+  float s[2] = {__uint_as_float(row[0]), __uint_as_float(row[16])};
+#pragma unroll
+  for (int r = 1; r < 16; ++r)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int moved = __builtin_amdgcn_update_dpp(0, __float_as_int(s[c]), 0x138, 0xF, 0xF, true);   // wave_shr:1
+      s[c] = __int_as_float(moved) + __uint_as_float(row[16 * c + r]);
+    }
+  // Rows of 16 lanes [a0 a1 a2 0] to [0 a0 a1 a2].
+  const auto odd = __builtin_amdgcn_permlane16_swap(0u, __float_as_uint(s[0]), false, false);   // [0 a0 0 a2], [0 a1 0 0]
+  const auto even = __builtin_amdgcn_permlane16_swap(odd[1], 0u, false, false);                 // ..., [a1 0 0 0]
+  const auto third = __builtin_amdgcn_permlane32_swap(0u, even[1], false, false);               // [0 0 a1 0], ...
+  s[1] += __uint_as_float(odd[0]) + __uint_as_float(third[0]);
+  // No two lanes share a place, so the order of a place's additions is the program's.
+  if (lane < 63) __hip_atomic_fetch_add(at + lane, s[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 constexpr int kDiagPad = 62;           // diagonals of a block near the diagonal that lie beyond far
 __host__ __device__ __forceinline__ int diag_entries(int far) { return 2 * (far + kDiagPad) + 1; }
 
 // dk and dv of 32 keys per wave, over one range of the (query head, 64-row
 // query tile) items that see them.
+//
+// Blocks of 32 rows run through three stages: S and dP (MFMA), P and dS (VALU),
+// dv and dk (MFMA).  A step works on the first stage of one block, the second
+// of the one before and the third of the one before that, so that the matrix
+// pipe has work while the VALU does: at d 128 the accumulators leave one wave
+// per SIMD, and no other wave would fill the gaps.  Tiles stay in a ring of
+// three for it.
 template <class T, int D, bool BIAS>
 __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_kernel(const CrossParams p) {
   constexpr int NW = kDkvWaves, NT = 64 * NW, KE = 64 * D;
-  __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];      // slots [Q | dO]
-  __shared__ __attribute__((aligned(16))) float2 ld[2][64];           // log2-LSE and delta of their rows
+  __shared__ __attribute__((aligned(1024))) u16 ring[3][2 * KE];      // slots [Q | dO]
+  __shared__ __attribute__((aligned(16))) float ld[3][2][64];         // -LSE / scale and -delta of their rows
   __shared__ uint16_t start[kMaxBucketSide];
   __shared__ float far_sum[2][NW];
   extern __shared__ __attribute__((aligned(16))) float bt[];          // the bias, then the sums per diagonal
@@ -241,20 +243,44 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
   lq.init(wave, lane, p.sq.t);
   lg.init(wave, lane, p.sdo.t);
   const int ra0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
+  // The item to be loaded next: its head and first row, and where they are.
+  const int q_begin = q_first * 64;
+  int in_h = hk * p.G + (per_head > 0 ? i0 / per_head : 0), in_q = (q_first + (per_head > 0 ? i0 % per_head : 0)) * 64;
+  const u16* qp = p.q + b * p.sq.b + in_h * p.sq.h + in_q * p.sq.t;
+  const u16* gp = p.dout + b * p.sdo.b + in_h * p.sdo.h + in_q * p.sdo.t;
+  const int64_t q_step = 64 * p.sq.t, g_step = 64 * p.sdo.t;
   float2 mine = make_float2(0.f, 0.f);
-  auto issue = [&](int it) {
-    const int h = hk * p.G + it / per_head, q0 = (q_first + it % per_head) * 64;
-    const uint32_t dst = lds_addr(ring[it & 1]);
-    lq.issue(dst, p.q + b * p.sq.b + h * p.sq.h + q0 * p.sq.t, p.sq.t, p.Lq - q0);
-    lg.issue(dst + KE * 2, p.dout + b * p.sdo.b + h * p.sdo.h + q0 * p.sdo.t, p.sdo.t, p.Lq - q0);
+  u32x4 q_buf, g_buf;
+  auto prepare = [&]() {
+    q_buf = lq.buffer(qp, p.sq.t, p.Lq - in_q);
+    g_buf = lg.buffer(gp, p.sdo.t, p.Lq - in_q);
     if (tid < 64) {
-      mine = make_float2(INFINITY, 0.f);                  // past the last row: weight 0
-      if (q0 + tid < p.Lq) mine = p.row_ld[((int64_t)b * p.H + h) * p.Lq + q0 + tid];
+      mine = make_float2(-INFINITY, 0.f);                 // past the last row: weight 0
+      if (in_q + tid < p.Lq) mine = p.row_ld[((int64_t)b * p.H + in_h) * p.Lq + in_q + tid];
+    }
+    in_q += 64;
+    qp += q_step;
+    gp += g_step;
+    if (in_q >= p.Lq) {
+      in_q = q_begin;
+      ++in_h;
+      qp = p.q + b * p.sq.b + in_h * p.sq.h + in_q * p.sq.t;
+      gp = p.dout + b * p.sdo.b + in_h * p.sdo.h + in_q * p.sdo.t;
     }
   };
+  auto slot_addr = [&](int slot) { return (uint32_t)__builtin_amdgcn_readfirstlane(lds_addr(ring[slot])); };
+  auto issue = [&](int slot) {
+    prepare();
+    const uint32_t dst = slot_addr(slot);
+    lq.go(q_buf, dst, lq.rel);
+    lg.go(g_buf, dst + KE * 2, lg.rel);
+  };
   // A tile that ends past the last row leaves those rows of its slot as they
-  // were: they have to be numbers, since they meet weights of zero.
-  for (int c = tid; c < 2 * 2 * KE / 8; c += NT) *reinterpret_cast<u32x4*>(&ring[0][0] + c * 8) = u32x4{0, 0, 0, 0};
+  // were: they have to be numbers, since they meet weights of zero.  So do the
+  // blocks before the first and after the last, and their statistics.
+  if (tid < 64)
+    for (int i = 0; i < 6; ++i) (&ld[0][0][0])[64 * i + tid] = 0.f;
+  for (int c = tid; c < 3 * 2 * KE / 8; c += NT) *reinterpret_cast<u32x4*>(&ring[0][0] + c * 8) = u32x4{0, 0, 0, 0};
   __syncthreads();
   // Bias: sums of dS by diagonal (each wave its own, so that their order is the
   // program's) and, beyond far, on either side of it.
@@ -304,90 +330,213 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
     __syncthreads();
     ++head;
   };
-  if (i0 < i1) issue(i0);
+  f32x16 x, y;                                            // S and dP of the block in the second stage
+  typename T::x8 pf[2], sf[2];                            // P and dS of the one in the third
+#pragma unroll
+  for (int s = 0; s < 2; ++s) pf[s] = sf[s] = typename T::x8{};
+  // The first stage's sums begin at the rows' -LSE / scale and -delta, so that
+  // the second finds S - LSE / scale and dP - delta.
+  auto begin = [&](const float* st, f32x16& xn, f32x16& yn) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(st + 8 * i + 4 * hw);
+      const f32x4 c = *reinterpret_cast<const f32x4*>(st + 64 + 8 * i + 4 * hw);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        xn[4 * i + j] = a[j];
+        yn[4 * i + j] = c[j];
+      }
+    }
+  };
+  auto first = [&](const u16* tile, const float* st, int ra, f32x16& xn, f32x16& yn) {
+    begin(st, xn, yn);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      xn = T::mfma(read_row<T>(tile + (ra ^ (16 * ks))), kf[ks], xn);
+      yn = T::mfma(read_row<T>(tile + KE + (ra ^ (16 * ks))), vf[ks], yn);
+    }
+  };
+  auto third = [&](const u16* tile, int g, int ca) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) {
+        dv[d] = T::mfma(read_col<T, D>(tile + KE, ca, d, 32 * g + 16 * s), pf[s], dv[d]);
+        dk[d] = T::mfma(read_col<T, D>(tile, ca, d, 32 * g + 16 * s), sf[s], dk[d]);
+      }
+  };
+  // One step: block (next, gn) in the first stage, with its rows' statistics st,
+  // the one whose smallest key minus query position is lo in the second, block
+  // (prev, gp) in the third.
+  auto step = [&](auto&& hook, const u16* next, int gn, const float* st, const u16* prev, int gp, int lo) {
+    constexpr int NM = D / 4;                             // slots, one MFMA each: first and third stage in turn
+    constexpr int LA = D == 64 ? 2 : 4;                                 // slots between an operand's read and its use
+    constexpr int PER = NM / 8;                           // slots per pair of rows of the second stage
+    // At d 128 registers are there for the lanes' addresses.
+    const int ra = (D == 64 ? fresh(ra0) : ra0) , ca = D == 64 ? fresh(ca0) : ca0;
+    f32x16 xn, yn;
+    begin(st, xn, yn);
+    typename T::x8 op[NM];
+    auto fetch = [&](int i) {
+      const int j = i >> 1;
+      if ((i & 1) == 0) {
+        op[i] = read_row<T>(next + (j & 1) * KE + 32 * gn * D + (ra ^ (16 * (j >> 1))));
+      } else {
+        const int s = j / (D / 16), d = j % (D / 16) >> 1;
+        op[i] = read_col<T, D>(prev + ((j & 1) ? 0 : KE), ca, d, 32 * gp + 16 * s);
+      }
+    };
+    auto mfma = [&](int i) {
+      const int j = i >> 1;
+      if ((i & 1) == 0) {
+        if (j & 1) yn = T::mfma(op[i], vf[j >> 1], yn);
+        else xn = T::mfma(op[i], kf[j >> 1], xn);
+      } else {
+        const int s = j / (D / 16), d = j % (D / 16) >> 1;
+        if (j & 1) dk[d] = T::mfma(op[i], sf[s], dk[d]);
+        else dv[d] = T::mfma(op[i], pf[s], dv[d]);
+      }
+    };
+    const float* at = bt + bias_entries(far) - 1;         // a masked key's: -inf
+    if (BIAS && key_ok) at = bt + bias_from(lo, far) + far + kPad + 31 + c32 - 4 * hw;
+    // Second stage, pair u: rows r and r + 1 of 8 (e / 4) + 4 hw + e % 4.
+    float bias[16], arg[16];
+    u32x4 wp[2], ws[2];
+    auto biases = [&](int u) {
+      const int e = 2 * u, r = 8 * (e >> 2) + (e & 3);
+      if (BIAS) {
+        bias[e] = at[-r];
+        bias[e + 1] = at[-r - 1];
+      }
+    };
+    auto stage_arg = [&](int u) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        arg[2 * u + k] = BIAS ? fmaf(x[2 * u + k], p.sl2, bias[2 * u + k]) : x[2 * u + k] * p.sl2;
+        pin(arg[2 * u + k]);
+      }
+    };
+    auto stage_exp = [&](int u) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        arg[2 * u + k] = fast_exp2(arg[2 * u + k]);
+        pin(arg[2 * u + k]);
+      }
+    };
+    auto stage_ds = [&](int u) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float v = arg[2 * u + k] * y[2 * u + k];
+        pin(v);
+        y[2 * u + k] = v;
+      }
+    };
+    auto stage_pack = [&](int u) {
+      uint32_t a = T::pack(arg[2 * u], arg[2 * u + 1]), c = T::pack(y[2 * u], y[2 * u + 1]);
+      asm volatile("" : "+v"(a), "+v"(c));
+      wp[u >> 2][u & 3] = a;
+      ws[u >> 2][u & 3] = c;
+    };
+    biases(0);
+#pragma unroll
+    for (int i = 0; i < LA; ++i) fetch(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < NM; ++i) {
+      const int u = i / PER, ph = i % PER;
+      if (i + LA < NM) fetch(i + LA);
+      if (ph == 0 && u + 1 < 8) biases(u + 1);
+      mfma(i);
+      hook(i);
+      if (ph == 0) stage_arg(u);
+      if (ph == 0 && u > 0 && PER == 2) stage_ds(u - 1);
+      if (ph == 1) stage_exp(u);
+      if (ph == 1 && u > 0 && PER == 2) stage_pack(u - 1);
+      if (ph == 2) stage_ds(u);
+      if (ph == 3) stage_pack(u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (PER == 2) {
+      stage_ds(7);
+      stage_pack(7);
+    }
+    if (BIAS) {
+      if (lo >= far || lo <= -far - 62) {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s += y[e];
+        if (lo >= far) above += s;
+        else below += s;
+      } else {
+        add_diagonals(y, dg + lo + far + kDiagPad, lane);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      pf[s] = __builtin_bit_cast(typename T::x8, wp[s]);
+      sf[s] = __builtin_bit_cast(typename T::x8, ws[s]);
+    }
+    x = xn;
+    y = yn;
+  };
+  auto put = [&](int slot) {
+    if (tid < 64) {
+      ld[slot][0][tid] = mine.x;
+      ld[slot][1][tid] = mine.y;
+    }
+  };
+  if (i0 < i1) issue(0);
   if (BIAS) {
     for (int i = tid; i < NW * nd; i += NT) bt[bias_entries(far) + i] = 0.f;
     fill_bias<T, NT>(bt, start, p, hk * p.G, tid);
   }
-  if (i0 < i1 && tid < 64) ld[i0 & 1][tid] = mine;
-  for (int it = i0; it < i1; ++it) {
+  int q0 = in_q, g_head = in_h - hk * p.G;                // of the current item
+  if (i0 < i1) {
+    q0 = (q_first + i0 % per_head) * 64;
+    g_head = i0 / per_head;
+    put(0);
+    if (i0 + 1 < i1) issue(1);
     wait_vmem();
+    if (i0 + 1 < i1) put(1);
     __syncthreads();
-    const int g_head = it / per_head, q0 = (q_first + it % per_head) * 64;
+    first(ring[0], ld[0][0], ra0, x, y);
+  }
+  int slot = 0;                                           // of this item's tile
+  for (int it = i0; it < i1; ++it) {
     if (BIAS && g_head != head) {                         // another query head: its own bias
+      __syncthreads();
       while (head < g_head) flush();
       fill_bias<T, NT>(bt, start, p, hk * p.G + g_head, tid);
       __syncthreads();
     }
-    if (it + 1 < i1) issue(it + 1);
-    const int ra = fresh(ra0), ca = fresh(ca0);
-    const u16* sQ = ring[it & 1];
-    const u16* sG = sQ + KE;
-    const int rel = key - (q0 + 4 * hw + off);            // of this lane's first query of the tile
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      f32x16 x = f32x16{}, y = f32x16{};
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        x = T::mfma(read_row<T>(sQ + (ra ^ (16 * ks)) + 32 * g * D), kf[ks], x);
-        y = T::mfma(read_row<T>(sG + (ra ^ (16 * ks)) + 32 * g * D), vf[ks], y);
-      }
-      // The block's smallest and largest key minus query position.
-      const int lo = j0 + wave * 32 - (q0 + 32 * g + 31 + off), hi = lo + 62;
-      const bool right = lo >= far, beyond = right || hi <= -far;
-      if (BIAS) {
-        if (beyond) {
-          const float c = bt[right ? 2 * (far + kPad) : 0];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, c);
-        } else {
-          const float* at = bt + rel - 32 * g + far + kPad;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[-(8 * (e >> 2) + (e & 3))]);
-        }
-        if (p.rb.causal && hi > 0) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (rel - (32 * g + 8 * (e >> 2) + (e & 3)) > 0) x[e] = -INFINITY;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] *= p.sl2;
-      }
-      u32x4 wp[2], ws[2];
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const f32x4 s = *reinterpret_cast<const f32x4*>(&ld[it & 1][32 * g + 8 * (e >> 2) + 4 * hw + (e & 3)]);
-        const float a = fast_exp2(x[e] - s[0]), c = fast_exp2(x[e + 1] - s[2]);
-        y[e] = a * (y[e] - s[1]);
-        y[e + 1] = c * (y[e + 1] - s[3]);
-        wp[e >> 3][(e & 7) >> 1] = T::pack(a, c);
-        ws[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
-      }
-      if (BIAS) {
-        if (!key_ok) y = f32x16{};                        // its row of zeros is no key
-        if (beyond) {
-          float s = 0.f;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s += y[e];
-          if (right) above += s;
-          else below += s;
-        } else {
-          add_diagonals(y, dg + lo + far + kDiagPad, lane);
-        }
-      }
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const typename T::x8 pf = __builtin_bit_cast(typename T::x8, wp[s]), sf = __builtin_bit_cast(typename T::x8, ws[s]);
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          dv[d] = T::mfma(read_col<T, D>(sG, ca, d, 32 * g + 16 * s), pf, dv[d]);
-          dk[d] = T::mfma(read_col<T, D>(sQ, ca, d, 32 * g + 16 * s), sf, dk[d]);
-        }
-      }
+    const int after = slot == 2 ? 0 : slot + 1, before = slot == 0 ? 2 : slot - 1;
+    const int lo = j0 + wave * 32 - (q0 + 31 + off);
+    step([](int) {}, ring[slot], 1, ld[slot][0] + 32, ring[before], 1, lo);
+    wait_vmem();
+    if (it > i0 && it + 1 < i1) put(after);
+    __syncthreads();
+    // The tile after the next goes to the slot that the first step was the last
+    // to read, one load per slot of the second step.
+    const bool more = it + 2 < i1;
+    if (more) prepare();
+    const uint32_t dst = slot_addr(before);
+    step(
+        [&](int i) {
+          constexpr int PL = TileLoad<D, NW>::PER;
+          if (i < 2 * PL && more) {
+            if (i < PL) lq.issue_n(i, dst, q_buf);
+            else lg.issue_n(i - PL, dst + KE * 2, g_buf);
+          }
+        },
+        ring[after], 0, ld[after][0], ring[slot], 0, lo - 32);
+    slot = after;
+    q0 += 64;
+    if (q0 >= p.Lq) {
+      q0 = q_begin;
+      ++g_head;
     }
-    if (it + 1 < i1 && tid < 64) ld[(it + 1) & 1][tid] = mine;
   }
+  if (i0 < i1) third(ring[slot == 0 ? 2 : slot - 1], 1, ca0);
   if (BIAS) {
     __syncthreads();
     while (head < p.G) flush();
@@ -470,7 +619,23 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   c.splits = tiles > 0 && tiles < 256 ? clamp_splits(512 / tiles, nt / 4) : 1;
   const int64_t ktiles = (int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves));
   const int64_t items = (int64_t)p.G * ((p.Lq + 63) / 64);
-  c.kv_splits = ktiles > 0 && ktiles < 256 ? clamp_splits(512 / ktiles, items / 4) : 1;
+  // Ranges of the queries: rounds of as many workgroups as run at a time (two
+  // per CU at d 64, one at d 128), each item about 1.2 or 2.3 us and three more
+  // for a workgroup's start and end, and the partial sums' way through memory.
+  const double item = D == 64 ? 1.2 : 2.3, at_once = D == 64 ? 512 : 256;
+  double best = 0;
+  c.kv_splits = 1;
+  // (With an order mask the workgroups' lengths differ, and rounds do not end
+  // together: 384 of 12 heads x 4,095 tokens are faster whole, 216 us for 256.)
+  const int64_t most = bias && p.rb.causal && ktiles >= 256 ? 1 : 128;
+  for (int64_t n = 1; n <= most && (n == 1 || n * 2 <= items); ++n) {
+    const double rounds = (double)((int64_t)((ktiles * n + at_once - 1) / at_once)), per = (double)((items + n - 1) / n);
+    const double cost = rounds * (per + 3) * item + (n > 1 ? 8 + n * ((double)p.B * p.Hk * p.Lk * D * 16 / 4.8e6) : 0);
+    if (n == 1 || cost < best) {
+      best = cost;
+      c.kv_splits = (int)n;
+    }
+  }
   const int64_t rows = (int64_t)p.B * p.H * p.Lq;
   int64_t off = up256(rows * 8);                     // row_ld at 0
   c.part_o = off;

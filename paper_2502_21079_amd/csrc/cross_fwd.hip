@@ -171,13 +171,6 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
         for (int e = 0; e < 16; ++e)
           if (!((mine >> (32 * g + 8 * (e >> 2) + (e & 3))) & 1)) x[g][e] = -INFINITY;
     }
-    if (BIAS && p.rb.causal && t * 64 + 63 > r0 + wave * 32 + off) {
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (rel + 32 * g + 8 * (e >> 2) + (e & 3) > 0) x[g][e] = -INFINITY;
-    }
     typename T::x8 pb[2][2];
     acc.weigh(x, BIAS ? 1.f : p.sl2, pb);
 #pragma unroll

@@ -100,10 +100,20 @@ struct TileLoad {
       go<J + 1>(r, dst, off + step);
     }
   }
-  __device__ __forceinline__ void issue(uint32_t dst, const u16* first, int64_t row_stride, int valid) const {
+  __device__ __forceinline__ static u32x4 buffer(const u16* first, int64_t row_stride, int valid) {
     const int n = valid < ROWS ? valid : ROWS;
-    const uint32_t bytes = n <= 0 ? 0u : (uint32_t)((n - 1) * row_stride + D) * 2u;
-    go(rsrc_words(first, bytes), dst, rel);
+    return rsrc_words(first, n <= 0 ? 0u : ((uint32_t)(n - 1) * (uint32_t)row_stride + D) * 2u);
+  }
+  __device__ __forceinline__ void issue(uint32_t dst, const u16* first, int64_t row_stride, int valid) const {
+    go(buffer(first, row_stride, valid), dst, rel);
+  }
+  // Load n of this wave alone (a constant once the caller's loop is unrolled).
+  template <int J = 0>
+  __device__ __forceinline__ void issue_n(int n, uint32_t dst, u32x4 r) const {
+    if constexpr (J < PER) {
+      if (n == J) dma16<J * NW * 1024>(r, dst + wbase, rel + J * step, 0u);
+      else issue_n<J + 1>(n, dst, r);
+    }
   }
 };
 
@@ -146,8 +156,10 @@ __device__ __forceinline__ int mask_byte(const CrossParams& p, int b, int j0, in
 // one head's values, times log2(e), in LDS: rel = -far - kPad .. far + kPad.
 // A wave's tile of 32 x 64 scores spans 95 diagonals, so one that is not
 // wholly beyond far never leaves the table.
+// With `causal` the values of keys after the query are -inf.  Behind the table
+// stand 32 entries of -inf, where a masked key's lane reads.
 constexpr int kPad = 96;
-__host__ __device__ __forceinline__ int bias_entries(int far) { return 2 * (far + kPad) + 1; }
+__host__ __device__ __forceinline__ int bias_entries(int far) { return 2 * (far + kPad) + 1 + 32; }
 
 // Table row of a relative position.
 __device__ __forceinline__ int bucket_of(const uint16_t* start, const RelBias& rb, int rel) {
@@ -172,8 +184,18 @@ __device__ __forceinline__ void fill_bias(float* bt, uint16_t* start, const Cros
   for (int i = tid; i < p.rb.side; i += NT) start[i] = p.rb.start[i];
   __syncthreads();
   const int n = bias_entries(p.rb.far);
-  for (int i = tid; i < n; i += NT)
-    bt[i] = table_value<T>(p.rb, (int64_t)bucket_of(start, p.rb, i - p.rb.far - kPad) * p.H + h) * kLog2e;
+  for (int i = tid; i < n; i += NT) {
+    const int rel = i - p.rb.far - kPad;
+    float v = -INFINITY;
+    if (i < n - 32 && !(p.rb.causal && rel > 0))
+      v = table_value<T>(p.rb, (int64_t)bucket_of(start, p.rb, rel) * p.H + h) * kLog2e;
+    bt[i] = v;
+  }
+}
+// A 32 x 32 block whose smallest key minus query position is lo reads the
+// table from here on: blocks beyond far take its constant ends.
+__device__ __forceinline__ int bias_from(int lo, int far) {
+  return lo >= far ? far : (lo <= -far - 62 ? -far - 62 : lo);
 }
 __device__ __forceinline__ int query_offset(const CrossParams& p, int n) { return p.rb.at_end ? n - p.Lq : p.rb.q_offset; }
 
