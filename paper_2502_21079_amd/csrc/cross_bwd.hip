@@ -51,12 +51,13 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   }
   const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
   typename T::x8 qf[D / 16], gf[D / 16];
-  load_row<T, D>(p.q + ro.b * p.sq.b + ro.h * p.sq.h + ro.i * p.sq.t, row_ok, hw, qf);
-  load_row<T, D>(p.dout + ro.b * p.sdo.b + ro.h * p.sdo.h + ro.i * p.sdo.t, row_ok, hw, gf);
+  const TwoRows two = two_rows<BIAS>(p, unit, r0 + wave * 32, n_rows, lane);
+  load_tile<T, D>(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane, qf);
+  load_tile<T, D>(at(p.dout, p.sdo, two.a), two.a_ok, at(p.dout, p.sdo, two.b), two.b_ok, lane, gf);
   float lse2 = INFINITY, delta = 0.f;                      // a row without a key: every weight 0
   {
     typename T::x8 of[D / 16];
-    load_row<T, D>(p.out + ro.b * p.so.b + ro.h * p.so.h + ro.i * p.so.t, row_ok, hw, of);
+    load_tile<T, D>(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane, of);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
@@ -107,8 +108,8 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
       f32x16 x = f32x16{}, y = f32x16{};
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
-        x = T::mfma(read_row<T>(sK + (ka ^ (16 * ks)) + 32 * g * D), qf[ks], x);
-        y = T::mfma(read_row<T>(sV + (ka ^ (16 * ks)) + 32 * g * D), gf[ks], y);
+        x = T::mfma(read_row<T>(sK + (ka ^ (8 * row_chunk(ks))) + 32 * g * D), qf[ks], x);
+        y = T::mfma(read_row<T>(sV + (ka ^ (8 * row_chunk(ks))) + 32 * g * D), gf[ks], y);
       }
       // The 32 x 32 block's smallest and largest key minus query position.
       const int lo = t * 64 + 32 * g - (r0 + wave * 32 + 31 + off), hi = lo + 62;
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     const int64_t at = (int64_t)split * p.B * p.H * p.Lq + row;
     store_tile_f32<D>(acc, p.part_o + at * D, row_ok, hw);
   } else {
-    store_tile<T, D>(acc, p.scale, p.dq + ro.b * p.sdq.b + ro.h * p.sdq.h + ro.i * p.sdq.t, row_ok, hw);
+    store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, two.a), two.a_ok, at(p.dq, p.sdq, two.b), two.b_ok, lane);
   }
   // What cross_dkv_kernel takes as delta: the sum of P dP, free of the output's
   // rounding; where the keys are split, the one from the rounded output.
@@ -233,8 +234,16 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
   const int i0 = (int)(items * split / p.kv_splits), i1 = (int)(items * (split + 1) / p.kv_splits);
 
   typename T::x8 kf[D / 16], vf[D / 16];
-  load_row<T, D>(p.k + b * p.sk.b + hk * p.sk.h + (int64_t)key * p.sk.t, key_ok, hw, kf);
-  load_row<T, D>(p.v + b * p.sv.b + hk * p.sv.h + (int64_t)key * p.sv.t, key_ok, hw, vf);
+  // The two keys this lane loads and stores (key is the one it computes).
+  const int key_a = j0 + wave * 32 + (lane & 15), key_b = key_a + 16;
+  {
+    auto visible = [&](int k) { return k < n && !(p.key_mask && p.key_mask[b * p.mask_stride + k] == 0); };
+    const bool a_ok = visible(key_a), b_ok = visible(key_b);
+    const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+    const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+    load_tile<T, D>(kh + (int64_t)key_a * p.sk.t, a_ok, kh + (int64_t)key_b * p.sk.t, b_ok, lane, kf);
+    load_tile<T, D>(vh + (int64_t)key_a * p.sv.t, a_ok, vh + (int64_t)key_b * p.sv.t, b_ok, lane, vf);
+  }
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f32x16{};
@@ -352,8 +361,8 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
     begin(st, xn, yn);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
-      xn = T::mfma(read_row<T>(tile + (ra ^ (16 * ks))), kf[ks], xn);
-      yn = T::mfma(read_row<T>(tile + KE + (ra ^ (16 * ks))), vf[ks], yn);
+      xn = T::mfma(read_row<T>(tile + (ra ^ (8 * row_chunk(ks)))), kf[ks], xn);
+      yn = T::mfma(read_row<T>(tile + KE + (ra ^ (8 * row_chunk(ks)))), vf[ks], yn);
     }
   };
   auto third = [&](const u16* tile, int g, int ca) {
@@ -380,7 +389,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
     auto fetch = [&](int i) {
       const int j = i >> 1;
       if ((i & 1) == 0) {
-        op[i] = read_row<T>(next + (j & 1) * KE + 32 * gn * D + (ra ^ (16 * (j >> 1))));
+        op[i] = read_row<T>(next + (j & 1) * KE + 32 * gn * D + (ra ^ (8 * row_chunk(j >> 1))));
       } else {
         const int s = j / (D / 16), d = j % (D / 16) >> 1;
         op[i] = read_col<T, D>(prev + ((j & 1) ? 0 : KE), ca, d, 32 * gp + 16 * s);
@@ -553,8 +562,11 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
     store_tile_f32<D>(dv, p.part_kv + ((2 * split + 1) * all + at) * D, ok, hw);
     return;
   }
-  store_tile<T, D>(dk, p.scale, p.dk + b * p.sdk.b + hk * p.sdk.h + (int64_t)key * p.sdk.t, ok, hw);
-  store_tile<T, D>(dv, 1.f, p.dv + b * p.sdv.b + hk * p.sdv.h + (int64_t)key * p.sdv.t, ok, hw);
+  u16* dkh = p.dk + b * p.sdk.b + hk * p.sdk.h;
+  u16* dvh = p.dv + b * p.sdv.b + hk * p.sdv.h;
+  const bool a_in = key_a < p.Lk, b_in = key_b < p.Lk;
+  store_tile<T, D>(dk, p.scale, dkh + (int64_t)key_a * p.sdk.t, a_in, dkh + (int64_t)key_b * p.sdk.t, b_in, lane);
+  store_tile<T, D>(dv, 1.f, dvh + (int64_t)key_a * p.sdv.t, a_in, dvh + (int64_t)key_b * p.sdv.t, b_in, lane);
 }
 
 // out row = scale * sum over the splits of its partial rows, in order.

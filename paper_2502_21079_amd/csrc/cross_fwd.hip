@@ -104,7 +104,8 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
     __syncthreads();
   }
   typename T::x8 qf[D / 16];
-  load_row<T, D>(p.q + ro.b * p.sq.b + ro.h * p.sq.h + ro.i * p.sq.t, row_ok, hw, qf);
+  const TwoRows two = two_rows<BIAS>(p, unit, r0 + wave * 32, n_rows, lane);
+  load_tile<T, D>(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane, qf);
 
   Rows<T, D> acc;
   acc.init();
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
       x[g] = f32x16{};
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks)
-        x[g] = T::mfma(read_row<T>(sK + (ka ^ (16 * ks)) + 32 * g * D), qf[ks], x[g]);
+        x[g] = T::mfma(read_row<T>(sK + (ka ^ (8 * row_chunk(ks))) + 32 * g * D), qf[ks], x[g]);
     }
     const int rel = rel0 + t * 64;                       // of this lane's first key of the tile
     if (BIAS) {
@@ -188,7 +189,8 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
     if (row_ok && hw == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(acc.m, l);
     return;
   }
-  store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, p.out + ro.b * p.so.b + ro.h * p.so.h + ro.i * p.so.t, row_ok, hw);
+  store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, at(p.out, p.so, two.a), two.a_ok, at(p.out, p.so, two.b), two.b_ok,
+                   lane);
   if (p.lse && row_ok && hw == 0) p.lse[row] = l == 0.f ? -INFINITY : (acc.m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
@@ -197,7 +199,10 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 // next tile's queries are loaded while one is worked on.
 constexpr int kKeepBytes = 131072;     // of K and V
 template <int D>
-constexpr int kKeepWaves = D == 64 ? 16 : 8;
+#ifndef KW
+#define KW 16
+#endif
+constexpr int kKeepWaves = D == 64 ? KW : 8;
 
 template <class T, int D>
 __global__ __launch_bounds__(64 * kKeepWaves<D>, kKeepWaves<D> / 4) void cross_keep_kernel(const CrossParams p) {
@@ -239,25 +244,19 @@ __global__ __launch_bounds__(64 * kKeepWaves<D>, kKeepWaves<D> / 4) void cross_k
   __syncthreads();
 
   const int ka0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
-  typename T::x8 qf[D / 16], qn[D / 16];
-  auto fetch = [&](int rt, RowOf& ro, bool& ok) {
-    const int r = rt * 32 + c32;
-    ok = r < n_rows;
-    ro = row_of<false>(p, unit, ok ? r : 0);
-    load_row<T, D>(p.q + ro.b * p.sq.b + ro.h * p.sq.h + ro.i * p.sq.t, ok, hw, qn);
+  typename T::x8 qf[D / 16];
+  TileRegs<T, D> qn;
+  auto fetch = [&](int rt) {
+    const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, lane);
+    qn.load(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane);
   };
-  RowOf ro_n;
-  bool ok_n = false;
-  if (rt < rt1) fetch(rt, ro_n, ok_n);
+  if (rt < rt1) fetch(rt);
   for (; rt < rt1; rt += NW) {
-    const RowOf ro = ro_n;
-    const bool row_ok = ok_n;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = qn[ks];
-    if (rt + NW < rt1) fetch(rt + NW, ro_n, ok_n);
+    qn.operands(qf);
+    if (rt + NW < rt1) fetch(rt + NW);
     Rows<T, D> acc;
     acc.init();
-    for (int t = 0; t < nt; ++t) {
+    auto tile = [&](int t, bool masked) {
       const int ka = fresh(ka0), ca = fresh(ca0);
       const u16* tK = sK + t * 64 * D;
       const u16* tV = sV + t * 64 * D;
@@ -267,9 +266,9 @@ __global__ __launch_bounds__(64 * kKeepWaves<D>, kKeepWaves<D> / 4) void cross_k
         x[g] = f32x16{};
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
-          x[g] = T::mfma(read_row<T>(tK + (ka ^ (16 * ks)) + 32 * g * D), qf[ks], x[g]);
+          x[g] = T::mfma(read_row<T>(tK + (ka ^ (8 * row_chunk(ks))) + 32 * g * D), qf[ks], x[g]);
       }
-      if (!((whole >> t) & 1)) {
+      if (masked) {
         const float* at = sB + t * 64 + 4 * hw;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
@@ -283,11 +282,18 @@ __global__ __launch_bounds__(64 * kKeepWaves<D>, kKeepWaves<D> / 4) void cross_k
 #pragma unroll
         for (int s = 0; s < 4; ++s)
           acc.o[d] = T::mfma(read_col<T, D>(tV, ca, d, 16 * s), pb[s >> 1][s & 1], acc.o[d]);
-    }
+    };
+    // Whole tiles first, then those with masked keys.
+    for (uint32_t m = whole; m != 0; m &= m - 1) tile(__builtin_ctz(m), false);
+    for (uint32_t m = ~whole & ((1u << nt) - 1); m != 0; m &= m - 1) tile(__builtin_ctz(m), true);
     const float l = both_halves_sum(acc.l);
-    store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, p.out + ro.b * p.so.b + ro.h * p.so.h + ro.i * p.so.t, row_ok, hw);
-    if (p.lse && row_ok && hw == 0)
-      p.lse[((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i] = l == 0.f ? -INFINITY : (acc.m + __builtin_amdgcn_logf(l)) * kLn2;
+    const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, fresh(lane));
+    store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, at(p.out, p.so, two.a), two.a_ok, at(p.out, p.so, two.b),
+                     two.b_ok, lane);
+    // The rows of a unit are consecutive in lse.
+    const int r = rt * 32 + c32;
+    if (p.lse && r < n_rows && hw == 0)
+      p.lse[(int64_t)unit * n_rows + r] = l == 0.f ? -INFINITY : (acc.m + __builtin_amdgcn_logf(l)) * kLn2;
   }
 }
 

@@ -50,11 +50,15 @@ template <int D>
 __device__ __forceinline__ int row_order(int r) {
   return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
-// Lane address (elements) of a read along rows: row c32, chunk hw; chunk
-// 2 ks + hw of row 32 g + c32 is at (row_lane ^ 16 ks) + 32 g D.
+// MFMA step ks of a sum over D takes chunk row_chunk(ks) + 2 hw of each row:
+// steps come in pairs over four chunks, the way load_tile finds them.  (Any
+// order will do that both operands share.)
+__host__ __device__ constexpr int row_chunk(int ks) { return 4 * (ks >> 1) + (ks & 1); }
+// Lane address (elements) of a read along rows: row c32; the chunk of step ks
+// of row 32 g + c32 is at (row_lane ^ 8 row_chunk(ks)) + 32 g D.
 template <int D>
 __device__ __forceinline__ int row_lane(int c32, int hw) {
-  return c32 * D + (hw ^ row_order<D>(c32)) * 8;
+  return c32 * D + ((2 * hw) ^ row_order<D>(c32)) * 8;
 }
 // Lane address of a transposed read; output block d of rows 16 s further down
 // begins at (col_lane ^ 32 d) + 16 s D, and its second half at
@@ -199,26 +203,79 @@ __device__ __forceinline__ int bias_from(int lo, int far) {
 }
 __device__ __forceinline__ int query_offset(const CrossParams& p, int n) { return p.rb.at_end ? n - p.Lq : p.rb.q_offset; }
 
-// Writes a 32 x D tile held transposed (lane = row c32, columns 32 d + 8 i +
-// 4 hw + j), scaled by inv, to this lane's row: the half-waves exchange so
-// that each lane stores 16 contiguous bytes.
+// --- tiles of 32 rows between memory and registers ----------------------------
+// An MFMA operand has row c32 in lanes c32 and c32 + 32, so an access that
+// follows it takes 32 bytes of each of 32 rows.  Here each access takes 64 bytes
+// of 16 rows (groups of 16 lanes take one chunk each), and two accesses, the
+// lower and the upper 16 rows, exchange groups (one v_permlane16_swap per
+// register).  (The long video's forward pass without any products, one key tile
+// of four: see the kernel.)
 template <class T, int D>
-__device__ __forceinline__ void store_tile(const f32x16 (&o)[D / 32], float inv, u16* row, bool ok, int hw) {
+struct TileRegs {
+  u32x4 w[D / 16];                                       // chunk 4 j + lane / 16 of rows (2 j: lower, 2 j + 1: upper)
+  // a, b: this lane's rows lane % 16 and 16 + lane % 16.
+  __device__ __forceinline__ void load(const u16* a, bool a_ok, const u16* b, bool b_ok, int lane) {
+    const int g = lane >> 4;
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
+    for (int j = 0; j < D / 32; ++j) {
+      w[2 * j] = w[2 * j + 1] = u32x4{0, 0, 0, 0};
+      if (a_ok) w[2 * j] = *reinterpret_cast<const u32x4*>(a + 32 * j + 8 * g);
+      if (b_ok) w[2 * j + 1] = *reinterpret_cast<const u32x4*>(b + 32 * j + 8 * g);
+    }
+  }
+  // The operands of MFMA steps 2 j and 2 j + 1.
+  __device__ __forceinline__ void operands(typename T::x8 (&f)[D / 16]) const {
 #pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-      u32x4 w;
+    for (int j = 0; j < D / 32; ++j) {
+      u32x4 even, odd;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const auto r = __builtin_amdgcn_permlane16_swap(w[2 * j][i], w[2 * j + 1][i], false, false);
+        even[i] = r[0];
+        odd[i] = r[1];
+      }
+      f[2 * j] = __builtin_bit_cast(typename T::x8, even);
+      f[2 * j + 1] = __builtin_bit_cast(typename T::x8, odd);
+    }
+  }
+};
+template <class T, int D>
+__device__ __forceinline__ void load_tile(const u16* a, bool a_ok, const u16* b, bool b_ok, int lane,
+                                          typename T::x8 (&f)[D / 16]) {
+  TileRegs<T, D> t;
+  t.load(a, a_ok, b, b_ok, lane);
+  t.operands(f);
+}
+
+// Writes a 32 x D tile held transposed (lane = row c32, columns 32 d + 8 i +
+// 4 hw + j), scaled by inv: the halves, then groups of 16 lanes exchange until
+// each store takes 64 bytes of 16 rows (a, b: rows lane % 16 and 16 + lane % 16).
+template <class T, int D>
+__device__ __forceinline__ void store_tile(const f32x16 (&o)[D / 32], float inv, u16* a, bool a_ok, u16* b, bool b_ok,
+                                           int lane) {
+  const int g = lane >> 4, chunk = ((g & 1) << 1) | (g >> 1);
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) {
+    u32x4 w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const uint32_t a = T::pack(o[d][4 * i + 2 * j] * inv, o[d][4 * i + 2 * j + 1] * inv);
-        const uint32_t b = T::pack(o[d][4 * i + 4 + 2 * j] * inv, o[d][4 * i + 5 + 2 * j] * inv);
-        const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-        w[j] = r[0];
-        w[2 + j] = r[1];
+        const uint32_t x = T::pack(o[d][8 * i + 2 * j] * inv, o[d][8 * i + 2 * j + 1] * inv);
+        const uint32_t y = T::pack(o[d][8 * i + 4 + 2 * j] * inv, o[d][8 * i + 5 + 2 * j] * inv);
+        const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+        w[i][j] = r[0];
+        w[i][2 + j] = r[1];
       }
-      if (ok) *reinterpret_cast<u32x4*>(row + 32 * d + 8 * (i + hw)) = w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const auto r = __builtin_amdgcn_permlane16_swap(w[0][j], w[1][j], false, false);
+      w[0][j] = r[0];
+      w[1][j] = r[1];
     }
+    if (a_ok) *reinterpret_cast<u32x4*>(a + 32 * d + 8 * chunk) = w[0];
+    if (b_ok) *reinterpret_cast<u32x4*>(b + 32 * d + 8 * chunk) = w[1];
+  }
 }
 // The same in fp32, 16 bytes per lane as they lie.
 template <int D>
@@ -230,15 +287,6 @@ __device__ __forceinline__ void store_tile_f32(const f32x16 (&o)[D / 32], float*
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<f32x4*>(row + 32 * d + 8 * i + 4 * hw) =
           f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-}
-template <class T, int D>
-__device__ __forceinline__ void load_row(const u16* row, bool ok, int hw, typename T::x8 (&f)[D / 16]) {
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) {
-    u32x4 w = {0, 0, 0, 0};
-    if (ok) w = *reinterpret_cast<const u32x4*>(row + 16 * ks + 8 * hw);
-    f[ks] = __builtin_bit_cast(typename T::x8, w);
-  }
 }
 __device__ __forceinline__ float both_halves_max(float v) {
   float a, b;
@@ -257,6 +305,11 @@ __device__ __forceinline__ float both_halves_sum(float v) {
 struct RowOf {
   int b, h, i;
 };
+// Where the view with these strides has it.
+template <typename P>
+__device__ __forceinline__ P* at(P* base, const Strides& s, const RowOf& r) {
+  return base + r.b * s.b + r.h * s.h + r.i * s.t;
+}
 template <bool BIAS>
 __device__ __forceinline__ RowOf row_of(const CrossParams& p, int unit, int r) {
   RowOf o;
@@ -271,6 +324,22 @@ __device__ __forceinline__ RowOf row_of(const CrossParams& p, int unit, int r) {
     o.i = r - g * p.Lq;
   }
   return o;
+}
+
+// The two rows that a lane loads and stores of the 32 from r on.
+struct TwoRows {
+  RowOf a, b;
+  bool a_ok, b_ok;
+};
+template <bool BIAS>
+__device__ __forceinline__ TwoRows two_rows(const CrossParams& p, int unit, int r, int n_rows, int lane) {
+  TwoRows t;
+  const int a = r + (lane & 15);
+  t.a_ok = a < n_rows;
+  t.b_ok = a + 16 < n_rows;
+  t.a = row_of<BIAS>(p, unit, t.a_ok ? a : 0);
+  t.b = row_of<BIAS>(p, unit, t.b_ok ? a + 16 : 0);
+  return t;
 }
 
 }  // namespace adaspa
