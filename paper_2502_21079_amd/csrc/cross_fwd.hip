@@ -12,13 +12,15 @@ namespace adaspa {
 namespace {
 
 constexpr int kRows = 128;             // query rows of a workgroup: four waves of 32
-constexpr float kMaxRise = 8.f;        // log2 units a row's maximum may rise before its sums are rescaled
+constexpr float kSumLimit = 256.f;     // a lane's weights of one tile add up to no more, or the reference moves
 
 // Running softmax of the rows of a wave (lane = row c32, the two half-waves
-// hold its keys between them).  The reference m (log2 units) follows the
-// maximum, but stays where it is while the maximum is less than kMaxRise above
-// it: no weight then exceeds 2^8, which fp16 holds as well, and the output
-// accumulator is rescaled a few times per row instead of at every tile.
+// hold its keys between them).  Weights are taken against a reference m (log2
+// units): the maximum of a row's first tile, then whatever it is until the
+// weights of a tile, summed over one lane's 32 keys, pass kSumLimit; only then
+// is the maximum looked for, the reference moved there and the tile's weights
+// taken again.  So no weight exceeds 2^8, which fp16 holds too, and most tiles
+// need neither a maximum nor a rescaled accumulator.
 template <class T, int D>
 struct Rows {
   f32x16 o[D / 32];
@@ -29,27 +31,8 @@ struct Rows {
     m = -INFINITY;
     l = 0.f;
   }
-  // Scores of 64 keys in x (sl2 x in log2 units): weights into pb, their fp32
-  // sum into l, the accumulator rescaled where the reference moved.
-  __device__ __forceinline__ void weigh(const f32x16 (&x)[2], float sl2, typename T::x8 (&pb)[2][2]) {
-    float mt = -INFINITY;
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) mt = vmax(mt, vmax(x[g][e], x[g][e + 1]));
-    mt = both_halves_max(mt) * sl2;
-    // Also where the maximum is NaN: the row becomes NaN.
-    const bool move = !(mt <= m + kMaxRise) && mt != -INFINITY;
-    if (__any(move)) {
-      const float mn = move ? mt : m;
-      const float a = move ? fast_exp2(m - mn) : 1.f;
-      m = mn;
-      l *= a;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] *= a;
-    }
+  // Weights of 64 scores (sl2 x in log2 units), returns this lane's sum.
+  __device__ __forceinline__ float weights(const f32x16 (&x)[2], float sl2, typename T::x8 (&pb)[2][2]) const {
     const float ref = m == -INFINITY ? 0.f : -m;
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
@@ -65,7 +48,43 @@ struct Rows {
       pb[g][0] = __builtin_bit_cast(typename T::x8, w[0]);
       pb[g][1] = __builtin_bit_cast(typename T::x8, w[1]);
     }
-    l += s0 + s1;
+    return s0 + s1;
+  }
+  // Moves the reference of the rows that need it to the maximum where that is
+  // above it.  (In the first tile there is nothing yet to rescale.)
+  __device__ __forceinline__ void raise(const f32x16 (&x)[2], float sl2, bool first, bool need) {
+    float mt = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) mt = vmax(mt, vmax(x[g][e], x[g][e + 1]));
+    mt = both_halves_max(mt) * sl2;
+    const bool move = need && !(mt <= m);                  // also where it is NaN: the row becomes NaN
+    const float a = move ? fast_exp2(m - mt) : 1.f;
+    if (move) m = mt;
+    if (first) return;
+    l *= a;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] *= a;
+  }
+  // Scores of 64 keys: weights into pb, their fp32 sum into l.  first: of the
+  // first tile, whose rows have no reference yet.
+  __device__ __forceinline__ void weigh(const f32x16 (&x)[2], float sl2, typename T::x8 (&pb)[2][2], bool first) {
+    if (first) raise(x, sl2, true, true);
+    float s = weights(x, sl2, pb);
+    // A row that has seen no key yet has no reference either.  Whether a row
+    // moves is its own matter, so that its bits do not follow its neighbours.
+    if (!first) {
+      const float most = both_halves_max(s);
+      const bool need = !(most <= kSumLimit) || m == -INFINITY;
+      if (__any(need)) {
+        raise(x, sl2, false, need);
+        s = weights(x, sl2, pb);
+      }
+    }
+    l += s;
   }
 };
 
@@ -173,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
           if (!((mine >> (32 * g + 8 * (e >> 2) + (e & 3))) & 1)) x[g][e] = -INFINITY;
     }
     typename T::x8 pb[2][2];
-    acc.weigh(x, BIAS ? 1.f : p.sl2, pb);
+    acc.weigh(x, BIAS ? 1.f : p.sl2, pb, t == t0);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -197,29 +216,29 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 // Few keys, many rows: the keys and values of one (sample, key head) stay in
 // LDS, and each wave walks row tiles of 32 on its own, without barriers; the
 // next tile's queries are loaded while one is worked on.
-constexpr int kKeepBytes = 131072;     // of K and V
+constexpr int kKeepBytes = 131072;     // of K (the first half) and V
+constexpr int kKeepWaves = 8;
+// Row blocks of 32 that a wave works on at a time: at d 64 registers are there
+// for two, which share every operand read from LDS and twice the bytes in flight.
 template <int D>
-#ifndef KW
-#define KW 16
-#endif
-constexpr int kKeepWaves = D == 64 ? KW : 8;
+constexpr int kKeepRows = D == 64 ? 2 : 1;
 
 template <class T, int D>
-__global__ __launch_bounds__(64 * kKeepWaves<D>, kKeepWaves<D> / 4) void cross_keep_kernel(const CrossParams p) {
-  constexpr int NW = kKeepWaves<D>, NT = 64 * NW, CPR = D / 8, RPI = 64 / CPR;
+__global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_kernel(const CrossParams p) {
+  constexpr int NW = kKeepWaves, CPR = D / 8, RPI = 64 / CPR, QR = kKeepRows<D>;
   extern __shared__ __attribute__((aligned(1024))) u16 keep_lds[];     // [K | V | 0 or -inf per key]
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
   const int lid = xcd_remap(blockIdx.x, p.n_wg);
   const int unit = lid / p.splits, chunk = lid % p.splits;
   const int b = unit / p.Hk, hk = unit % p.Hk, n = key_count(p, b), nt = (n + 63) / 64;
-  const int n_rows = p.G * p.Lq, n_rt = (n_rows + 31) / 32;
+  const int n_rows = p.G * p.Lq, n_rt = (n_rows + 32 * QR - 1) / (32 * QR);
   const int rt1 = (int)((int64_t)n_rt * (chunk + 1) / p.splits);
   int rt = (int)((int64_t)n_rt * chunk / p.splits) + wave;
 
   u16* sK = keep_lds;
-  u16* sV = sK + nt * 64 * D;
-  float* sB = reinterpret_cast<float*>(sV + nt * 64 * D);
+  u16* sV = sK + kKeepBytes / 4;
+  float* sB = reinterpret_cast<float*>(sK + kKeepBytes / 2);
   const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
   const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
   // Rows past n and masked rows become zeros; the others come straight in.
@@ -243,57 +262,79 @@ __global__ __launch_bounds__(64 * kKeepWaves<D>, kKeepWaves<D> / 4) void cross_k
   }
   __syncthreads();
 
-  const int ka0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
-  typename T::x8 qf[D / 16];
-  TileRegs<T, D> qn;
+  // This lane's operands in tile 0: a step's chunk of its row, an output block's
+  // column (second half: 8 rows on).  Tiles lie at constant distances, so the
+  // rest of an address is the instruction's own.
+  const u16* kp[D / 16];
+  const u16* vp[D / 32][2];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) kp[ks] = sK + (row_lane<D>(c32, hw) ^ (8 * row_chunk(ks)));
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) vp[d][h] = sV + (col_lane<D>(lane) ^ (16 * h) ^ (32 * d));
+  typename T::x8 qf[QR][D / 16];
+  TileRegs<T, D> qn[QR];
   auto fetch = [&](int rt) {
-    const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, lane);
-    qn.load(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane);
+#pragma unroll
+    for (int r = 0; r < QR; ++r) {
+      const TwoRows two = two_rows<false>(p, unit, (rt * QR + r) * 32, n_rows, lane);
+      qn[r].load(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane);
+    }
   };
   if (rt < rt1) fetch(rt);
   for (; rt < rt1; rt += NW) {
-    qn.operands(qf);
+#pragma unroll
+    for (int r = 0; r < QR; ++r) qn[r].operands(qf[r]);
     if (rt + NW < rt1) fetch(rt + NW);
-    Rows<T, D> acc;
-    acc.init();
-    auto tile = [&](int t, bool masked) {
-      const int ka = fresh(ka0), ca = fresh(ca0);
-      const u16* tK = sK + t * 64 * D;
-      const u16* tV = sV + t * 64 * D;
-      f32x16 x[2];
+    Rows<T, D> acc[QR];
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        x[g] = f32x16{};
+    for (int r = 0; r < QR; ++r) acc[r].init();
+    static_for<kKeepBytes / 256 / D>([&](auto t) {
+      if (t >= nt) return;
+      f32x16 x[QR][2];
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-          x[g] = T::mfma(read_row<T>(tK + (ka ^ (8 * row_chunk(ks))) + 32 * g * D), qf[ks], x[g]);
-      }
-      if (masked) {
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const typename T::x8 kf = read_row<T>(kp[ks] + (64 * t + 32 * g) * D);
+#pragma unroll
+          for (int r = 0; r < QR; ++r) x[r][g] = T::mfma(kf, qf[r][ks], ks == 0 ? f32x16{} : x[r][g]);
+        }
+      if (!((whole >> t) & 1)) {
         const float* at = sB + t * 64 + 4 * hw;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[g][e] += at[32 * g + 8 * (e >> 2) + (e & 3)];
+          for (int e = 0; e < 16; ++e)
+#pragma unroll
+            for (int r = 0; r < QR; ++r) x[r][g][e] += at[32 * g + 8 * (e >> 2) + (e & 3)];
       }
-      typename T::x8 pb[2][2];
-      acc.weigh(x, p.sl2, pb);
+      typename T::x8 pb[QR][2][2];
+#pragma unroll
+      for (int r = 0; r < QR; ++r) acc[r].weigh(x[r], p.sl2, pb[r], t == 0);
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-          acc.o[d] = T::mfma(read_col<T, D>(tV, ca, d, 16 * s), pb[s >> 1][s & 1], acc.o[d]);
-    };
-    // Whole tiles first, then those with masked keys.
-    for (uint32_t m = whole; m != 0; m &= m - 1) tile(__builtin_ctz(m), false);
-    for (uint32_t m = ~whole & ((1u << nt) - 1); m != 0; m &= m - 1) tile(__builtin_ctz(m), true);
-    const float l = both_halves_sum(acc.l);
-    const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, fresh(lane));
-    store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, at(p.out, p.so, two.a), two.a_ok, at(p.out, p.so, two.b),
-                     two.b_ok, lane);
-    // The rows of a unit are consecutive in lse.
-    const int r = rt * 32 + c32;
-    if (p.lse && r < n_rows && hw == 0)
-      p.lse[(int64_t)unit * n_rows + r] = l == 0.f ? -INFINITY : (acc.m + __builtin_amdgcn_logf(l)) * kLn2;
+        for (int s = 0; s < 4; ++s) {
+          const int row = 64 * t + 16 * s;
+          const typename T::x8 vf = read_cols<T>(vp[d][0] + row * D, vp[d][1] + (row + 8) * D);
+#pragma unroll
+          for (int r = 0; r < QR; ++r) acc[r].o[d] = T::mfma(vf, pb[r][s >> 1][s & 1], acc[r].o[d]);
+        }
+    });
+#pragma unroll
+    for (int r = 0; r < QR; ++r) {
+      const float l = both_halves_sum(acc[r].l);
+      const int r0 = (rt * QR + r) * 32;
+      const TwoRows two = two_rows<false>(p, unit, r0, n_rows, fresh(lane));
+      store_tile<T, D>(acc[r].o, l == 0.f ? 0.f : 1.f / l, at(p.out, p.so, two.a), two.a_ok, at(p.out, p.so, two.b),
+                       two.b_ok, lane);
+      // The rows of a unit are consecutive in lse.
+      if (p.lse && r0 + c32 < n_rows && hw == 0)
+        p.lse[(int64_t)unit * n_rows + r0 + c32] =
+            l == 0.f ? -INFINITY : (acc[r].m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
   }
 }
 
@@ -356,7 +397,7 @@ CrossPlan plan_fwd(const CrossParams& p, int D, bool bias) {
   // Rows enough for two tiles a wave on every CU, keys few enough for LDS: the
   // keys stay there, and a unit's rows are shared among as many workgroups as
   // fill the rounds of 256 best (one workgroup's loading counts as three tiles).
-  const int64_t waves = D == 64 ? kKeepWaves<64> : kKeepWaves<128>, rt = (rows + 31) / 32;
+  const int64_t waves = kKeepWaves, wide = 32 * (D == 64 ? kKeepRows<64> : kKeepRows<128>), rt = (rows + wide - 1) / wide;
   c.resident = !bias && nt * 64 * D * 4 <= kKeepBytes && units * rt >= 512 * waves;
   if (c.resident) {
     int64_t best = -1;
@@ -388,8 +429,8 @@ static hipError_t run_fwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rows = bias ? p.Lq : (int64_t)p.G * p.Lq;
   if (c.resident) {
     p.n_wg = (int)(units * p.splits);
-    const uint32_t lds = (uint32_t)((p.Lk + 63) / 64 * 64 * (D * 4 + 4));
-    hipLaunchKernelGGL((cross_keep_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves<D>), lds, st, p);
+    const uint32_t lds = kKeepBytes + (uint32_t)(p.Lk + 63) / 64 * 256;
+    hipLaunchKernelGGL((cross_keep_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves), lds, st, p);
     return hipGetLastError();
   }
   p.n_wg = (int)(units * ((rows + kRows - 1) / kRows) * p.splits);

@@ -72,15 +72,19 @@ template <class T>
 __device__ __forceinline__ typename T::x8 read_row(const u16* p) {
   return *reinterpret_cast<const typename T::x8*>(p);
 }
-// Transposed operand: 16 rows from `r16` on of output block d.
-template <class T, int D>
-__device__ __forceinline__ typename T::x8 read_col(const u16* tile, int ca, int d, int r16) {
-  const s16x4 lo = lds_read_tr16(tile + (ca ^ (32 * d)) + r16 * D);
-  const s16x4 hi = lds_read_tr16(tile + (ca ^ 16 ^ (32 * d)) + (r16 + 8) * D);
+// Transposed operand from this lane's places in its two halves of 8 rows.
+template <class T>
+__device__ __forceinline__ typename T::x8 read_cols(const u16* lower, const u16* upper) {
+  const s16x4 lo = lds_read_tr16(lower), hi = lds_read_tr16(upper);
   typename T::x8 v;
   __builtin_memcpy(&v, &lo, 8);
   __builtin_memcpy(reinterpret_cast<char*>(&v) + 8, &hi, 8);
   return v;
+}
+// Transposed operand: 16 rows from `r16` on of output block d.
+template <class T, int D>
+__device__ __forceinline__ typename T::x8 read_col(const u16* tile, int ca, int d, int r16) {
+  return read_cols<T>(tile + (ca ^ (32 * d)) + r16 * D, tile + (ca ^ 16 ^ (32 * d)) + (r16 + 8) * D);
 }
 
 // Loads of ROWS-row tiles straight into LDS by NW waves.  The source is the
@@ -127,6 +131,15 @@ struct TileLoad {
 __device__ __forceinline__ int fresh(int v) {
   asm volatile("" : "+v"(v));
   return v;
+}
+
+// f(0) ... f(N - 1) with compile-time indices.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(integral_constant<int, I>{});
+    static_for<N, I + 1>(f);
+  }
 }
 
 // Clears rows of a tile whose bit in `keep` is 0 (rows below n), so that
