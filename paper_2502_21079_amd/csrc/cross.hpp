@@ -56,11 +56,45 @@ struct CrossParams {
 // Row tiles, splits and scratch of a call: by its shape alone, so that a
 // workspace size, the launches and the results follow the shape.
 struct CrossPlan {
-  bool resident;                       // forward: the keys of a head stay in LDS, splits workgroups share its rows
+  bool resident;                       // the keys of a head stay in LDS, splits workgroups share its rows
   int splits, kv_splits;
   int64_t part_o, part_ml, row_ld, part_kv, part_t;   // byte offsets into the workspace
   int64_t bytes;
 };
+
+// Keys of a head kept in LDS: few enough for it, and rows enough for a tile of
+// each wave of 256 workgroups.
+constexpr int kKeepBytes = 131072;     // K, then V
+constexpr int kKeepWaves = 8;
+// Row blocks of 32 that a wave of the forward kernel works on at a time: at d 64
+// registers are there for two, which share every operand read from LDS and
+// have twice the bytes in flight.
+constexpr int keep_rows(int D) { return D == 64 ? 2 : 1; }
+inline int64_t keep_tiles(const CrossParams& p, int row_blocks) {
+  return ((int64_t)p.G * p.Lq + 32 * row_blocks - 1) / (32 * row_blocks);
+}
+inline bool keep_keys(const CrossParams& p, int D, bool bias, int row_blocks) {
+  return !bias && (int64_t)(p.Lk + 63) / 64 * 64 * D * 4 <= kKeepBytes &&
+         (int64_t)p.B * p.Hk * keep_tiles(p, row_blocks) >= 256 * kKeepWaves;
+}
+// Workgroups that share a unit's rows: as many as fill the rounds of 256 best
+// (a workgroup's start counts as three tiles), and at least two rounds where
+// samples have lengths of their own, so that those with few keys make room.
+inline int keep_chunks(const CrossParams& p, int row_blocks) {
+  const int64_t units = (int64_t)p.B * p.Hk, tiles = keep_tiles(p, row_blocks);
+  int64_t best = -1, chunks = 1;
+  for (int64_t n = 1; n <= 256 && n * kKeepWaves < tiles + kKeepWaves; ++n) {
+    if (p.key_lens && units * n < 512 && (n + 1) * kKeepWaves < tiles + kKeepWaves) continue;
+    const int64_t cost = (units * n + 255) / 256 * ((tiles + n * kKeepWaves - 1) / (n * kKeepWaves) + 3);
+    if (best < 0 || cost < best) {
+      best = cost;
+      chunks = n;
+    }
+  }
+  return (int)chunks;
+}
+inline uint32_t keep_lds_bytes(int Lk) { return kKeepBytes + (uint32_t)(Lk + 63) / 64 * 256; }
+
 CrossPlan plan_fwd(const CrossParams& p, int D, bool bias);
 CrossPlan plan_bwd(const CrossParams& p, int D, bool bias);
 

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 
   const int n_rows = BIAS ? p.Lq : p.G * p.Lq, n_rt = (n_rows + kDqRows - 1) / kDqRows;
   const int lid = xcd_remap(blockIdx.x, p.n_wg);
-  const int unit = lid / (n_rt * p.splits), split = lid / n_rt % p.splits, r0 = lid % n_rt * kDqRows;
+  const int unit = unit_at(p, lid / (n_rt * p.splits), BIAS ? p.H : p.Hk), split = lid / n_rt % p.splits, r0 = lid % n_rt * kDqRows;
   const int r = r0 + wave * 32 + c32;
   const bool row_ok = r < n_rows;
   const RowOf ro = row_of<BIAS>(p, unit, row_ok ? r : 0);
@@ -165,6 +165,98 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   if (p.splits == 1 && row_ok && hw == 0) p.row_ld[row] = make_float2(-lse2 / p.sl2, -exact);
 }
 
+// dq with few keys: they stay in LDS, as in the forward pass, and each wave
+// walks row tiles of 32 on its own, without barriers.
+template <class T, int D>
+__global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq_kernel(const CrossParams p) {
+  constexpr int NW = kKeepWaves;
+  extern __shared__ __attribute__((aligned(1024))) u16 keep_lds[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+  const int lid = xcd_remap(blockIdx.x, p.n_wg);
+  const int unit = unit_at(p, lid / p.splits, p.Hk), chunk = lid % p.splits;
+  const int b = unit / p.Hk, hk = unit % p.Hk, n = key_count(p, b);
+  const int n_rows = p.G * p.Lq, n_rt = (n_rows + 31) / 32;
+  const int rt1 = (int)((int64_t)n_rt * (chunk + 1) / p.splits);
+  int rt = (int)((int64_t)n_rt * chunk / p.splits) + wave;
+
+  const KeptKeys<T, D> keys(p, b, hk, n, keep_lds, wave, lane, tid, []() {});
+  for (; rt < rt1; rt += NW) {
+    const int r = rt * 32 + c32;
+    const int64_t row = (int64_t)unit * n_rows + r;        // a unit's rows are consecutive
+    typename T::x8 qf[D / 16], gf[D / 16];
+    float delta = 0.f, nlse2 = -INFINITY;                  // -log2-LSE; a row without a key: every weight 0
+    {
+      const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, fresh(lane));
+      TileRegs<T, D> q, g, o;
+      g.load(at(p.dout, p.sdo, two.a), two.a_ok, at(p.dout, p.sdo, two.b), two.b_ok, lane);
+      o.load(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane);
+      q.load(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane);
+      const float z = r < n_rows ? p.lse[row] : -INFINITY;
+      if (z != -INFINITY) nlse2 = -z * kLog2e;
+      typename T::x8 of[D / 16];
+      g.operands(gf);
+      o.operands(of);
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
+      delta = both_halves_sum(delta);
+      q.operands(qf);
+    }
+    f32x16 acc[D / 32], from;                              // dP's sums begin at -delta
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) from[e] = -delta;
+    float more = 0.f;                                      // sum of dS: what delta lacks
+    static_for<2 * KeptKeys<T, D>::TILES>([&](auto j) {
+      constexpr int t = j / 2, row0 = 32 * j;
+      if (t >= keys.nt) return;
+      f32x16 x = f32x16{}, y = from;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        x = T::mfma(read_row<T>(keys.kp[ks] + row0 * D), qf[ks], x);
+        y = T::mfma(read_row<T>(keys.vrow[ks] + row0 * D), gf[ks], y);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, nlse2);
+      if (!((keys.whole >> t) & 1)) {
+        const float* at = keys.mask + row0 + 4 * hw;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] += at[8 * (e >> 2) + (e & 3)];
+      }
+      u32x4 w[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] *= fast_exp2(x[e]);
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        s0 += y[e];
+        s1 += y[e + 1];
+        w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+      }
+      more += s0 + s1;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const typename T::x8 ds = __builtin_bit_cast(typename T::x8, w[s]);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+          const u16* lo = keys.kcol[d][0] + (row0 + 16 * s) * D;
+          const u16* hi = keys.kcol[d][1] + (row0 + 16 * s + 8) * D;
+          acc[d] = T::mfma(read_cols<T>(lo, hi), ds, acc[d]);
+        }
+      }
+    });
+    // What cross_dkv_kernel takes as delta is free of the output's rounding: the
+    // weights add up to 1, so the sum of P dP is delta and the sum of dS.
+    const float exact = delta + both_halves_sum(more);
+    if (r < n_rows && hw == 0) p.row_ld[row] = make_float2(nlse2 / p.sl2, -exact);
+    const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, fresh(lane));
+    store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, two.a), two.a_ok, at(p.dq, p.sdq, two.b), two.b_ok, lane);
+  }
+}
+
 // Diagonal sums of a 32 x 32 block held as lane (hw, c32) = column c32, element
 // e = row 8 (e / 4) + 4 hw + e % 4, added to at[31 + column - row].  Row by row,
 // the sum so far moves up one lane and the next row is added, so a diagonal's
@@ -220,7 +312,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
 
   const int n_kt = (p.Lk + 32 * NW - 1) / (32 * NW);
   const int lid = xcd_remap(blockIdx.x, p.n_wg);
-  const int unit = lid / (n_kt * p.kv_splits), split = lid / n_kt % p.kv_splits, j0 = lid % n_kt * 32 * NW;
+  const int unit = unit_at(p, lid / (n_kt * p.kv_splits), p.Hk), split = lid / n_kt % p.kv_splits, j0 = lid % n_kt * 32 * NW;
   const int b = unit / p.Hk, hk = unit % p.Hk;
   const int n = key_count(p, b), off = query_offset(p, n);
   const int key = j0 + wave * 32 + c32;
@@ -629,6 +721,8 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), tiles = units * row_tiles(p, bias);
   const int64_t nt = (p.Lk + 63) / 64;
   c.splits = tiles > 0 && tiles < 256 ? clamp_splits(512 / tiles, nt / 4) : 1;
+  c.resident = keep_keys(p, D, bias, 1);
+  if (c.resident) c.splits = keep_chunks(p, 1);
   const int64_t ktiles = (int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves));
   const int64_t items = (int64_t)p.G * ((p.Lq + 63) / 64);
   // Ranges of the queries: rounds of as many workgroups as run at a time (two
@@ -651,7 +745,7 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   const int64_t rows = (int64_t)p.B * p.H * p.Lq;
   int64_t off = up256(rows * 8);                     // row_ld at 0
   c.part_o = off;
-  if (c.splits > 1) off += up256(c.splits * rows * D * 4);
+  if (c.splits > 1 && !c.resident) off += up256(c.splits * rows * D * 4);
   c.part_kv = off;
   if (c.kv_splits > 1) off += up256((int64_t)c.kv_splits * 2 * p.B * p.Hk * p.Lk * D * 4);
   c.part_t = off;
@@ -667,8 +761,10 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rt = row_tiles(p, bias);
   const int64_t rows = (int64_t)p.B * p.H * p.Lq, keys = (int64_t)p.B * p.Hk * p.Lk;
   const uint32_t lds = bias ? bias_entries(p.rb.far) * 4 : 0, per = 256 / (D / 4);
-  p.n_wg = (int)(units * rt * p.splits);
-  if (p.n_wg > 0) {
+  p.n_wg = (int)(units * (c.resident ? 1 : rt) * p.splits);
+  if (c.resident) {
+    hipLaunchKernelGGL((cross_keep_dq_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves), keep_lds_bytes(p.Lk), st, p);
+  } else if (p.n_wg > 0) {
     if (bias) hipLaunchKernelGGL((cross_dq_kernel<T, D, true>), dim3(p.n_wg), dim3(256), lds, st, p);
     else hipLaunchKernelGGL((cross_dq_kernel<T, D, false>), dim3(p.n_wg), dim3(256), 0, st, p);
     if (p.splits > 1)

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 
   const int n_rows = BIAS ? p.Lq : p.G * p.Lq, n_rt = (n_rows + kRows - 1) / kRows;
   const int lid = xcd_remap(blockIdx.x, p.n_wg);
-  const int unit = lid / (n_rt * p.splits), split = lid / n_rt % p.splits, r0 = lid % n_rt * kRows;
+  const int unit = unit_at(p, lid / (n_rt * p.splits), BIAS ? p.H : p.Hk), split = lid / n_rt % p.splits, r0 = lid % n_rt * kRows;
   const int r = r0 + wave * 32 + c32;
   const bool row_ok = r < n_rows;
   const RowOf ro = row_of<BIAS>(p, unit, row_ok ? r : 0);
@@ -214,65 +214,21 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 }
 
 // Few keys, many rows: the keys and values of one (sample, key head) stay in
-// LDS, and each wave walks row tiles of 32 on its own, without barriers; the
-// next tile's queries are loaded while one is worked on.
-constexpr int kKeepBytes = 131072;     // of K (the first half) and V
-constexpr int kKeepWaves = 8;
-// Row blocks of 32 that a wave works on at a time: at d 64 registers are there
-// for two, which share every operand read from LDS and twice the bytes in flight.
-template <int D>
-constexpr int kKeepRows = D == 64 ? 2 : 1;
-
+// LDS, and each wave walks row tiles on its own, without barriers; the next
+// tile's queries are loaded while one is worked on.
 template <class T, int D>
 __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_kernel(const CrossParams p) {
-  constexpr int NW = kKeepWaves, CPR = D / 8, RPI = 64 / CPR, QR = kKeepRows<D>;
+  constexpr int NW = kKeepWaves, QR = keep_rows(D);
   extern __shared__ __attribute__((aligned(1024))) u16 keep_lds[];     // [K | V | 0 or -inf per key]
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
   const int lid = xcd_remap(blockIdx.x, p.n_wg);
-  const int unit = lid / p.splits, chunk = lid % p.splits;
-  const int b = unit / p.Hk, hk = unit % p.Hk, n = key_count(p, b), nt = (n + 63) / 64;
+  const int unit = unit_at(p, lid / p.splits, p.Hk), chunk = lid % p.splits;
+  const int b = unit / p.Hk, hk = unit % p.Hk, n = key_count(p, b);
   const int n_rows = p.G * p.Lq, n_rt = (n_rows + 32 * QR - 1) / (32 * QR);
   const int rt1 = (int)((int64_t)n_rt * (chunk + 1) / p.splits);
   int rt = (int)((int64_t)n_rt * chunk / p.splits) + wave;
 
-  u16* sK = keep_lds;
-  u16* sV = sK + kKeepBytes / 4;
-  float* sB = reinterpret_cast<float*>(sK + kKeepBytes / 2);
-  const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
-  const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
-  // Rows past n and masked rows become zeros; the others come straight in.
-  for (int i = wave; i < nt * 64 / RPI; i += NW) {
-    const int row = i * RPI + lane / CPR, chunk16 = (lane % CPR) ^ row_order<D>(row);
-    const bool ok = row < n && !(p.key_mask && p.key_mask[b * p.mask_stride + row] == 0);
-    u32x4 wk = {0, 0, 0, 0}, wv = {0, 0, 0, 0};
-    if (ok) {
-      wk = *reinterpret_cast<const u32x4*>(kh + row * p.sk.t + chunk16 * 8);
-      wv = *reinterpret_cast<const u32x4*>(vh + row * p.sv.t + chunk16 * 8);
-    }
-    *reinterpret_cast<u32x4*>(sK + i * 512 + lane * 8) = wk;
-    *reinterpret_cast<u32x4*>(sV + i * 512 + lane * 8) = wv;
-  }
-  uint32_t whole = 0;                                    // tiles whose 64 keys are all visible
-  for (int t = 0; t < nt; ++t) {
-    const int key = t * 64 + lane;
-    const bool ok = key < n && !(p.key_mask && p.key_mask[b * p.mask_stride + key] == 0);
-    if (__ballot(ok) == ~0ull) whole |= 1u << t;
-    else if (wave == 0) sB[key] = ok ? 0.f : -INFINITY;
-  }
-  __syncthreads();
-
-  // This lane's operands in tile 0: a step's chunk of its row, an output block's
-  // column (second half: 8 rows on).  Tiles lie at constant distances, so the
-  // rest of an address is the instruction's own.
-  const u16* kp[D / 16];
-  const u16* vp[D / 32][2];
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) kp[ks] = sK + (row_lane<D>(c32, hw) ^ (8 * row_chunk(ks)));
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) vp[d][h] = sV + (col_lane<D>(lane) ^ (16 * h) ^ (32 * d));
   typename T::x8 qf[QR][D / 16];
   TileRegs<T, D> qn[QR];
   auto fetch = [&](int rt) {
@@ -282,7 +238,9 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_ke
       qn[r].load(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane);
     }
   };
-  if (rt < rt1) fetch(rt);
+  const KeptKeys<T, D> keys(p, b, hk, n, keep_lds, wave, lane, tid, [&]() {
+    if (rt < rt1) fetch(rt);
+  });
   for (; rt < rt1; rt += NW) {
 #pragma unroll
     for (int r = 0; r < QR; ++r) qn[r].operands(qf[r]);
@@ -290,19 +248,19 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_ke
     Rows<T, D> acc[QR];
 #pragma unroll
     for (int r = 0; r < QR; ++r) acc[r].init();
-    static_for<kKeepBytes / 256 / D>([&](auto t) {
-      if (t >= nt) return;
+    static_for<KeptKeys<T, D>::TILES>([&](auto t) {
+      if (t >= keys.nt) return;
       f32x16 x[QR][2];
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-          const typename T::x8 kf = read_row<T>(kp[ks] + (64 * t + 32 * g) * D);
+          const typename T::x8 kf = read_row<T>(keys.kp[ks] + (64 * t + 32 * g) * D);
 #pragma unroll
           for (int r = 0; r < QR; ++r) x[r][g] = T::mfma(kf, qf[r][ks], ks == 0 ? f32x16{} : x[r][g]);
         }
-      if (!((whole >> t) & 1)) {
-        const float* at = sB + t * 64 + 4 * hw;
+      if (!((keys.whole >> t) & 1)) {
+        const float* at = keys.mask + t * 64 + 4 * hw;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -318,7 +276,7 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_ke
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
           const int row = 64 * t + 16 * s;
-          const typename T::x8 vf = read_cols<T>(vp[d][0] + row * D, vp[d][1] + (row + 8) * D);
+          const typename T::x8 vf = read_cols<T>(keys.vp[d][0] + row * D, keys.vp[d][1] + (row + 8) * D);
 #pragma unroll
           for (int r = 0; r < QR; ++r) acc[r].o[d] = T::mfma(vf, pb[r][s >> 1][s & 1], acc[r].o[d]);
         }
@@ -394,20 +352,9 @@ CrossPlan plan_fwd(const CrossParams& p, int D, bool bias) {
   CrossPlan c{};
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rows = bias ? p.Lq : (int64_t)p.G * p.Lq;
   const int64_t tiles = units * ((rows + kRows - 1) / kRows), nt = (p.Lk + 63) / 64;
-  // Rows enough for two tiles a wave on every CU, keys few enough for LDS: the
-  // keys stay there, and a unit's rows are shared among as many workgroups as
-  // fill the rounds of 256 best (one workgroup's loading counts as three tiles).
-  const int64_t waves = kKeepWaves, wide = 32 * (D == 64 ? kKeepRows<64> : kKeepRows<128>), rt = (rows + wide - 1) / wide;
-  c.resident = !bias && nt * 64 * D * 4 <= kKeepBytes && units * rt >= 512 * waves;
+  c.resident = keep_keys(p, D, bias, keep_rows(D));
   if (c.resident) {
-    int64_t best = -1;
-    for (int64_t n = 1; n <= 256 && n * waves <= rt + waves; ++n) {
-      const int64_t cost = (units * n + 255) / 256 * ((rt + n * waves - 1) / (n * waves) + 3);
-      if (best < 0 || cost < best) {
-        best = cost;
-        c.splits = (int)n;
-      }
-    }
+    c.splits = keep_chunks(p, keep_rows(D));
     return c;
   }
   // Keys are split where the row tiles alone leave CUs without work, into
@@ -429,8 +376,7 @@ static hipError_t run_fwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rows = bias ? p.Lq : (int64_t)p.G * p.Lq;
   if (c.resident) {
     p.n_wg = (int)(units * p.splits);
-    const uint32_t lds = kKeepBytes + (uint32_t)(p.Lk + 63) / 64 * 256;
-    hipLaunchKernelGGL((cross_keep_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves), lds, st, p);
+    hipLaunchKernelGGL((cross_keep_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves), keep_lds_bytes(p.Lk), st, p);
     return hipGetLastError();
   }
   p.n_wg = (int)(units * ((rows + kRows - 1) / kRows) * p.splits);

@@ -312,12 +312,87 @@ __device__ __forceinline__ float both_halves_sum(float v) {
   return a + b;
 }
 
+// --- keys of a head kept in LDS ------------------------------------------------
+// All keys and values of one (sample, key head), for kKeepWaves waves: K in the
+// first half of kKeepBytes of LDS, V in the second, then 0 or -inf per key.
+// Tiles lie at constant distances, so a lane needs its places in tile 0 and the
+// rest of an address is the instruction's own.
+template <class T, int D>
+struct KeptKeys {
+  static constexpr int TILES = kKeepBytes / 256 / D;
+  int nt;                                                // tiles of 64 keys
+  uint32_t whole;                                        // those of which every key is visible
+  const float* mask;
+  const u16* kp[D / 16];                                 // K along rows, per MFMA step
+  const u16* vrow[D / 16];                               // V along rows
+  const u16* vp[D / 32][2];                              // V transposed, per output block and half of 8 rows
+  const u16* kcol[D / 32][2];                            // K transposed
+  // meanwhile(): done while the tiles are on their way.
+  template <typename F>
+  __device__ __forceinline__ KeptKeys(const CrossParams& p, int b, int hk, int n, u16* lds, int wave, int lane, int tid,
+                                      F&& meanwhile) {
+    u16* sK = lds;
+    u16* sV = lds + kKeepBytes / 4;
+    float* sB = reinterpret_cast<float*>(lds + kKeepBytes / 2);
+    const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+    const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+    nt = (n + 63) / 64;
+    // All tiles are on their way before the first is waited for.
+    TileLoad<D, kKeepWaves> lk, lv;
+    lk.init(wave, lane, p.sk.t);
+    lv.init(wave, lane, p.sv.t);
+    int mb[TILES];
+    static_for<TILES>([&](auto t) {
+      mb[t] = 1;
+      if (t >= nt) return;
+      lk.issue(lds_addr(sK) + t * 128 * D, kh + t * 64 * p.sk.t, p.sk.t, n - t * 64);
+      lv.issue(lds_addr(sV) + t * 128 * D, vh + t * 64 * p.sv.t, p.sv.t, n - t * 64);
+      if (p.key_mask) mb[t] = mask_byte(p, b, t * 64, n, lane);
+    });
+    meanwhile();
+    wait_vmem();
+    __syncthreads();
+    // Masked rows and those past n become zeros.
+    whole = 0;
+    static_for<TILES>([&](auto t) {
+      if (t >= nt) return;
+      const uint64_t keep = below(t * 64, n) & __ballot(mb[t] != 0);
+      if (keep == ~0ull) {
+        whole |= 1u << t;
+        return;
+      }
+      if (wave == 0) sB[t * 64 + lane] = (keep >> lane) & 1 ? 0.f : -INFINITY;
+      clear_rows<D, 64 * kKeepWaves>(sK + t * 64 * D, keep, tid);
+      clear_rows<D, 64 * kKeepWaves>(sV + t * 64 * D, keep, tid);
+    });
+    __syncthreads();
+    mask = sB;
+    const int ra = row_lane<D>(lane & 31, lane >> 5), ca = col_lane<D>(lane);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      kp[ks] = sK + (ra ^ (8 * row_chunk(ks)));
+      vrow[ks] = sV + (ra ^ (8 * row_chunk(ks)));
+    }
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        vp[d][h] = sV + (ca ^ (16 * h) ^ (32 * d));
+        kcol[d][h] = sK + (ca ^ (16 * h) ^ (32 * d));
+      }
+  }
+};
+
 // Which query row a lane works on.  Without a bias the query heads that share
 // a key head are rows of one problem (unit = (sample, key head), G * Lq rows);
 // with one a unit is a (sample, query head).
 struct RowOf {
   int b, h, i;
 };
+// The unit (sample b, head h; b * heads + h) at place u of the launch order:
+// samples change first, so that every XCD, which gets a run of that order, has
+// a share of the long samples and of the short ones.
+__device__ __forceinline__ int unit_at(const CrossParams& p, int u, int heads) { return u % p.B * heads + u / p.B; }
 // Where the view with these strides has it.
 template <typename P>
 __device__ __forceinline__ P* at(P* base, const Strides& s, const RowOf& r) {
