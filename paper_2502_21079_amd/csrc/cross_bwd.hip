@@ -45,10 +45,6 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   const int nt = (kend + 63) / 64;
   const int t0 = (int)((int64_t)nt * split / p.splits), t1 = (int)((int64_t)nt * (split + 1) / p.splits);
 
-  if (BIAS) {
-    fill_bias<T, 256>(bt, reinterpret_cast<uint16_t*>(ring), p, unit % p.H, tid);
-    __syncthreads();
-  }
   const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
   typename T::x8 qf[D / 16], gf[D / 16];
   const TwoRows two = two_rows<BIAS>(p, unit, r0 + wave * 32, n_rows, lane);
@@ -88,6 +84,10 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   const int rel0 = 4 * hw - (ro.i + off);
 
   if (t0 < t1) issue(t0);
+  if (BIAS) {
+    __shared__ uint16_t start[kMaxBucketSide];
+    fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
+  }
   for (int t = t0; t < t1; ++t) {
     wait_vmem();
     const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb != 0) : ~0ull);
@@ -661,25 +661,34 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
   store_tile<T, D>(dv, 1.f, dvh + (int64_t)key_a * p.sdv.t, a_in, dvh + (int64_t)key_b * p.sdv.t, b_in, lane);
 }
 
-// out row = scale * sum over the splits of its partial rows, in order.
+// Rows of a result from the splits' partial rows, added in order.  Two results
+// (dk and dv) side by side in one launch: blockIdx.y chooses.
+struct SumOf {
+  const float* part;
+  u16* out;
+  Strides so;
+  float scale;
+};
 template <class T, int D>
-__global__ __launch_bounds__(256) void cross_sum_kernel(const float* part, int64_t stride, int splits, int64_t rows,
-                                                        int heads, int len, u16* out, Strides so, float scale) {
+__global__ __launch_bounds__(256) void cross_sum_kernel(SumOf first, SumOf second, int64_t stride, int splits,
+                                                        int64_t rows, int heads, int len) {
   constexpr int TPR = D / 4;
+  const SumOf& s = blockIdx.y == 0 ? first : second;
   const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
   if (row >= rows) return;
   const int c = threadIdx.x % TPR * 4;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(part + s * stride + row * D + c);
+#pragma unroll 4
+  for (int i = 0; i < splits; ++i) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(s.part + i * stride + row * D + c);
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] += v[j];
   }
-  const int i = (int)(row % len), h = (int)(row / len % heads), b = (int)(row / len / heads);
+  const RowOf r = {(int)(row / len / heads), (int)(row / len % heads), (int)(row % len)};
   uint2 w;
-  w.x = T::pack(o[0] * scale, o[1] * scale);
-  w.y = T::pack(o[2] * scale, o[3] * scale);
-  *reinterpret_cast<uint2*>(out + b * so.b + h * so.h + i * so.t + c) = w;
+  w.x = T::pack(o[0] * s.scale, o[1] * s.scale);
+  w.y = T::pack(o[2] * s.scale, o[3] * s.scale);
+  *reinterpret_cast<uint2*>(at(s.out, s.so, r) + c) = w;
 }
 
 // dtable[u, h]: the shares of head h over samples and workgroups, eight runs of
@@ -767,22 +776,20 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   } else if (p.n_wg > 0) {
     if (bias) hipLaunchKernelGGL((cross_dq_kernel<T, D, true>), dim3(p.n_wg), dim3(256), lds, st, p);
     else hipLaunchKernelGGL((cross_dq_kernel<T, D, false>), dim3(p.n_wg), dim3(256), 0, st, p);
+    const SumOf dq = {p.part_o, p.dq, p.sdq, p.scale};
     if (p.splits > 1)
-      hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, st,
-                         p.part_o, rows * D, p.splits, rows, p.H, p.Lq, p.dq, p.sdq, p.scale);
+      hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, st, dq, dq,
+                         rows * D, p.splits, rows, p.H, p.Lq);
   }
   p.n_wg = (int)((int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves)) * p.kv_splits);
   if (p.n_wg > 0) {
     if (bias) hipLaunchKernelGGL((cross_dkv_kernel<T, D, true>), dim3(p.n_wg), dim3(64 * kDkvWaves),
                                  lds + kDkvWaves * diag_entries(p.rb.far) * 4, st, p);
     else hipLaunchKernelGGL((cross_dkv_kernel<T, D, false>), dim3(p.n_wg), dim3(64 * kDkvWaves), 0, st, p);
-    if (p.kv_splits > 1) {
-      const dim3 grid((uint32_t)((keys + per - 1) / per));
-      hipLaunchKernelGGL((cross_sum_kernel<T, D>), grid, dim3(256), 0, st, p.part_kv, 2 * keys * D, p.kv_splits, keys,
-                         p.Hk, p.Lk, p.dk, p.sdk, p.scale);
-      hipLaunchKernelGGL((cross_sum_kernel<T, D>), grid, dim3(256), 0, st, p.part_kv + keys * D, 2 * keys * D,
-                         p.kv_splits, keys, p.Hk, p.Lk, p.dv, p.sdv, 1.f);
-    }
+    const SumOf dk = {p.part_kv, p.dk, p.sdk, p.scale}, dv = {p.part_kv + keys * D, p.dv, p.sdv, 1.f};
+    if (p.kv_splits > 1)
+      hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((keys + per - 1) / per), 2), dim3(256), 0, st, dk, dv,
+                         2 * keys * D, p.kv_splits, keys, p.Hk, p.Lk);
   }
   if (bias) {
     const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;

@@ -91,11 +91,13 @@ struct Rows {
 }  // namespace
 
 // Workgroup: 128 query rows of one unit over one range of its keys, 64-key
-// tiles through a ring of two in LDS, the next one loaded while one is used.
-template <class T, int D, bool BIAS>
+// tiles through a ring of RING slots in LDS, RING - 1 of them on their way while
+// one is used.
+template <class T, int D, bool BIAS, int RING>
 __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
-  __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];
+  __shared__ __attribute__((aligned(1024))) u16 ring[RING][2 * KE];
+  __shared__ uint16_t start[BIAS ? kMaxBucketSide : 1];
   extern __shared__ __attribute__((aligned(16))) float bt[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
   const int n_rows = BIAS ? p.Lq : p.G * p.Lq, n_rt = (n_rows + kRows - 1) / kRows;
   const int lid = xcd_remap(blockIdx.x, p.n_wg);
   const int unit = unit_at(p, lid / (n_rt * p.splits), BIAS ? p.H : p.Hk), split = lid / n_rt % p.splits, r0 = lid % n_rt * kRows;
-  const int r = r0 + wave * 32 + c32;
+  const int rw = r0 + wave * 32, r = rw + c32;           // first row of the wave, row of the lane
   const bool row_ok = r < n_rows;
   const RowOf ro = row_of<BIAS>(p, unit, row_ok ? r : 0);
   const int b = BIAS ? unit / p.H : unit / p.Hk, hk = BIAS ? (unit % p.H) / p.G : unit % p.Hk;
@@ -117,58 +119,67 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
   const int nt = (kend + 63) / 64;
   const int t0 = (int)((int64_t)nt * split / p.splits), t1 = (int)((int64_t)nt * (split + 1) / p.splits);
 
-  if (BIAS) {
-    uint16_t* start = reinterpret_cast<uint16_t*>(ring);
-    fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
-    __syncthreads();
-  }
-  typename T::x8 qf[D / 16];
-  const TwoRows two = two_rows<BIAS>(p, unit, r0 + wave * 32, n_rows, lane);
-  load_tile<T, D>(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane, qf);
-
-  Rows<T, D> acc;
-  acc.init();
   TileLoad<D, NW> lk, lv;
   lk.init(wave, lane, p.sk.t);
   lv.init(wave, lane, p.sv.t);
   const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
   const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
-  int mb = 1;
-  auto issue = [&](int t) {
-    const uint32_t dst = lds_addr(ring[t & 1]);
+  int mb[RING];
+  auto issue = [&](auto slot, int t) {
+    const uint32_t dst = lds_addr(ring[0]) + slot * 4 * KE;
     lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
     lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
-    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, fresh(lane));
+    if (p.key_mask) mb[slot] = mask_byte(p, b, t * 64, n, fresh(lane));
   };
-  const int ka0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
+  static_for<RING>([&](auto u) {
+    mb[u] = 1;
+    if (u < RING - 1 && t0 + u < t1) issue(u, t0 + u);
+  });
+  typename T::x8 qf[D / 16];
+  const TwoRows two = two_rows<BIAS>(p, unit, rw, n_rows, lane);
+  load_tile<T, D>(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane, qf);
+  if (BIAS) fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
+
+  Rows<T, D> acc;
+  acc.init();
+  // This lane's places in slot 0; the slots lie at constant distances.
+  const u16* kp[D / 16];
+  const u16* vp[D / 32][2];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) kp[ks] = ring[0] + (row_lane<D>(c32, hw) ^ (8 * row_chunk(ks)));
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) vp[d][h] = ring[0] + KE + (col_lane<D>(lane) ^ (16 * h) ^ (32 * d));
   // Key minus query position of this lane's first key of tile 0.
   const int rel0 = 4 * hw - (ro.i + off);
 
-  if (t0 < t1) issue(t0);
-  for (int t = t0; t < t1; ++t) {
-    wait_vmem();
-    const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb != 0) : ~0ull);
+  auto tile = [&](auto u, int t) {
+    // This tile is there when no more than the younger ones' loads are left.
+    constexpr int YOUNGER = (RING - 2) * 2 * TileLoad<D, NW>::PER;
+    static_assert(YOUNGER < 16, "fits the wait's low bits");
+    if (RING > 2 && t + RING - 2 < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | YOUNGER);
+    else wait_vmem();
+    const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb[u] != 0) : ~0ull);
     __syncthreads();
-    if (t + 1 < t1) issue(t + 1);
-    const int ka = fresh(ka0), ca = fresh(ca0);
-    u16* sK = ring[t & 1];
-    u16* sV = sK + KE;
+    if (t + RING - 1 < t1) issue(integral_constant<int, (u + RING - 1) % RING>{}, t + RING - 1);
     if (keep != ~0ull) {
-      if (keep == 0) continue;
-      clear_rows<D, 256>(sV, keep, fresh(tid));
+      if (keep == 0) return;
+      clear_rows<D, 256>(ring[u] + KE, keep, fresh(tid));
       __syncthreads();
     }
+    // A wave without rows, or whose rows come before all of these keys.
+    if (rw >= n_rows || (BIAS && p.rb.causal && t * 64 > rw + 31 + off)) return;
     f32x16 x[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       x[g] = f32x16{};
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks)
-        x[g] = T::mfma(read_row<T>(sK + (ka ^ (8 * row_chunk(ks))) + 32 * g * D), qf[ks], x[g]);
+        x[g] = T::mfma(read_row<T>(kp[ks] + u * 2 * KE + 32 * g * D), qf[ks], x[g]);
     }
-    const int rel = rel0 + t * 64;                       // of this lane's first key of the tile
     if (BIAS) {
-      const int far = p.rb.far, lo = t * 64 - (r0 + wave * 32 + 31 + off), hi = t * 64 + 63 - (r0 + wave * 32 + off);
+      const int far = p.rb.far, lo = t * 64 - (rw + 31 + off), hi = t * 64 + 63 - (rw + off);
       if (lo >= far || hi <= -far) {
         const float c = bt[lo >= far ? 2 * (far + kPad) : 0];
 #pragma unroll
@@ -176,7 +187,7 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[g][e] = fmaf(x[g][e], p.sl2, c);
       } else {
-        const float* at = bt + (row_ok ? rel : lo) + far + kPad;
+        const float* at = bt + (row_ok ? rel0 + t * 64 : lo) + far + kPad;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -196,9 +207,15 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        acc.o[d] = T::mfma(read_col<T, D>(sV, ca, d, 16 * s), pb[s >> 1][s & 1], acc.o[d]);
-  }
+      for (int s = 0; s < 4; ++s) {
+        const int row = u * 128 + 16 * s;                  // a slot is two tiles of 64 rows
+        acc.o[d] = T::mfma(read_cols<T>(vp[d][0] + row * D, vp[d][1] + (row + 8) * D), pb[s >> 1][s & 1], acc.o[d]);
+      }
+  };
+  for (int t = t0; t < t1; t += RING)
+    static_for<RING>([&](auto u) {
+      if (t + u < t1) tile(u, t + u);
+    });
 
   const float l = both_halves_sum(acc.l);
   const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
@@ -381,9 +398,17 @@ static hipError_t run_fwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   }
   p.n_wg = (int)(units * ((rows + kRows - 1) / kRows) * p.splits);
   if (p.n_wg == 0) return hipSuccess;
-  if (bias)
-    hipLaunchKernelGGL((cross_fwd_kernel<T, D, true>), dim3(p.n_wg), dim3(256), bias_entries(p.rb.far) * 4, st, p);
-  else hipLaunchKernelGGL((cross_fwd_kernel<T, D, false>), dim3(p.n_wg), dim3(256), 0, st, p);
+  // Few rows are a matter of bytes on their way: at d 64 three tiles per
+  // workgroup then, where one leaves room for a third workgroup per CU.
+  constexpr int DEEP = D == 64 ? 4 : 2;
+  const uint32_t lds = bias ? bias_entries(p.rb.far) * 4 : 0;
+  if (rows <= 32) {
+    if (bias) hipLaunchKernelGGL((cross_fwd_kernel<T, D, true, DEEP>), dim3(p.n_wg), dim3(256), lds, st, p);
+    else hipLaunchKernelGGL((cross_fwd_kernel<T, D, false, DEEP>), dim3(p.n_wg), dim3(256), lds, st, p);
+  } else {
+    if (bias) hipLaunchKernelGGL((cross_fwd_kernel<T, D, true, 2>), dim3(p.n_wg), dim3(256), lds, st, p);
+    else hipLaunchKernelGGL((cross_fwd_kernel<T, D, false, 2>), dim3(p.n_wg), dim3(256), lds, st, p);
+  }
   if (p.splits > 1) {
     const int64_t all = (int64_t)p.B * p.H * p.Lq;
     hipLaunchKernelGGL((cross_join_kernel<T, D>), dim3((uint32_t)all), dim3(256), 0, st, p);
