@@ -57,6 +57,7 @@ struct CrossParams {
 // workspace size, the launches and the results follow the shape.
 struct CrossPlan {
   bool resident;                       // the keys of a head stay in LDS, splits workgroups share its rows
+  bool small;                          // backward: queries and keys of a head fit in LDS, one kernel does all
   int splits, kv_splits;
   int64_t part_o, part_ml, row_ld, part_kv, part_t;   // byte offsets into the workspace
   int64_t bytes;

@@ -24,14 +24,15 @@ template <class T, int D, bool BIAS>
 __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
   __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];
-  extern __shared__ __attribute__((aligned(16))) float bt[];     // the bias, then sums of dS per diagonal
+  __shared__ uint16_t start[BIAS ? kMaxBucketSide : 1];
+  extern __shared__ __attribute__((aligned(16))) float bt[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
 
   const int n_rows = BIAS ? p.Lq : p.G * p.Lq, n_rt = (n_rows + kDqRows - 1) / kDqRows;
   const int lid = xcd_remap(blockIdx.x, p.n_wg);
   const int unit = unit_at(p, lid / (n_rt * p.splits), BIAS ? p.H : p.Hk), split = lid / n_rt % p.splits, r0 = lid % n_rt * kDqRows;
-  const int r = r0 + wave * 32 + c32;
+  const int rw = r0 + wave * 32, r = rw + c32;             // first row of the wave, row of the lane
   const bool row_ok = r < n_rows;
   const RowOf ro = row_of<BIAS>(p, unit, row_ok ? r : 0);
   const int b = BIAS ? unit / p.H : unit / p.Hk, hk = BIAS ? (unit % p.H) / p.G : unit % p.Hk;
@@ -45,12 +46,26 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   const int nt = (kend + 63) / 64;
   const int t0 = (int)((int64_t)nt * split / p.splits), t1 = (int)((int64_t)nt * (split + 1) / p.splits);
 
+  TileLoad<D, NW> lk, lv;
+  lk.init(wave, lane, p.sk.t);
+  lv.init(wave, lane, p.sv.t);
+  const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+  const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+  int mb = 1;
+  auto issue = [&](auto slot, int t) {
+    const uint32_t dst = lds_addr(ring[0]) + slot * 4 * KE;
+    lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
+    lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
+    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, fresh(lane));
+  };
+  if (t0 < t1) issue(integral_constant<int, 0>{}, t0);
+
   const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
+  const TwoRows two = two_rows<BIAS>(p, unit, rw, n_rows, lane);
   typename T::x8 qf[D / 16], gf[D / 16];
-  const TwoRows two = two_rows<BIAS>(p, unit, r0 + wave * 32, n_rows, lane);
   load_tile<T, D>(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane, qf);
   load_tile<T, D>(at(p.dout, p.sdo, two.a), two.a_ok, at(p.dout, p.sdo, two.b), two.b_ok, lane, gf);
-  float lse2 = INFINITY, delta = 0.f;                      // a row without a key: every weight 0
+  float nlse2 = -INFINITY, delta = 0.f;                    // -log2-LSE; a row without a key: every weight 0
   {
     typename T::x8 of[D / 16];
     load_tile<T, D>(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane, of);
@@ -60,73 +75,64 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
       for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
     delta = both_halves_sum(delta);
     const float z = row_ok ? p.lse[row] : -INFINITY;
-    if (z != -INFINITY) lse2 = z * kLog2e;
-    if (p.splits > 1 && row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(-lse2 / p.sl2, -delta);
+    if (z != -INFINITY) nlse2 = -z * kLog2e;
   }
-  float exact = 0.f;                                       // delta again, as the sum of P dP in fp32
+  if (BIAS) fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
+  float more = 0.f;                                        // sum of dS: what delta lacks
 
   f32x16 acc[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
-  TileLoad<D, NW> lk, lv;
-  lk.init(wave, lane, p.sk.t);
-  lv.init(wave, lane, p.sv.t);
-  const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
-  const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
-  int mb = 1;
-  auto issue = [&](int t) {
-    const uint32_t dst = lds_addr(ring[t & 1]);
-    lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
-    lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
-    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, fresh(lane));
-  };
-  const int ka0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
+  // This lane's places in slot 0; the slots lie at constant distances.
+  const u16* kp[D / 16];
+  const u16* kcol[D / 32][2];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) kp[ks] = ring[0] + (row_lane<D>(c32, hw) ^ (8 * row_chunk(ks)));
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) kcol[d][h] = ring[0] + (col_lane<D>(lane) ^ (16 * h) ^ (32 * d));
   const int rel0 = 4 * hw - (ro.i + off);
 
-  if (t0 < t1) issue(t0);
-  if (BIAS) {
-    __shared__ uint16_t start[kMaxBucketSide];
-    fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
-  }
-  for (int t = t0; t < t1; ++t) {
+  auto tile = [&](auto u, int t) {
     wait_vmem();
     const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb != 0) : ~0ull);
     __syncthreads();
-    if (t + 1 < t1) issue(t + 1);
-    const int ka = fresh(ka0), ca = fresh(ca0);
-    u16* sK = ring[t & 1];
-    u16* sV = sK + KE;
+    if (t + 1 < t1) issue(integral_constant<int, 1 - u>{}, t + 1);
     if (keep != ~0ull) {
-      if (keep == 0) continue;
-      clear_rows<D, 256>(sK, keep, fresh(tid));
-      clear_rows<D, 256>(sV, keep, fresh(tid));
+      if (keep == 0) return;
+      clear_rows<D, 256>(ring[u], keep, fresh(tid));
+      clear_rows<D, 256>(ring[u] + KE, keep, fresh(tid));
       __syncthreads();
     }
-    const int far = BIAS ? p.rb.far : 0, rel = rel0 + t * 64;
+    // A wave without rows, or whose rows come before all of these keys.
+    if (rw >= n_rows || (BIAS && p.rb.causal && t * 64 > rw + 31 + off)) return;
+    const int far = BIAS ? p.rb.far : 0;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      f32x16 x = f32x16{}, y = f32x16{};
+      const int row0 = u * 128 + 32 * g;                   // a slot is two tiles of 64 rows
+      f32x16 x = f32x16{}, y;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] = -delta;          // dP's sums begin at -delta
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
-        x = T::mfma(read_row<T>(sK + (ka ^ (8 * row_chunk(ks))) + 32 * g * D), qf[ks], x);
-        y = T::mfma(read_row<T>(sV + (ka ^ (8 * row_chunk(ks))) + 32 * g * D), gf[ks], y);
+        x = T::mfma(read_row<T>(kp[ks] + row0 * D), qf[ks], x);
+        y = T::mfma(read_row<T>(kp[ks] + KE + row0 * D), gf[ks], y);
       }
-      // The 32 x 32 block's smallest and largest key minus query position.
-      const int lo = t * 64 + 32 * g - (r0 + wave * 32 + 31 + off), hi = lo + 62;
-      const bool above = lo >= far, beyond = BIAS && (above || hi <= -far);
       if (BIAS) {
-        if (beyond) {
-          const float c = bt[above ? 2 * (far + kPad) : 0] - lse2;
+        const int lo = t * 64 + 32 * g - (rw + 31 + off);  // the block's smallest key minus query position
+        if (lo >= far || lo <= -far - 62) {
+          const float c = bt[lo >= far ? 2 * (far + kPad) : 0] + nlse2;
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, c);
         } else {
-          const float* at = bt + (row_ok ? rel + 32 * g : lo) + far + kPad;
+          const float* at = bt + (row_ok ? rel0 + t * 64 + 32 * g : lo) + far + kPad;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[8 * (e >> 2) + (e & 3)] - lse2);
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[8 * (e >> 2) + (e & 3)] + nlse2);
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, -lse2);
+        for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, nlse2);
       }
       if (keep != ~0ull) {
         const uint32_t mine = (uint32_t)(keep >> (32 * g)) >> (4 * hw);
@@ -136,21 +142,27 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
       }
       u32x4 w[2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[e] = fast_exp2(x[e]);
-        exact = fmaf(x[e], y[e], exact);
-        y[e] = x[e] * (y[e] - delta);
-      }
+      for (int e = 0; e < 16; ++e) y[e] *= fast_exp2(x[e]);
+      float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+      for (int e = 0; e < 16; e += 2) {
+        s0 += y[e];
+        s1 += y[e + 1];
+        w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+      }
+      more += s0 + s1;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const typename T::x8 ds = __builtin_bit_cast(typename T::x8, w[s]);
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
-          acc[d] = T::mfma(read_col<T, D>(sK, ca, d, 32 * g + 16 * s), ds, acc[d]);
+          acc[d] = T::mfma(read_cols<T>(kcol[d][0] + (row0 + 16 * s) * D, kcol[d][1] + (row0 + 16 * s + 8) * D), ds, acc[d]);
       }
     }
+  };
+  for (int t = t0; t < t1; t += 2) {
+    tile(integral_constant<int, 0>{}, t);
+    if (t + 1 < t1) tile(integral_constant<int, 1>{}, t + 1);
   }
 
   if (p.splits > 1) {
@@ -159,10 +171,11 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   } else {
     store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, two.a), two.a_ok, at(p.dq, p.sdq, two.b), two.b_ok, lane);
   }
-  // What cross_dkv_kernel takes as delta: the sum of P dP, free of the output's
-  // rounding; where the keys are split, the one from the rounded output.
-  exact = both_halves_sum(exact);
-  if (p.splits == 1 && row_ok && hw == 0) p.row_ld[row] = make_float2(-lse2 / p.sl2, -exact);
+  // What cross_dkv_kernel takes as delta is free of the output's rounding: the
+  // weights add up to 1, so the sum of P dP is delta and the sum of dS.  Where
+  // the keys are split, it is the one from the rounded output.
+  const float exact = delta + (p.splits > 1 ? 0.f : both_halves_sum(more));
+  if (row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(nlse2 / p.sl2, -exact);
 }
 
 // dq with few keys: they stay in LDS, as in the forward pass, and each wave
@@ -290,6 +303,295 @@ __device__ __forceinline__ void add_diagonals(const f32x16& x, float* at, int la
 constexpr int kDiagPad = 62;           // diagonals of a block near the diagonal that lie beyond far
 __host__ __device__ __forceinline__ int diag_entries(int far) { return 2 * (far + kDiagPad) + 1; }
 
+// A workgroup's sums of dS for the head it is at: by diagonal in LDS (each wave
+// its own, so that their order is the program's), and beyond far on either side
+// in registers.  They lie behind the bias table bt.
+template <int NW>
+struct TableSums {
+  float *bt, *all, *mine;
+  float (*far_sum)[NW];
+  const uint16_t* start;
+  int far, nd, buckets, wave, lane, tid;
+  float below, above;
+  __device__ __forceinline__ TableSums(const CrossParams& p, float* bt, float (*far_sum)[NW], const uint16_t* start, int far,
+                                       int wave, int lane, int tid)
+      : bt(bt), all(bt + bias_entries(far)), far_sum(far_sum), start(start), far(far), nd(diag_entries(far)),
+        buckets(p.rb.both ? 2 * p.rb.side : p.rb.side), wave(wave), lane(lane), tid(tid), below(0.f), above(0.f) {
+    mine = all + wave * nd;
+  }
+  __device__ __forceinline__ void clear() {
+    for (int i = tid; i < NW * nd; i += 64 * NW) all[i] = 0.f;
+  }
+  // dS of a block whose smallest key minus query position is lo.
+  __device__ __forceinline__ void add(const f32x16& ds, int lo) {
+    if (lo >= far || lo <= -far - 62) {
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s += ds[e];
+      if (lo >= far) above += s;
+      else below += s;
+    } else {
+      add_diagonals(ds, mine + lo + far + kDiagPad, lane);
+    }
+  }
+  // Writes the share and starts over (the bias table is overwritten).
+  __device__ __forceinline__ void flush(const CrossParams& p, float* share) {
+    const float lo = wave_sum(below), hi = wave_sum(above);
+    below = above = 0.f;
+    if (lane == 0) {
+      far_sum[0][wave] = lo;
+      far_sum[1][wave] = hi;
+    }
+    __syncthreads();
+    for (int i = tid; i < nd; i += 64 * NW) {
+      float s = 0.f;
+      for (int w = 0; w < NW; ++w) {
+        s += all[w * nd + i];
+        all[w * nd + i] = 0.f;
+      }
+      bt[i] = s;
+    }
+    __syncthreads();
+    const int mid = far + kDiagPad;
+    for (int u = wave; u < buckets; u += NW) {
+      const bool ahead = u >= p.rb.side;
+      const int m = ahead ? u - p.rb.side : u;
+      const bool last = m == p.rb.side - 1;
+      int d = start[m];
+      const int d1 = last ? mid + 1 : start[m + 1];
+      if (ahead && d == 0) d = 1;
+      float s = 0.f;
+      for (d += lane; d < d1; d += 64) s += bt[ahead ? mid + d : mid - d];
+      if (!p.rb.both && u == 0)                           // one direction: every key after the query
+        for (int i = mid + 1 + lane; i < nd; i += 64) s += bt[i];
+      s = wave_sum(s);
+      if (last)
+        for (int w = 0; w < NW; ++w) s += far_sum[ahead][w];
+      if (!p.rb.both && u == 0)
+        for (int w = 0; w < NW; ++w) s += far_sum[1][w];
+      if (lane == 0) share[u] = s;
+    }
+    __syncthreads();
+  }
+};
+
+// The whole backward pass of one (sample, key head) whose queries and keys both
+// fit in LDS (256 of each at d 64, 128 at d 128), in one launch: a wave takes 32
+// rows for dq and delta, then, with the rows' statistics in LDS, 32 keys for dk
+// and dv.  A text encoder's prompts are of this size, and three launches one
+// after the other cost more than their work (8 x 24 heads x 226 tokens, d 64:
+// see the kernels' times in the design notes).
+template <int D>
+constexpr int kSmallWaves = D == 64 ? 8 : 4;
+constexpr int kSmallFar = 256;         // the most far with which the sums by diagonal fit as well
+
+template <class T, int D, bool BIAS>
+__global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_small_bwd_kernel(const CrossParams p) {
+  constexpr int NW = kSmallWaves<D>, NT = 64 * NW, L = 32 * NW, TILES = L / 64;
+  __shared__ __attribute__((aligned(1024))) u16 sQ[L * D], sG[L * D], sK[L * D], sV[L * D];
+  __shared__ __attribute__((aligned(16))) float st[2][L]; // -LSE / scale and -delta of the rows
+  __shared__ float mask[L];                               // 0 or -inf per key
+  __shared__ uint16_t start[BIAS ? kMaxBucketSide : 1];
+  __shared__ float far_sum[2][NW];
+  extern __shared__ __attribute__((aligned(16))) float bt[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+  const int unit = unit_at(p, xcd_remap(blockIdx.x, p.n_wg), p.Hk), b = unit / p.Hk, hk = unit % p.Hk;
+  const int n = key_count(p, b), off = query_offset(p, n), far = BIAS ? p.rb.far : 0;
+  const int rw = wave * 32;                               // the wave's first row, and first key
+  const int nkb = (n + 31) / 32, nqb = (p.Lq + 31) / 32;
+
+  TileLoad<D, NW> ld;
+  auto load = [&](u16* dst, const u16* first, int64_t stride, int count) {
+    ld.init(wave, lane, stride);
+    for (int t = 0; t < TILES; ++t)
+      if (t * 64 < count) ld.issue(__builtin_amdgcn_readfirstlane(lds_addr(dst + t * 64 * D)), first + t * 64 * stride, stride, count - t * 64);
+  };
+  const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+  const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+  load(sK, kh, p.sk.t, n);
+  load(sV, vh, p.sv.t, n);
+  load(sQ, p.q + b * p.sq.b + hk * p.G * p.sq.h, p.sq.t, p.Lq);
+  load(sG, p.dout + b * p.sdo.b + hk * p.G * p.sdo.h, p.sdo.t, p.Lq);
+  auto visible = [&](int key) { return key < n && !(p.key_mask && p.key_mask[b * p.mask_stride + key] == 0); };
+  if (tid < L) mask[tid] = visible(tid) ? 0.f : -INFINITY;
+  TableSums<NW> table(p, bt, far_sum, start, far, wave, lane, tid);
+  if (BIAS) table.clear();
+  wait_vmem();
+  __syncthreads();
+  // Whatever the loads have left out or a mask hides is zero.
+  for (int i = tid; i < L * (D / 8); i += NT) {
+    const int row = i / (D / 8);
+    if (mask[row] != 0.f) {
+      *reinterpret_cast<u32x4*>(sK + i * 8) = u32x4{0, 0, 0, 0};
+      *reinterpret_cast<u32x4*>(sV + i * 8) = u32x4{0, 0, 0, 0};
+    }
+    if (row >= p.Lq) {
+      *reinterpret_cast<u32x4*>(sQ + i * 8) = u32x4{0, 0, 0, 0};
+      *reinterpret_cast<u32x4*>(sG + i * 8) = u32x4{0, 0, 0, 0};
+    }
+  }
+  __syncthreads();
+
+  const int ra0 = row_lane<D>(c32, hw), ca0 = col_lane<D>(lane);
+  const bool key_ok = mask[rw + c32] == 0.f;
+  uint32_t whole = 0;                                     // blocks of 32 keys that are all visible
+  for (int j = 0; j < nkb; ++j)
+    if (__all(mask[32 * j + c32] == 0.f)) whole |= 1u << j;
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f32x16{};
+
+  for (int g = 0; g < p.G; ++g) {
+    const int h = hk * p.G + g;
+    if (g > 0) {                                          // the next query head that shares these keys
+      load(sQ, p.q + b * p.sq.b + h * p.sq.h, p.sq.t, p.Lq);
+      load(sG, p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.t, p.Lq);
+    }
+    if (BIAS) fill_bias<T, NT>(bt, start, p, h, tid);
+    wait_vmem();
+    __syncthreads();
+
+    // dq of rows rw .. rw + 31.
+    {
+      const int i = rw + c32;
+      const int64_t row = ((int64_t)b * p.H + h) * p.Lq + i;
+      const RowOf lower = {b, h, rw + (lane & 15)}, upper = {b, h, rw + (lane & 15) + 16};
+      const bool a_ok = lower.i < p.Lq, b_ok = upper.i < p.Lq;
+      const int ra = fresh(ra0);
+      typename T::x8 qf[D / 16], gf[D / 16], of[D / 16];
+      const u16* out = p.out;
+      load_tile<T, D>(at(out, p.so, lower), a_ok, at(out, p.so, upper), b_ok, lane, of);
+      const float z = i < p.Lq ? p.lse[row] : -INFINITY;
+      const float nlse2 = z == -INFINITY ? -INFINITY : -z * kLog2e;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        qf[ks] = read_row<T>(sQ + (ra ^ (8 * row_chunk(ks))) + rw * D);
+        gf[ks] = read_row<T>(sG + (ra ^ (8 * row_chunk(ks))) + rw * D);
+      }
+      float delta = 0.f, more = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
+      delta = both_halves_sum(delta);
+      f32x16 acc[D / 32];
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
+      if (rw < p.Lq) {
+        for (int j = 0; j < nkb; ++j) {
+          const int ra = fresh(ra0), ca = fresh(ca0);
+          const u16* tK = sK + 32 * j * D;
+          const u16* tV = sV + 32 * j * D;
+          const int lo = 32 * j - (rw + 31 + off);        // the block's smallest key minus query position
+          if (BIAS && p.rb.causal && lo > 0) break;
+          f32x16 x = f32x16{}, y;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) y[e] = -delta;
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            x = T::mfma(read_row<T>(tK + (ra ^ (8 * row_chunk(ks)))), qf[ks], x);
+            y = T::mfma(read_row<T>(tV + (ra ^ (8 * row_chunk(ks)))), gf[ks], y);
+          }
+          const float* at = bt + bias_from(lo, far) + far + kPad + 31 + 4 * hw - c32;
+          u32x4 w[2];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, BIAS ? at[8 * (e >> 2) + (e & 3)] + nlse2 : nlse2);
+          if (!((whole >> j) & 1)) {
+            const float* hide = mask + 32 * j + 4 * hw;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] += hide[8 * (e >> 2) + (e & 3)];
+          }
+          float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            y[e] *= fast_exp2(x[e]);
+            y[e + 1] *= fast_exp2(x[e + 1]);
+            s0 += y[e];
+            s1 += y[e + 1];
+          }
+          more += s0 + s1;
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+              acc[d] = T::mfma(read_col<T, D>(tK, ca, d, 16 * s), __builtin_bit_cast(typename T::x8, w[s]), acc[d]);
+        }
+      }
+      // The statistics that dk and dv take: delta free of the output's rounding.
+      more = both_halves_sum(more);
+      if (hw == 0) {
+        st[0][i] = nlse2 / p.sl2;                         // past the last row -inf: weight 0
+        st[1][i] = -(delta + more);
+      }
+      store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, lower), a_ok, at(p.dq, p.sdq, upper), b_ok, lane);
+    }
+    __syncthreads();
+
+    // dk and dv of keys rw .. rw + 31.
+    if (rw < n) {
+      const int ra = fresh(ra0);
+      typename T::x8 kf[D / 16], vf[D / 16];
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        kf[ks] = read_row<T>(sK + (ra ^ (8 * row_chunk(ks))) + rw * D);
+        vf[ks] = read_row<T>(sV + (ra ^ (8 * row_chunk(ks))) + rw * D);
+      }
+      const int first = BIAS && p.rb.causal && rw - off > 0 ? (rw - off) / 32 : 0;
+      for (int i = first; i < nqb; ++i) {
+        const int ra = fresh(ra0), ca = fresh(ca0);
+        const u16* tQ = sQ + 32 * i * D;
+        const u16* tG = sG + 32 * i * D;
+        const int lo = rw - (32 * i + 31 + off);
+        f32x16 x, y;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          x[e] = st[0][32 * i + 8 * (e >> 2) + 4 * hw + (e & 3)];
+          y[e] = st[1][32 * i + 8 * (e >> 2) + 4 * hw + (e & 3)];
+        }
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          x = T::mfma(read_row<T>(tQ + (ra ^ (8 * row_chunk(ks)))), kf[ks], x);
+          y = T::mfma(read_row<T>(tG + (ra ^ (8 * row_chunk(ks)))), vf[ks], y);
+        }
+        const float* at = bt + bias_entries(far) - 1;     // a masked key's: -inf
+        if (BIAS && key_ok) at = bt + bias_from(lo, far) + far + kPad + 31 + c32 - 4 * hw;
+        u32x4 wp[2], ws[2];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const int r = 8 * (e >> 2) + (e & 3);
+          const float a = fast_exp2(BIAS ? fmaf(x[e], p.sl2, at[-r]) : x[e] * p.sl2);
+          const float c = fast_exp2(BIAS ? fmaf(x[e + 1], p.sl2, at[-r - 1]) : x[e + 1] * p.sl2);
+          y[e] *= a;
+          y[e + 1] *= c;
+          wp[e >> 3][(e & 7) >> 1] = T::pack(a, c);
+          ws[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+        }
+        if (BIAS) table.add(y, lo);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) {
+            dv[d] = T::mfma(read_col<T, D>(tG, ca, d, 16 * s), __builtin_bit_cast(typename T::x8, wp[s]), dv[d]);
+            dk[d] = T::mfma(read_col<T, D>(tQ, ca, d, 16 * s), __builtin_bit_cast(typename T::x8, ws[s]), dk[d]);
+          }
+      }
+    }
+    __syncthreads();
+    if (BIAS) table.flush(p, p.part_t + ((int64_t)b * p.H + h) * table.buckets);
+  }
+  if (!key_ok) {                                          // a masked key took part with a row of zeros
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f32x16{};
+  }
+  const RowOf lower = {b, hk, rw + (lane & 15)}, upper = {b, hk, rw + (lane & 15) + 16};
+  const bool a_ok = lower.i < p.Lk, b_ok = upper.i < p.Lk;
+  store_tile<T, D>(dk, p.scale, at(p.dk, p.sdk, lower), a_ok, at(p.dk, p.sdk, upper), b_ok, lane);
+  store_tile<T, D>(dv, 1.f, at(p.dv, p.sdv, lower), a_ok, at(p.dv, p.sdv, upper), b_ok, lane);
+}
+
 // dk and dv of 32 keys per wave, over one range of the (query head, 64-row
 // query tile) items that see them.
 //
@@ -383,52 +685,13 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
     for (int i = 0; i < 6; ++i) (&ld[0][0][0])[64 * i + tid] = 0.f;
   for (int c = tid; c < 3 * 2 * KE / 8; c += NT) *reinterpret_cast<u32x4*>(&ring[0][0] + c * 8) = u32x4{0, 0, 0, 0};
   __syncthreads();
-  // Bias: sums of dS by diagonal (each wave its own, so that their order is the
-  // program's) and, beyond far, on either side of it.
-  const int far = BIAS ? p.rb.far : 0, nd = diag_entries(far);
-  float* dg = bt + bias_entries(far) + wave * nd;
-  float below = 0.f, above = 0.f;
+  const int far = BIAS ? p.rb.far : 0;
+  TableSums<NW> table(p, bt, far_sum, start, far, wave, lane, tid);
   int head = 0;
-  // The sums of the head that the workgroup leaves become its share of dtable.
+  // The head that the workgroup leaves: its share of dtable.
   auto flush = [&]() {
-    const float lo = wave_sum(below), hi = wave_sum(above);
-    below = above = 0.f;
-    if (lane == 0) {
-      far_sum[0][wave] = lo;
-      far_sum[1][wave] = hi;
-    }
-    __syncthreads();
-    float* all = bt + bias_entries(far);
-    for (int i = tid; i < nd; i += NT) {
-      float s = 0.f;
-      for (int w = 0; w < NW; ++w) {
-        s += all[w * nd + i];
-        all[w * nd + i] = 0.f;
-      }
-      bt[i] = s;                                          // the bias is loaded again for the next head
-    }
-    __syncthreads();
-    const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side, mid = far + kDiagPad;
-    float* share = p.part_t + ((((int64_t)b * p.H + hk * p.G + head) * n_kt + j0 / (32 * NW)) * p.kv_splits + split) * buckets;
-    for (int u = wave; u < buckets; u += NW) {
-      const bool ahead = u >= p.rb.side;
-      const int m = ahead ? u - p.rb.side : u;
-      const bool last = m == p.rb.side - 1;
-      int d = start[m];
-      const int d1 = last ? mid + 1 : start[m + 1];
-      if (ahead && d == 0) d = 1;
-      float s = 0.f;
-      for (d += lane; d < d1; d += 64) s += bt[ahead ? mid + d : mid - d];
-      if (!p.rb.both && u == 0)                           // one direction: every key after the query
-        for (int i = mid + 1 + lane; i < nd; i += 64) s += bt[i];
-      s = wave_sum(s);
-      if (last)
-        for (int w = 0; w < NW; ++w) s += far_sum[ahead][w];
-      if (!p.rb.both && u == 0)
-        for (int w = 0; w < NW; ++w) s += far_sum[1][w];
-      if (lane == 0) share[u] = s;
-    }
-    __syncthreads();
+    table.flush(p, p.part_t + ((((int64_t)b * p.H + hk * p.G + head) * n_kt + j0 / (32 * NW)) * p.kv_splits + split) *
+                                  table.buckets);
     ++head;
   };
   f32x16 x, y;                                            // S and dP of the block in the second stage
@@ -562,15 +825,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
       stage_pack(7);
     }
     if (BIAS) {
-      if (lo >= far || lo <= -far - 62) {
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s += y[e];
-        if (lo >= far) above += s;
-        else below += s;
-      } else {
-        add_diagonals(y, dg + lo + far + kDiagPad, lane);
-      }
+      table.add(y, lo);
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -588,7 +843,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
   };
   if (i0 < i1) issue(0);
   if (BIAS) {
-    for (int i = tid; i < NW * nd; i += NT) bt[bias_entries(far) + i] = 0.f;
+    table.clear();
     fill_bias<T, NT>(bt, start, p, hk * p.G, tid);
   }
   int q0 = in_q, g_head = in_h - hk * p.G;                // of the current item
@@ -729,6 +984,13 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   CrossPlan c{};
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), tiles = units * row_tiles(p, bias);
   const int64_t nt = (p.Lk + 63) / 64;
+  const int fit = 32 * (D == 64 ? kSmallWaves<64> : kSmallWaves<128>);
+  c.small = p.Lq > 0 && p.Lq <= fit && p.Lk <= fit && (!bias || p.rb.far <= kSmallFar);
+  if (c.small) {
+    c.splits = c.kv_splits = 1;
+    c.bytes = bias ? up256((int64_t)p.B * p.H * (p.rb.both ? 2 : 1) * p.rb.side * 4) : 0;
+    return c;
+  }
   c.splits = tiles > 0 && tiles < 256 ? clamp_splits(512 / tiles, nt / 4) : 1;
   c.resident = keep_keys(p, D, bias, 1);
   if (c.resident) c.splits = keep_chunks(p, 1);
@@ -770,6 +1032,19 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   const int64_t units = (int64_t)p.B * (bias ? p.H : p.Hk), rt = row_tiles(p, bias);
   const int64_t rows = (int64_t)p.B * p.H * p.Lq, keys = (int64_t)p.B * p.Hk * p.Lk;
   const uint32_t lds = bias ? bias_entries(p.rb.far) * 4 : 0, per = 256 / (D / 4);
+  const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
+  const dim3 table(p.H, (buckets + 31) / 32);
+  if (c.small) {
+    p.n_wg = p.B * p.Hk;
+    constexpr int NW = kSmallWaves<D>;
+    if (p.n_wg > 0 && !bias)
+      hipLaunchKernelGGL((cross_small_bwd_kernel<T, D, false>), dim3(p.n_wg), dim3(64 * NW), 0, st, p);
+    if (p.n_wg > 0 && bias)
+      hipLaunchKernelGGL((cross_small_bwd_kernel<T, D, true>), dim3(p.n_wg), dim3(64 * NW),
+                         lds + NW * diag_entries(p.rb.far) * 4, st, p);
+    if (bias) hipLaunchKernelGGL((cross_dtable_kernel<T>), table, dim3(256), 0, st, p, 1);
+    return hipGetLastError();
+  }
   p.n_wg = (int)(units * (c.resident ? 1 : rt) * p.splits);
   if (c.resident) {
     hipLaunchKernelGGL((cross_keep_dq_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves), keep_lds_bytes(p.Lk), st, p);
@@ -791,11 +1066,9 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
       hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((keys + per - 1) / per), 2), dim3(256), 0, st, dk, dv,
                          2 * keys * D, p.kv_splits, keys, p.Hk, p.Lk);
   }
-  if (bias) {
-    const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
-    hipLaunchKernelGGL((cross_dtable_kernel<T>), dim3(p.H, (buckets + 31) / 32), dim3(256), 0, st, p,
+  if (bias)
+    hipLaunchKernelGGL((cross_dtable_kernel<T>), table, dim3(256), 0, st, p,
                        (int)((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves) * p.kv_splits));
-  }
   return hipGetLastError();
 }
 

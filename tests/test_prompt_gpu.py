@@ -361,7 +361,7 @@ def test_graph_replays_match_eager_calls():
 # --- refusals ---------------------------------------------------------------------
 
 def test_refusals():
-    q, k, v, g = make(2, 4, 2, 8, 9, 64, BF)
+    q, k, v, g = make(2, 4, 2, 300, 9, 64, BF)
     table = table_of(32, 4)
     out, lse = ad.cross_attn(q, k, v)
     err = pytest.raises(ad.AdaspaError)
