@@ -18,11 +18,19 @@ namespace adaspa {
 namespace {
 constexpr int kDqRows = 128;           // query rows of a workgroup of cross_dq_kernel
 constexpr int kDkvWaves = 4;           // waves of 32 keys of a workgroup of cross_dkv_kernel
+// delta from the rounded output is off by about its rounding, which dq carries
+// times sum_j P_ij k_j.  Where registers allow that sum next to dq (d 64), dq is
+// put right by it once the row's exact delta is known: dq's error against 64 bits
+// falls from about 1.5 to 1.4 times that of the final rounding alone (the rest
+// is dS, rounded for the product).
+template <int D>
+constexpr bool kExactDq = D == 64;
 }  // namespace
 
 template <class T, int D, bool BIAS>
 __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
+  constexpr bool EXACT = kExactDq<D>;
   __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];
   __shared__ uint16_t start[BIAS ? kMaxBucketSide : 1];
   extern __shared__ __attribute__((aligned(16))) float bt[];
@@ -80,9 +88,13 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   if (BIAS) fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
   float more = 0.f;                                        // sum of dS: what delta lacks
 
-  f32x16 acc[D / 32];
+  f32x16 acc[D / 32], pk[EXACT ? D / 32 : 1];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
+  if (EXACT) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) pk[EXACT ? d : 0] = f32x16{};
+  }
   // This lane's places in slot 0; the slots lie at constant distances.
   const u16* kp[D / 16];
   const u16* kcol[D / 32][2];
@@ -108,10 +120,10 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     // A wave without rows, or whose rows come before all of these keys.
     if (rw >= n_rows || (BIAS && p.rb.causal && t * 64 > rw + 31 + off)) return;
     const int far = BIAS ? p.rb.far : 0;
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    // P and dP - delta of the tile's keys 32 g and on.
+    auto block = [&](int g, f32x16& x, f32x16& y) {
       const int row0 = u * 128 + 32 * g;                   // a slot is two tiles of 64 rows
-      f32x16 x = f32x16{}, y;
+      x = f32x16{};
 #pragma unroll
       for (int e = 0; e < 16; ++e) y[e] = -delta;          // dP's sums begin at -delta
 #pragma unroll
@@ -140,23 +152,47 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
         for (int e = 0; e < 16; ++e)
           if (!((mine >> (8 * (e >> 2) + (e & 3))) & 1)) x[e] = -INFINITY;
       }
-      u32x4 w[2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] *= fast_exp2(x[e]);
+      for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
+    };
+    if (!EXACT && nt == 1) {                               // all keys are here: delta exactly, before dS
+      float s = 0.f;
+      delta = 0.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        f32x16 x, y;
+        block(g, x, y);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s = fmaf(x[e], y[e], s);
+      }
+      delta = both_halves_sum(s);
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int row0 = u * 128 + 32 * g;
+      f32x16 x, y;
+      block(g, x, y);
+      u32x4 w[2], wp[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] *= x[e];
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         s0 += y[e];
         s1 += y[e + 1];
         w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+        wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
       }
       more += s0 + s1;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const typename T::x8 ds = __builtin_bit_cast(typename T::x8, w[s]);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-          acc[d] = T::mfma(read_cols<T>(kcol[d][0] + (row0 + 16 * s) * D, kcol[d][1] + (row0 + 16 * s + 8) * D), ds, acc[d]);
+        for (int d = 0; d < D / 32; ++d) {
+          const typename T::x8 kf = read_cols<T>(kcol[d][0] + (row0 + 16 * s) * D, kcol[d][1] + (row0 + 16 * s + 8) * D);
+          acc[d] = T::mfma(kf, ds, acc[d]);
+          if (EXACT) pk[EXACT ? d : 0] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wp[s]), pk[EXACT ? d : 0]);
+        }
       }
     }
   };
@@ -165,6 +201,13 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     if (t + 1 < t1) tile(integral_constant<int, 1>{}, t + 1);
   }
 
+  more = p.splits > 1 ? 0.f : both_halves_sum(more);
+  if (EXACT) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[d][e] = fmaf(-more, pk[EXACT ? d : 0][e], acc[d][e]);
+  }
   if (p.splits > 1) {
     const int64_t at = (int64_t)split * p.B * p.H * p.Lq + row;
     store_tile_f32<D>(acc, p.part_o + at * D, row_ok, hw);
@@ -174,7 +217,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   // What cross_dkv_kernel takes as delta is free of the output's rounding: the
   // weights add up to 1, so the sum of P dP is delta and the sum of dS.  Where
   // the keys are split, it is the one from the rounded output.
-  const float exact = delta + (p.splits > 1 ? 0.f : both_halves_sum(more));
+  const float exact = delta + more;
   if (row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(nlse2 / p.sl2, -exact);
 }
 
@@ -183,6 +226,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 template <class T, int D>
 __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq_kernel(const CrossParams p) {
   constexpr int NW = kKeepWaves;
+  constexpr bool EXACT = kExactDq<D>;
   extern __shared__ __attribute__((aligned(1024))) u16 keep_lds[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
@@ -194,6 +238,10 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
   int rt = (int)((int64_t)n_rt * chunk / p.splits) + wave;
 
   const KeptKeys<T, D> keys(p, b, hk, n, keep_lds, wave, lane, tid, []() {});
+  // With one tile of keys S and dP are formed twice, delta exactly from the
+  // first time, and the output is not read at all: that long the rows' way
+  // through memory takes longer than the products.
+  const bool one_tile = keys.nt <= 1;
   for (; rt < rt1; rt += NW) {
     const int r = rt * 32 + c32;
     const int64_t row = (int64_t)unit * n_rows + r;        // a unit's rows are consecutive
@@ -203,30 +251,27 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
       const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, fresh(lane));
       TileRegs<T, D> q, g, o;
       g.load(at(p.dout, p.sdo, two.a), two.a_ok, at(p.dout, p.sdo, two.b), two.b_ok, lane);
-      o.load(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane);
+      if (!one_tile) o.load(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane);
       q.load(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane);
       const float z = r < n_rows ? p.lse[row] : -INFINITY;
       if (z != -INFINITY) nlse2 = -z * kLog2e;
-      typename T::x8 of[D / 16];
       g.operands(gf);
-      o.operands(of);
+      if (!one_tile) {
+        typename T::x8 of[D / 16];
+        o.operands(of);
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
+        for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
-      delta = both_halves_sum(delta);
+          for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
+      }
       q.operands(qf);
     }
-    f32x16 acc[D / 32], from;                              // dP's sums begin at -delta
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
-#pragma unroll
-    for (int e = 0; e < 16; ++e) from[e] = -delta;
-    float more = 0.f;                                      // sum of dS: what delta lacks
-    static_for<2 * KeptKeys<T, D>::TILES>([&](auto j) {
-      constexpr int t = j / 2, row0 = 32 * j;
-      if (t >= keys.nt) return;
-      f32x16 x = f32x16{}, y = from;
+    // P and dP - delta of block j of 32 keys.
+    f32x16 from;                                           // dP's sums begin at -delta
+    auto block = [&](auto j, f32x16& x, f32x16& y) {
+      constexpr int row0 = 32 * j;
+      x = f32x16{};
+      y = from;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         x = T::mfma(read_row<T>(keys.kp[ks] + row0 * D), qf[ks], x);
@@ -234,20 +279,46 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, nlse2);
-      if (!((keys.whole >> t) & 1)) {
+      if (!((keys.whole >> (j / 2)) & 1)) {
         const float* at = keys.mask + row0 + 4 * hw;
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] += at[8 * (e >> 2) + (e & 3)];
       }
-      u32x4 w[2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] *= fast_exp2(x[e]);
+      for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
+    };
+    if (one_tile) {
+      from = f32x16{};
+      static_for<2>([&](auto j) {
+        if (keys.nt == 0) return;
+        f32x16 x, y;
+        block(j, x, y);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) delta = fmaf(x[e], y[e], delta);
+      });
+    }
+    delta = both_halves_sum(delta);
+    f32x16 acc[D / 32], pk[EXACT ? D / 32 : 1];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) acc[d] = pk[EXACT ? d : 0] = f32x16{};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) from[e] = -delta;
+    float more = 0.f;                                      // sum of dS: what delta lacks
+    static_for<2 * KeptKeys<T, D>::TILES>([&](auto j) {
+      constexpr int row0 = 32 * j;
+      if (j / 2 >= keys.nt) return;
+      f32x16 x, y;
+      block(j, x, y);
+      u32x4 w[2], wp[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] *= x[e];
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         s0 += y[e];
         s1 += y[e + 1];
         w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+        wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
       }
       more += s0 + s1;
 #pragma unroll
@@ -257,13 +328,22 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
         for (int d = 0; d < D / 32; ++d) {
           const u16* lo = keys.kcol[d][0] + (row0 + 16 * s) * D;
           const u16* hi = keys.kcol[d][1] + (row0 + 16 * s + 8) * D;
-          acc[d] = T::mfma(read_cols<T>(lo, hi), ds, acc[d]);
+          const typename T::x8 kf = read_cols<T>(lo, hi);
+          acc[d] = T::mfma(kf, ds, acc[d]);
+          if (EXACT) pk[EXACT ? d : 0] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wp[s]), pk[EXACT ? d : 0]);
         }
       }
     });
     // What cross_dkv_kernel takes as delta is free of the output's rounding: the
     // weights add up to 1, so the sum of P dP is delta and the sum of dS.
-    const float exact = delta + both_halves_sum(more);
+    more = both_halves_sum(more);
+    const float exact = delta + more;
+    if (EXACT) {
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] = fmaf(-more, pk[EXACT ? d : 0][e], acc[d][e]);
+    }
     if (r < n_rows && hw == 0) p.row_ld[row] = make_float2(nlse2 / p.sl2, -exact);
     const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, fresh(lane));
     store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, two.a), two.a_ok, at(p.dq, p.sdq, two.b), two.b_ok, lane);
@@ -452,16 +532,15 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
     wait_vmem();
     __syncthreads();
 
-    // dq of rows rw .. rw + 31.
+    // dq of rows rw .. rw + 31, in two walks over the keys: the first adds up
+    // delta as the sum of P dP, free of the output's rounding.
     {
       const int i = rw + c32;
       const int64_t row = ((int64_t)b * p.H + h) * p.Lq + i;
       const RowOf lower = {b, h, rw + (lane & 15)}, upper = {b, h, rw + (lane & 15) + 16};
       const bool a_ok = lower.i < p.Lq, b_ok = upper.i < p.Lq;
       const int ra = fresh(ra0);
-      typename T::x8 qf[D / 16], gf[D / 16], of[D / 16];
-      const u16* out = p.out;
-      load_tile<T, D>(at(out, p.so, lower), a_ok, at(out, p.so, upper), b_ok, lane, of);
+      typename T::x8 qf[D / 16], gf[D / 16];
       const float z = i < p.Lq ? p.lse[row] : -INFINITY;
       const float nlse2 = z == -INFINITY ? -INFINITY : -z * kLog2e;
 #pragma unroll
@@ -469,62 +548,65 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
         qf[ks] = read_row<T>(sQ + (ra ^ (8 * row_chunk(ks))) + rw * D);
         gf[ks] = read_row<T>(sG + (ra ^ (8 * row_chunk(ks))) + rw * D);
       }
-      float delta = 0.f, more = 0.f;
+      int last = rw < p.Lq ? nkb : 0;                     // blocks of keys that some row sees
+      if (BIAS && p.rb.causal && rw + 31 + off < 32 * last) last = rw + 31 + off < 0 ? 0 : (rw + 31 + off) / 32 + 1;
+      // P and dP - delta of block j.
+      auto block = [&](int j, float delta, f32x16& x, f32x16& y) {
+        const int ra = fresh(ra0);
+        const u16* tK = sK + 32 * j * D;
+        const u16* tV = sV + 32 * j * D;
+        x = f32x16{};
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
+        for (int e = 0; e < 16; ++e) y[e] = -delta;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
+        for (int ks = 0; ks < D / 16; ++ks) {
+          x = T::mfma(read_row<T>(tK + (ra ^ (8 * row_chunk(ks)))), qf[ks], x);
+          y = T::mfma(read_row<T>(tV + (ra ^ (8 * row_chunk(ks)))), gf[ks], y);
+        }
+        const int lo = 32 * j - (rw + 31 + off);          // the block's smallest key minus query position
+        const float* at = bt + bias_from(lo, far) + far + kPad + 31 + 4 * hw - c32;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, BIAS ? at[8 * (e >> 2) + (e & 3)] + nlse2 : nlse2);
+        if (!((whole >> j) & 1)) {
+          const float* hide = mask + 32 * j + 4 * hw;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] += hide[8 * (e >> 2) + (e & 3)];
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
+      };
+      float delta = 0.f;
+      for (int j = 0; j < last; ++j) {
+        f32x16 x, y;
+        block(j, 0.f, x, y);
+        float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          s0 = fmaf(x[e], y[e], s0);
+          s1 = fmaf(x[e + 1], y[e + 1], s1);
+        }
+        delta += s0 + s1;
+      }
       delta = both_halves_sum(delta);
       f32x16 acc[D / 32];
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
-      if (rw < p.Lq) {
-        for (int j = 0; j < nkb; ++j) {
-          const int ra = fresh(ra0), ca = fresh(ca0);
-          const u16* tK = sK + 32 * j * D;
-          const u16* tV = sV + 32 * j * D;
-          const int lo = 32 * j - (rw + 31 + off);        // the block's smallest key minus query position
-          if (BIAS && p.rb.causal && lo > 0) break;
-          f32x16 x = f32x16{}, y;
+      for (int j = 0; j < last; ++j) {
+        f32x16 x, y;
+        block(j, delta, x, y);
+        const int ca = fresh(ca0);
+        u32x4 w[2];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) y[e] = -delta;
+        for (int e = 0; e < 16; e += 2) w[e >> 3][(e & 7) >> 1] = T::pack(x[e] * y[e], x[e + 1] * y[e + 1]);
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            x = T::mfma(read_row<T>(tK + (ra ^ (8 * row_chunk(ks)))), qf[ks], x);
-            y = T::mfma(read_row<T>(tV + (ra ^ (8 * row_chunk(ks)))), gf[ks], y);
-          }
-          const float* at = bt + bias_from(lo, far) + far + kPad + 31 + 4 * hw - c32;
-          u32x4 w[2];
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, BIAS ? at[8 * (e >> 2) + (e & 3)] + nlse2 : nlse2);
-          if (!((whole >> j) & 1)) {
-            const float* hide = mask + 32 * j + 4 * hw;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] += hide[8 * (e >> 2) + (e & 3)];
-          }
-          float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            y[e] *= fast_exp2(x[e]);
-            y[e + 1] *= fast_exp2(x[e + 1]);
-            s0 += y[e];
-            s1 += y[e + 1];
-          }
-          more += s0 + s1;
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d)
-              acc[d] = T::mfma(read_col<T, D>(tK, ca, d, 16 * s), __builtin_bit_cast(typename T::x8, w[s]), acc[d]);
-        }
+          for (int d = 0; d < D / 32; ++d)
+            acc[d] = T::mfma(read_col<T, D>(sK + 32 * j * D, ca, d, 16 * s), __builtin_bit_cast(typename T::x8, w[s]), acc[d]);
       }
-      // The statistics that dk and dv take: delta free of the output's rounding.
-      more = both_halves_sum(more);
       if (hw == 0) {
         st[0][i] = nlse2 / p.sl2;                         // past the last row -inf: weight 0
-        st[1][i] = -(delta + more);
+        st[1][i] = -delta;
       }
       store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, lower), a_ok, at(p.dq, p.sdq, upper), b_ok, lane);
     }
