@@ -45,6 +45,7 @@ struct CrossParams {
   int splits;                          // ranges that an axis is divided into
   float* part_o;                       // forward: [splits, B*H*Lq, D]; backward dq: the same
   float* part_ml;                      // forward: [splits, B*H*Lq, 2] reference and sum
+  float* part_d;                       // backward: [splits, B*H*Lq] shares of delta
   float2* row_ld;                      // backward: [B*H*Lq] -LSE / scale (-inf for an empty row) and -delta
   float* part_kv;                      // backward: [splits, 2, B*Hk*Lk, D]
   int kv_splits;
@@ -59,7 +60,7 @@ struct CrossPlan {
   bool resident;                       // the keys of a head stay in LDS, splits workgroups share its rows
   bool small;                          // backward: queries and keys of a head fit in LDS, one kernel does all
   int splits, kv_splits;
-  int64_t part_o, part_ml, row_ld, part_kv, part_t;   // byte offsets into the workspace
+  int64_t part_o, part_ml, part_d, row_ld, part_kv, part_t;   // byte offsets into the workspace
   int64_t bytes;
 };
 

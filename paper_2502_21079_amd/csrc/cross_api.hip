@@ -185,6 +185,7 @@ adaspa_status backward(const adaspa_cross_problem* prob, const adaspa_rel_bias* 
   char* ws = (char*)workspace;
   c.row_ld = (float2*)(ws + plan.row_ld);
   c.part_o = (float*)(ws + plan.part_o);
+  c.part_d = (float*)(ws + plan.part_d);
   c.part_kv = (float*)(ws + plan.part_kv);
   c.part_t = (float*)(ws + plan.part_t);
   return launch_cross_bwd(c, prob->head_dim, prob->dtype == ADASPA_FP16, with_bias, plan, (hipStream_t)stream) ==

@@ -25,12 +25,19 @@ constexpr int kDkvWaves = 4;           // waves of 32 keys of a workgroup of cro
 // is dS, rounded for the product).
 template <int D>
 constexpr bool kExactDq = D == 64;
+
+// What a launch of cross_dq_kernel does.  Where few rows share many keys the
+// keys are split, and delta, which needs them all, comes first: DELTA leaves each
+// range's sum of P dP, DQ adds these up and forms its range's dq.  (With delta
+// from the rounded output there, 25 queries over 18,266 keys had dq off by 5.4e-3
+// of its size where rounding dS and dq alone gives 2.4e-3.)
+enum { WHOLE = 0, DELTA = 1, DQ = 2 };
 }  // namespace
 
-template <class T, int D, bool BIAS>
+template <class T, int D, bool BIAS, int PASS>
 __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
-  constexpr bool EXACT = kExactDq<D>;
+  constexpr bool EXACT = PASS == WHOLE && kExactDq<D>;
   __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];
   __shared__ uint16_t start[BIAS ? kMaxBucketSide : 1];
   extern __shared__ __attribute__((aligned(16))) float bt[];
@@ -74,7 +81,8 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   load_tile<T, D>(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane, qf);
   load_tile<T, D>(at(p.dout, p.sdo, two.a), two.a_ok, at(p.dout, p.sdo, two.b), two.b_ok, lane, gf);
   float nlse2 = -INFINITY, delta = 0.f;                    // -log2-LSE; a row without a key: every weight 0
-  {
+  const int64_t all_rows = (int64_t)p.B * p.H * p.Lq;
+  if (PASS == WHOLE) {
     typename T::x8 of[D / 16];
     load_tile<T, D>(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane, of);
 #pragma unroll
@@ -82,11 +90,17 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
     delta = both_halves_sum(delta);
+  }
+  if (PASS == DQ && row_ok) {
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) delta += p.part_d[s * all_rows + row];
+  }
+  {
     const float z = row_ok ? p.lse[row] : -INFINITY;
     if (z != -INFINITY) nlse2 = -z * kLog2e;
   }
   if (BIAS) fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
-  float more = 0.f;                                        // sum of dS: what delta lacks
+  float more = 0.f;                                        // sum of dS: what delta lacks (DELTA: of P dP)
 
   f32x16 acc[D / 32], pk[EXACT ? D / 32 : 1];
 #pragma unroll
@@ -155,7 +169,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
     };
-    if (!EXACT && nt == 1) {                               // all keys are here: delta exactly, before dS
+    if (PASS == WHOLE && !EXACT && nt == 1) {              // all keys are here: delta exactly, before dS
       float s = 0.f;
       delta = 0.f;
 #pragma unroll
@@ -172,10 +186,19 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
       const int row0 = u * 128 + 32 * g;
       f32x16 x, y;
       block(g, x, y);
+      float s0 = 0.f, s1 = 0.f;
+      if (PASS == DELTA) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          s0 = fmaf(x[e], y[e], s0);
+          s1 = fmaf(x[e + 1], y[e + 1], s1);
+        }
+        more += s0 + s1;
+        continue;
+      }
       u32x4 w[2], wp[2];
 #pragma unroll
       for (int e = 0; e < 16; ++e) y[e] *= x[e];
-      float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         s0 += y[e];
@@ -201,23 +224,22 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     if (t + 1 < t1) tile(integral_constant<int, 1>{}, t + 1);
   }
 
-  more = p.splits > 1 ? 0.f : both_halves_sum(more);
+  more = both_halves_sum(more);
+  if (PASS == DELTA) {
+    if (row_ok && hw == 0) p.part_d[split * all_rows + row] = more;
+    return;
+  }
   if (EXACT) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[d][e] = fmaf(-more, pk[EXACT ? d : 0][e], acc[d][e]);
   }
-  if (p.splits > 1) {
-    const int64_t at = (int64_t)split * p.B * p.H * p.Lq + row;
-    store_tile_f32<D>(acc, p.part_o + at * D, row_ok, hw);
-  } else {
-    store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, two.a), two.a_ok, at(p.dq, p.sdq, two.b), two.b_ok, lane);
-  }
+  if (PASS == DQ) store_tile_f32<D>(acc, p.part_o + (split * all_rows + row) * D, row_ok, hw);
+  else store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, two.a), two.a_ok, at(p.dq, p.sdq, two.b), two.b_ok, lane);
   // What cross_dkv_kernel takes as delta is free of the output's rounding: the
-  // weights add up to 1, so the sum of P dP is delta and the sum of dS.  Where
-  // the keys are split, it is the one from the rounded output.
-  const float exact = delta + more;
+  // weights add up to 1, so the sum of P dP is delta and the sum of dS.
+  const float exact = PASS == DQ ? delta : delta + more;
   if (row_ok && hw == 0 && split == 0) p.row_ld[row] = make_float2(nlse2 / p.sl2, -exact);
 }
 
@@ -1028,24 +1050,26 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(SumOf first, SumOf secon
   *reinterpret_cast<uint2*>(at(s.out, s.so, r) + c) = w;
 }
 
-// dtable[u, h]: the shares of head h over samples and workgroups, eight runs of
-// them at a time, each in order.
+// dtable[u, h]: the shares of head h over samples and workgroups, 64 runs of them
+// for four buckets at a time, each in order, then the runs' sums in order.
 template <class T>
 __global__ __launch_bounds__(256) void cross_dtable_kernel(const CrossParams p, int per) {
-  __shared__ float sum[8][32];
+  __shared__ float sum[64][4];
   const int h = blockIdx.x, buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
-  const int t = threadIdx.x & 31, u = blockIdx.y * 32 + t, part = threadIdx.x >> 5;
+  const int t = threadIdx.x & 3, u = blockIdx.y * 4 + t, part = threadIdx.x >> 2;
   float s = 0.f;
   if (u < buckets) {
     const int64_t n = (int64_t)p.B * per;
-#pragma unroll 8
-    for (int64_t a = n * part / 8; a < n * (part + 1) / 8; ++a)
+#pragma unroll 4
+    for (int64_t a = n * part / 64; a < n * (part + 1) / 64; ++a)
       s += p.part_t[((a / per * p.H + h) * per + a % per) * buckets + u];
   }
   sum[part][t] = s;
   __syncthreads();
   if (part != 0 || u >= buckets) return;
-  s = ((sum[0][t] + sum[1][t]) + (sum[2][t] + sum[3][t])) + ((sum[4][t] + sum[5][t]) + (sum[6][t] + sum[7][t]));
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 64; ++i) s += sum[i][t];
   const int64_t at = (int64_t)u * p.H + h;
   if (p.rb.table_f32) ((float*)p.rb.dtable)[at] = s;
   else T::store(p.rb.dtable, at, s);
@@ -1073,7 +1097,11 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
     c.bytes = bias ? up256((int64_t)p.B * p.H * (p.rb.both ? 2 : 1) * p.rb.side * 4) : 0;
     return c;
   }
-  c.splits = tiles > 0 && tiles < 256 ? clamp_splits(512 / tiles, nt / 4) : 1;
+  // Split keys cost a pass for delta and a sum, so only for few rows: whole calls
+  // whole against split, us: 200 tiles of d 64 x 49 key tiles 233 and 254 (in two),
+  // 192 of d 128 x 15 116 and 141, 64 of d 64 x 63 163 and 126, 16 x 286 567 and
+  // 128, 24 of d 128 x 24 83 and 69, 24 of d 64 x 11 75 and 83.
+  c.splits = tiles > 0 && tiles <= 96 && nt > 12 ? clamp_splits(512 / tiles, nt / 4) : 1;
   c.resident = keep_keys(p, D, bias, 1);
   if (c.resident) c.splits = keep_chunks(p, 1);
   const int64_t ktiles = (int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves));
@@ -1099,12 +1127,20 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   int64_t off = up256(rows * 8);                     // row_ld at 0
   c.part_o = off;
   if (c.splits > 1 && !c.resident) off += up256(c.splits * rows * D * 4);
+  c.part_d = off;
+  if (c.splits > 1 && !c.resident) off += up256(c.splits * rows * 4);
   c.part_kv = off;
   if (c.kv_splits > 1) off += up256((int64_t)c.kv_splits * 2 * p.B * p.Hk * p.Lk * D * 4);
   c.part_t = off;
   if (bias) off += up256(ktiles * p.G * c.kv_splits * (p.rb.both ? 2 : 1) * p.rb.side * 4);
   c.bytes = off;
   return c;
+}
+
+template <class T, int D, int PASS>
+static void launch_dq(const CrossParams& p, bool bias, uint32_t lds, hipStream_t st) {
+  if (bias) hipLaunchKernelGGL((cross_dq_kernel<T, D, true, PASS>), dim3(p.n_wg), dim3(256), lds, st, p);
+  else hipLaunchKernelGGL((cross_dq_kernel<T, D, false, PASS>), dim3(p.n_wg), dim3(256), 0, st, p);
 }
 
 template <class T, int D>
@@ -1115,7 +1151,7 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   const int64_t rows = (int64_t)p.B * p.H * p.Lq, keys = (int64_t)p.B * p.Hk * p.Lk;
   const uint32_t lds = bias ? bias_entries(p.rb.far) * 4 : 0, per = 256 / (D / 4);
   const int buckets = p.rb.both ? 2 * p.rb.side : p.rb.side;
-  const dim3 table(p.H, (buckets + 31) / 32);
+  const dim3 table(p.H, (buckets + 3) / 4);
   if (c.small) {
     p.n_wg = p.B * p.Hk;
     constexpr int NW = kSmallWaves<D>;
@@ -1131,12 +1167,15 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   if (c.resident) {
     hipLaunchKernelGGL((cross_keep_dq_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves), keep_lds_bytes(p.Lk), st, p);
   } else if (p.n_wg > 0) {
-    if (bias) hipLaunchKernelGGL((cross_dq_kernel<T, D, true>), dim3(p.n_wg), dim3(256), lds, st, p);
-    else hipLaunchKernelGGL((cross_dq_kernel<T, D, false>), dim3(p.n_wg), dim3(256), 0, st, p);
-    const SumOf dq = {p.part_o, p.dq, p.sdq, p.scale};
-    if (p.splits > 1)
+    if (p.splits > 1) {
+      launch_dq<T, D, DELTA>(p, bias, lds, st);
+      launch_dq<T, D, DQ>(p, bias, lds, st);
+      const SumOf dq = {p.part_o, p.dq, p.sdq, p.scale};
       hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, st, dq, dq,
                          rows * D, p.splits, rows, p.H, p.Lq);
+    } else {
+      launch_dq<T, D, WHOLE>(p, bias, lds, st);
+    }
   }
   p.n_wg = (int)((int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves)) * p.kv_splits);
   if (p.n_wg > 0) {

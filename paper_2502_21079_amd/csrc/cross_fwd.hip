@@ -314,16 +314,19 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_ke
 }
 
 // Joins the ranges of a split call: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
-// A workgroup per row: groups of D / 4 threads take every NG-th range each,
-// then join their sums, all in a fixed order.
-template <class T, int D>
+// NG groups of D / 4 threads share a row, take every NG-th range each and join
+// their sums, all in a fixed order.  Many ranges come with few rows and want a
+// workgroup per row (NG = 256 / (D / 4)); few ranges come with many rows, and one
+// group per row then leaves no thread without a range (24,776 rows of d 64 in two
+// ranges: 36 us with a workgroup per row, 5.7 so).
+template <class T, int D, int NG>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossParams p) {
-  constexpr int TPR = D / 4, NG = 256 / TPR;
-  __shared__ f32x4 so[NG][TPR];
-  __shared__ float sm[NG], sl[NG];
-  const int64_t rows = (int64_t)p.B * p.H * p.Lq, row = blockIdx.x;
-  const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+  constexpr int TPR = D / 4;
+  const int64_t rows = (int64_t)p.B * p.H * p.Lq, row = (int64_t)blockIdx.x * (256 / (TPR * NG)) + threadIdx.x / (TPR * NG);
+  if (row >= rows) return;                                 // (with groups to join, never)
+  const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR % NG;
   float m = -INFINITY, l = 0.f;
+#pragma unroll 4
   for (int s = grp; s < p.splits; s += NG) m = vmax(m, p.part_ml[2 * (s * rows + row)]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -335,22 +338,26 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossParams p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] += w * v[j];
   }
-  so[grp][t] = o;
-  if (t == 0) {
-    sm[grp] = m;
-    sl[grp] = l;
-  }
-  __syncthreads();
-  if (grp != 0) return;
-  for (int g = 1; g < NG; ++g) m = vmax(m, sm[g]);
-  l = 0.f;
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int g = 0; g < NG; ++g) {
-    const float w = sm[g] == -INFINITY ? 0.f : fast_exp2(sm[g] - m);
-    const f32x4 v = so[g][t];
-    l += w * sl[g];
+  if constexpr (NG > 1) {
+    __shared__ f32x4 so[NG][TPR];
+    __shared__ float sm[NG], sl[NG];
+    so[grp][t] = o;
+    if (t == 0) {
+      sm[grp] = m;
+      sl[grp] = l;
+    }
+    __syncthreads();
+    if (grp != 0) return;
+    for (int g = 1; g < NG; ++g) m = vmax(m, sm[g]);
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < NG; ++g) {
+      const float w = sm[g] == -INFINITY ? 0.f : fast_exp2(sm[g] - m);
+      const f32x4 v = so[g][t];
+      l += w * sl[g];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] += w * v[j];
+      for (int j = 0; j < 4; ++j) o[j] += w * v[j];
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int i = (int)(row % p.Lq), h = (int)(row / p.Lq % p.H), b = (int)(row / p.Lq / p.H);
@@ -375,10 +382,18 @@ CrossPlan plan_fwd(const CrossParams& p, int D, bool bias) {
     return c;
   }
   // Keys are split where the row tiles alone leave CUs without work, into
-  // ranges of no less than four tiles; up to 1,024 keys the join's launch and
-  // scratch cost more than the shorter walk gains (one query over 512 keys, 32
-  // heads, d 128: 17.5 us a call, 9 without).
-  int64_t s = tiles > 0 && tiles < 256 && nt > 16 ? 512 / tiles : 1;
+  // ranges of no less than four tiles; below 1,024 keys the join's launch and
+  // scratch cost more than the shorter walk gains (us a call, whole and split: one
+  // query over 512 keys, 32 heads, d 128 9 and 17.5, over 1,000 keys, 48 units,
+  // d 64 17.6 and 15.4).  And where all row tiles run at once but end apart, under
+  // an order mask or at d 64 with one workgroup on some CUs and two on others
+  // (causal 12 x 4,095 of d 128 113 and 101, 6 x 6,199 of d 64 118 and 73,
+  // 12 x 8,191 194 and 175, but 32 x 4,096, 1,024 tiles, 126 and 138, and
+  // 24 x 2,048 46 and 48; without order 6 x 6,199 of d 64 131 and 96, but
+  // 12 x 4,095 of d 128 125 and 134).
+  int64_t s = 1;
+  if (tiles > 0 && tiles < 256 && nt >= 16) s = 512 / tiles;
+  else if (nt >= 48 && (bias && p.rb.causal ? tiles < 1024 : D == 64 && tiles < 384)) s = D == 64 ? 4 : 2;
   s = s < nt / 4 ? s : nt / 4;
   c.splits = s < 1 ? 1 : (s > 128 ? 128 : (int)s);
   if (c.splits > 1) {
@@ -413,7 +428,9 @@ static hipError_t run_fwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   }
   if (p.splits > 1) {
     const int64_t all = (int64_t)p.B * p.H * p.Lq;
-    hipLaunchKernelGGL((cross_join_kernel<T, D>), dim3((uint32_t)all), dim3(256), 0, st, p);
+    constexpr int NG = 1024 / D;                           // a workgroup's groups
+    if (p.splits > 8) hipLaunchKernelGGL((cross_join_kernel<T, D, NG>), dim3((uint32_t)all), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((cross_join_kernel<T, D, 1>), dim3((uint32_t)((all + NG - 1) / NG)), dim3(256), 0, st, p);
   }
   return hipGetLastError();
 }
