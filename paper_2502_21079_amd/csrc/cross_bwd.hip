@@ -244,11 +244,15 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 }
 
 // dq with few keys: they stay in LDS, as in the forward pass, and each wave
-// walks row tiles of 32 on its own, without barriers.
-template <class T, int D>
+// walks row tiles of 32 on its own, without barriers.  ONE is for one tile of
+// keys: S and dP are formed twice, delta exactly from the first time, and the
+// output is not read, since there the rows' way through memory takes longer than
+// the products (24 x 110,080 rows over 64 keys, one walk and the output against
+// two walks: d 64 311 and 259 us, d 128 593 and 452).
+template <class T, int D, bool ONE>
 __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq_kernel(const CrossParams p) {
   constexpr int NW = kKeepWaves;
-  constexpr bool EXACT = kExactDq<D>;
+  constexpr bool EXACT = !ONE && kExactDq<D>;
   extern __shared__ __attribute__((aligned(1024))) u16 keep_lds[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
@@ -260,10 +264,6 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
   int rt = (int)((int64_t)n_rt * chunk / p.splits) + wave;
 
   const KeptKeys<T, D> keys(p, b, hk, n, keep_lds, wave, lane, tid, []() {});
-  // With one tile of keys S and dP are formed twice, delta exactly from the
-  // first time, and the output is not read at all: that long the rows' way
-  // through memory takes longer than the products.
-  const bool one_tile = keys.nt <= 1;
   for (; rt < rt1; rt += NW) {
     const int r = rt * 32 + c32;
     const int64_t row = (int64_t)unit * n_rows + r;        // a unit's rows are consecutive
@@ -273,12 +273,12 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
       const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, fresh(lane));
       TileRegs<T, D> q, g, o;
       g.load(at(p.dout, p.sdo, two.a), two.a_ok, at(p.dout, p.sdo, two.b), two.b_ok, lane);
-      if (!one_tile) o.load(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane);
+      if (!ONE) o.load(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane);
       q.load(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane);
       const float z = r < n_rows ? p.lse[row] : -INFINITY;
       if (z != -INFINITY) nlse2 = -z * kLog2e;
       g.operands(gf);
-      if (!one_tile) {
+      if (!ONE) {
         typename T::x8 of[D / 16];
         o.operands(of);
 #pragma unroll
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
     };
-    if (one_tile) {
+    if (ONE) {
       from = f32x16{};
       static_for<2>([&](auto j) {
         if (keys.nt == 0) return;
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
 #pragma unroll
     for (int e = 0; e < 16; ++e) from[e] = -delta;
     float more = 0.f;                                      // sum of dS: what delta lacks
-    static_for<2 * KeptKeys<T, D>::TILES>([&](auto j) {
+    static_for<ONE ? 2 : 2 * KeptKeys<T, D>::TILES>([&](auto j) {
       constexpr int row0 = 32 * j;
       if (j / 2 >= keys.nt) return;
       f32x16 x, y;
@@ -1165,7 +1165,9 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   }
   p.n_wg = (int)(units * (c.resident ? 1 : rt) * p.splits);
   if (c.resident) {
-    hipLaunchKernelGGL((cross_keep_dq_kernel<T, D>), dim3(p.n_wg), dim3(64 * kKeepWaves), keep_lds_bytes(p.Lk), st, p);
+    const dim3 grid(p.n_wg), block(64 * kKeepWaves);
+    if (p.Lk <= 64) hipLaunchKernelGGL((cross_keep_dq_kernel<T, D, true>), grid, block, keep_lds_bytes(p.Lk), st, p);
+    else hipLaunchKernelGGL((cross_keep_dq_kernel<T, D, false>), grid, block, keep_lds_bytes(p.Lk), st, p);
   } else if (p.n_wg > 0) {
     if (p.splits > 1) {
       launch_dq<T, D, DELTA>(p, bias, lds, st);
