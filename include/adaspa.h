@@ -21,6 +21,13 @@
  * and adaspa_single_pass_online_search, the same results with one pass over
  * Q K^T instead of two.
  *
+ * Beside it stand the attentions of the prompt side, with their gradients:
+ * adaspa_cross_attn (video tokens over a text encoder's states) and
+ * adaspa_rel_bias_attn (the encoder's own, with a learned relative position
+ * bias).  Their tensors, strides and masks are described at their declarations;
+ * what is said below of ownership, streams, errors and determinism holds for
+ * them too.
+ *
  * Conventions shared by every call
  * --------------------------------
  *  - Tensors are DEVICE pointers, contiguous, 16-byte aligned.
@@ -340,8 +347,9 @@ adaspa_status adaspa_block_sparse_attn_noalloc(const adaspa_problem* prob, const
  *
  * over the visible keys: j < key_lens[b], key_mask[b, j] != 0 and, with
  * `causal`, j <= i + offset.  A row that sees no key (a dropped prompt) gives
- * out = 0, lse = -inf and no gradient.  Whatever masked keys hold, infinities
- * and NaN too, takes no part.
+ * out = 0, lse = -inf and no gradient.  Whatever keys past key_lens or with a
+ * 0 in key_mask hold, infinities and NaN too, takes no part; keys that only
+ * the order hides from a row must be finite, as those that it sees.
  *
  * Tensors are bf16 or fp16 views [B, heads, tokens, D], D contiguous, with
  * strides of their own (elements; multiples of 8, the token stride below 2^23;
@@ -353,8 +361,9 @@ adaspa_status adaspa_block_sparse_attn_noalloc(const adaspa_problem* prob, const
  * dS are rounded to the inputs' type for the second products, results once.
  * The workspace is scratch, 256-byte aligned, of the size that the matching
  * _workspace call names (0: invalid arguments; 16: the call takes none, NULL
- * will do), not shared by calls that may overlap.  Ownership, streams, errors and determinism are those above: every
- * sum over more than one workgroup is taken in a fixed order. */
+ * will do), not shared by calls that may overlap.  Ownership, streams, errors and
+ * determinism are those above: every sum over more than one workgroup is taken
+ * in a fixed order. */
 enum { ADASPA_BF16 = 0, ADASPA_FP16 = 1 };
 
 typedef struct {

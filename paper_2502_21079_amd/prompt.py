@@ -346,17 +346,17 @@ def cross_attn_bwd_workspace(q_shape, k_shape) -> int:
 
 
 def rel_bias_attn_workspace(q_shape, k_shape, num_buckets: int, *, max_distance: int = 128,
-                            bidirectional: bool = True) -> int:
+                            bidirectional: bool = True, causal: bool = False) -> int:
     """Bytes of the workspace of :func:`rel_bias_attn`."""
-    return _workspace(False, q_shape, k_shape, (index(num_buckets), index(max_distance), bool(bidirectional), False, 0,
-                                                False))
+    return _workspace(False, q_shape, k_shape, (index(num_buckets), index(max_distance), bool(bidirectional), bool(causal),
+                                                0, False))
 
 
 def rel_bias_attn_bwd_workspace(q_shape, k_shape, num_buckets: int, *, max_distance: int = 128,
-                                bidirectional: bool = True) -> int:
+                                bidirectional: bool = True, causal: bool = False) -> int:
     """Bytes of the workspace of :func:`rel_bias_attn_bwd`."""
-    return _workspace(True, q_shape, k_shape, (index(num_buckets), index(max_distance), bool(bidirectional), False, 0,
-                                               False))
+    return _workspace(True, q_shape, k_shape, (index(num_buckets), index(max_distance), bool(bidirectional), bool(causal),
+                                                0, False))
 
 
 # --- autograd ------------------------------------------------------------------

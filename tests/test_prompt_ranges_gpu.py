@@ -132,3 +132,26 @@ def test_gradients_do_not_carry_the_outputs_rounding(D, Lq, Lk):
     assert rel(dq, ref["dq"][0]) < 2 * u
     assert rel(dk, ref["dk"][0]) < 2 * u
     assert rel(dt, ref["dtable"][0]) < 2 * u
+
+
+@pytest.mark.parametrize("B,H,Lq,Lk,causal", [(1, 6, 3300, 3300, True), (1, 6, 3300, 3300, False),
+                                              (2, 2, 200, 2000, False), (1, 2, 700, 900, True)])
+def test_workspaces_of_the_named_sizes(B, H, Lq, Lk, causal):
+    """A caller's workspaces, of just the named sizes, give the results of the
+    call's own; one byte less is refused."""
+    q, k, v, g = make(B, H, H, Lq, Lk, 64, BF, seed=3)
+    table = table_of(32, H)
+    kw = dict(bidirectional=not causal, causal=causal)
+    out, lse = ad.rel_bias_attn(q, k, v, table, **kw)
+    grads = ad.rel_bias_attn_bwd(g, q, k, v, table, out, lse, **kw)
+    sizes = [f(q.shape, k.shape, 32, **kw) for f in (ad.rel_bias_attn_workspace, ad.rel_bias_attn_bwd_workspace)]
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+    again = ad.rel_bias_attn(q, k, v, table, workspace=ws[0], **kw)
+    again += ad.rel_bias_attn_bwd(g, q, k, v, table, *again, workspace=ws[1], **kw)
+    for x, y in zip((out, lse) + grads, again):
+        assert torch.equal(x, y)
+    if sizes[0] > 16:
+        with pytest.raises(ad.AdaspaError):
+            ad.rel_bias_attn(q, k, v, table, workspace=ws[0][:-1], **kw)
+    with pytest.raises(ad.AdaspaError):
+        ad.rel_bias_attn_bwd(g, q, k, v, table, out, lse, workspace=ws[1][:-1], **kw)
