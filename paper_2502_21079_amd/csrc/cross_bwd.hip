@@ -25,6 +25,18 @@ constexpr int kDkvWaves = 4;           // waves of 32 keys of a workgroup of cro
 // is dS, rounded for the product).
 template <int D>
 constexpr bool kExactDq = D == 64;
+// At d 128 they do not, and delta's error can be as large as dS's rounding (162
+// rows over 2,245 keys: 1.6 times the final rounding together).  There dS goes
+// into the product as a sum of two values, its upper bits and what they leave, so
+// that delta's error and the final rounding are all that is left.
+template <class T>
+__device__ __forceinline__ uint32_t split_pair(float a, float b, uint32_t& rest) {
+  const uint32_t hi = T::pack(a, b);
+  float c, d;
+  T::unpack(hi, c, d);
+  rest = T::pack(a - c, b - d);
+  return hi;
+}
 
 // What a launch of cross_dq_kernel does.  Where few rows share many keys the
 // keys are split, and delta, which needs them all, comes first: DELTA leaves each
@@ -37,7 +49,7 @@ enum { WHOLE = 0, DELTA = 1, DQ = 2 };
 template <class T, int D, bool BIAS, int PASS>
 __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
-  constexpr bool EXACT = PASS == WHOLE && kExactDq<D>;
+  constexpr bool EXACT = PASS == WHOLE && kExactDq<D>, SPLIT = PASS == WHOLE && !kExactDq<D>;
   __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];
   __shared__ uint16_t start[BIAS ? kMaxBucketSide : 1];
   extern __shared__ __attribute__((aligned(16))) float bt[];
@@ -45,8 +57,8 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   const int hw = lane >> 5, c32 = lane & 31;
 
   const int n_rows = BIAS ? p.Lq : p.G * p.Lq, n_rt = (n_rows + kDqRows - 1) / kDqRows;
-  const int lid = xcd_remap(blockIdx.x, p.n_wg);
-  const int unit = unit_at(p, lid / (n_rt * p.splits), BIAS ? p.H : p.Hk), split = lid / n_rt % p.splits, r0 = lid % n_rt * kDqRows;
+  const Place place = place_of<BIAS>(p, BIAS ? p.H : p.Hk, n_rt, p.splits, true);
+  const int unit = place.unit, split = place.split, r0 = place.tile * kDqRows;
   const int rw = r0 + wave * 32, r = rw + c32;             // first row of the wave, row of the lane
   const bool row_ok = r < n_rows;
   const RowOf ro = row_of<BIAS>(p, unit, row_ok ? r : 0);
@@ -66,14 +78,19 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   lv.init(wave, lane, p.sv.t);
   const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
   const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
-  int mb = 1;
+  int mb[2] = {1, 1};
   auto issue = [&](auto slot, int t) {
     const uint32_t dst = lds_addr(ring[0]) + slot * 4 * KE;
     lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
     lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
-    if (p.key_mask) mb = mask_byte(p, b, t * 64, n, fresh(lane));
+    if (p.key_mask) mb[slot] = mask_byte(p, b, t * 64, n, fresh(lane));
   };
+  // Both tiles of a short walk fit in the ring: there delta comes exactly from a walk
+  // of its own.  Rows with few keys have the largest outputs, whose rounding would
+  // be more than dS's (36 causal rows: dq 1.5 times the final rounding without).
+  const bool few = SPLIT && nt <= 2;
   if (t0 < t1) issue(integral_constant<int, 0>{}, t0);
+  if (few && nt == 2) issue(integral_constant<int, 1>{}, 1);
 
   const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
   const TwoRows two = two_rows<BIAS>(p, unit, rw, n_rows, lane);
@@ -120,72 +137,85 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     for (int h = 0; h < 2; ++h) kcol[d][h] = ring[0] + (col_lane<D>(lane) ^ (16 * h) ^ (32 * d));
   const int rel0 = 4 * hw - (ro.i + off);
 
-  auto tile = [&](auto u, int t) {
+  const int far = BIAS ? p.rb.far : 0;
+  // Waits for tile t and has the next one loaded; its visible keys, the others
+  // cleared (none: left as it is).
+  auto enter = [&](auto u, int t) {
     wait_vmem();
-    const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb != 0) : ~0ull);
+    const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb[u] != 0) : ~0ull);
     __syncthreads();
-    if (t + 1 < t1) issue(integral_constant<int, 1 - u>{}, t + 1);
-    if (keep != ~0ull) {
-      if (keep == 0) return;
+    if (!few && t + 1 < t1) issue(integral_constant<int, 1 - u>{}, t + 1);
+    if (keep != ~0ull && keep != 0) {
       clear_rows<D, 256>(ring[u], keep, fresh(tid));
       clear_rows<D, 256>(ring[u] + KE, keep, fresh(tid));
       __syncthreads();
     }
-    // A wave without rows, or whose rows come before all of these keys.
-    if (rw >= n_rows || (BIAS && p.rb.causal && t * 64 > rw + 31 + off)) return;
-    const int far = BIAS ? p.rb.far : 0;
-    // P and dP - delta of the tile's keys 32 g and on.
-    auto block = [&](int g, f32x16& x, f32x16& y) {
-      const int row0 = u * 128 + 32 * g;                   // a slot is two tiles of 64 rows
-      x = f32x16{};
+    return keep;
+  };
+  // Not for a wave without rows, or whose rows come before all of these keys.
+  auto idle = [&](int t) { return rw >= n_rows || (BIAS && p.rb.causal && t * 64 > rw + 31 + off); };
+  // P and dP - delta of tile t's keys 32 g and on.
+  auto block = [&](auto u, int t, int g, uint64_t keep, f32x16& x, f32x16& y) {
+    const int row0 = u * 128 + 32 * g;                     // a slot is two tiles of 64 rows
+    x = f32x16{};
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = -delta;          // dP's sums begin at -delta
+    for (int e = 0; e < 16; ++e) y[e] = -delta;            // dP's sums begin at -delta
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        x = T::mfma(read_row<T>(kp[ks] + row0 * D), qf[ks], x);
-        y = T::mfma(read_row<T>(kp[ks] + KE + row0 * D), gf[ks], y);
-      }
-      if (BIAS) {
-        const int lo = t * 64 + 32 * g - (rw + 31 + off);  // the block's smallest key minus query position
-        if (lo >= far || lo <= -far - 62) {
-          const float c = bt[lo >= far ? 2 * (far + kPad) : 0] + nlse2;
+    for (int ks = 0; ks < D / 16; ++ks) {
+      x = T::mfma(read_row<T>(kp[ks] + row0 * D), qf[ks], x);
+      y = T::mfma(read_row<T>(kp[ks] + KE + row0 * D), gf[ks], y);
+    }
+    if (BIAS) {
+      const int lo = t * 64 + 32 * g - (rw + 31 + off);    // the block's smallest key minus query position
+      if (lo >= far || lo <= -far - 62) {
+        const float c = bt[lo >= far ? 2 * (far + kPad) : 0] + nlse2;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, c);
-        } else {
-          const float* at = bt + (row_ok ? rel0 + t * 64 + 32 * g : lo) + far + kPad;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[8 * (e >> 2) + (e & 3)] + nlse2);
-        }
+        for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, c);
       } else {
+        const float* at = bt + (row_ok ? rel0 + t * 64 + 32 * g : lo) + far + kPad;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, nlse2);
+        for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, at[8 * (e >> 2) + (e & 3)] + nlse2);
       }
-      if (keep != ~0ull) {
-        const uint32_t mine = (uint32_t)(keep >> (32 * g)) >> (4 * hw);
+    } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!((mine >> (8 * (e >> 2) + (e & 3))) & 1)) x[e] = -INFINITY;
-      }
+      for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], p.sl2, nlse2);
+    }
+    if (keep != ~0ull) {
+      const uint32_t mine = (uint32_t)(keep >> (32 * g)) >> (4 * hw);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
-    };
-    if (PASS == WHOLE && !EXACT && nt == 1) {              // all keys are here: delta exactly, before dS
-      float s = 0.f;
-      delta = 0.f;
+      for (int e = 0; e < 16; ++e)
+        if (!((mine >> (8 * (e >> 2) + (e & 3))) & 1)) x[e] = -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
+  };
+  uint64_t keeps[2] = {0, 0};                              // of a short walk's tiles
+  if (few) {
+    static_for<2>([&](auto u) {
+      if (u < nt) keeps[u] = enter(u, u);
+    });
+    float s = 0.f;
+    delta = 0.f;
+    static_for<2>([&](auto u) {
+      if (keeps[u] == 0 || idle(u)) return;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         f32x16 x, y;
-        block(g, x, y);
+        block(u, u, g, keeps[u], x, y);
 #pragma unroll
         for (int e = 0; e < 16; ++e) s = fmaf(x[e], y[e], s);
       }
-      delta = both_halves_sum(s);
-    }
+    });
+    delta = both_halves_sum(s);
+  }
+  auto tile = [&](auto u, int t) {
+    const uint64_t keep = few ? keeps[u] : enter(u, t);
+    if (keep == 0 || idle(t)) return;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int row0 = u * 128 + 32 * g;
       f32x16 x, y;
-      block(g, x, y);
+      block(u, t, g, keep, x, y);
       float s0 = 0.f, s1 = 0.f;
       if (PASS == DELTA) {
 #pragma unroll
@@ -203,8 +233,14 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
       for (int e = 0; e < 16; e += 2) {
         s0 += y[e];
         s1 += y[e + 1];
-        w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
-        wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
+        if (SPLIT) {
+          uint32_t rest;
+          w[e >> 3][(e & 7) >> 1] = split_pair<T>(y[e], y[e + 1], rest);
+          wp[e >> 3][(e & 7) >> 1] = rest;
+        } else {
+          w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+          wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
+        }
       }
       more += s0 + s1;
 #pragma unroll
@@ -214,6 +250,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
         for (int d = 0; d < D / 32; ++d) {
           const typename T::x8 kf = read_cols<T>(kcol[d][0] + (row0 + 16 * s) * D, kcol[d][1] + (row0 + 16 * s + 8) * D);
           acc[d] = T::mfma(kf, ds, acc[d]);
+          if (SPLIT) acc[d] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wp[s]), acc[d]);
           if (EXACT) pk[EXACT ? d : 0] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wp[s]), pk[EXACT ? d : 0]);
         }
       }
@@ -249,10 +286,12 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 // output is not read, since there the rows' way through memory takes longer than
 // the products (24 x 110,080 rows over 64 keys, one walk and the output against
 // two walks: d 64 311 and 259 us, d 128 593 and 452).
-template <class T, int D, bool ONE>
+template <int D>
+constexpr int kTwiceBlocks = D == 64 ? 2 : 4;              // blocks of 32 keys that are walked twice
+template <class T, int D, bool TWICE>
 __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq_kernel(const CrossParams p) {
   constexpr int NW = kKeepWaves;
-  constexpr bool EXACT = !ONE && kExactDq<D>;
+  constexpr bool EXACT = !TWICE && kExactDq<D>, SPLIT = !TWICE && !kExactDq<D>;
   extern __shared__ __attribute__((aligned(1024))) u16 keep_lds[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
@@ -273,12 +312,12 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
       const TwoRows two = two_rows<false>(p, unit, rt * 32, n_rows, fresh(lane));
       TileRegs<T, D> q, g, o;
       g.load(at(p.dout, p.sdo, two.a), two.a_ok, at(p.dout, p.sdo, two.b), two.b_ok, lane);
-      if (!ONE) o.load(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane);
+      if (!TWICE) o.load(at((const u16*)p.out, p.so, two.a), two.a_ok, at((const u16*)p.out, p.so, two.b), two.b_ok, lane);
       q.load(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane);
       const float z = r < n_rows ? p.lse[row] : -INFINITY;
       if (z != -INFINITY) nlse2 = -z * kLog2e;
       g.operands(gf);
-      if (!ONE) {
+      if (!TWICE) {
         typename T::x8 of[D / 16];
         o.operands(of);
 #pragma unroll
@@ -309,10 +348,10 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
     };
-    if (ONE) {
+    if (TWICE) {
       from = f32x16{};
-      static_for<2>([&](auto j) {
-        if (keys.nt == 0) return;
+      static_for<kTwiceBlocks<D>>([&](auto j) {
+        if (j / 2 >= keys.nt) return;
         f32x16 x, y;
         block(j, x, y);
 #pragma unroll
@@ -326,7 +365,7 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
 #pragma unroll
     for (int e = 0; e < 16; ++e) from[e] = -delta;
     float more = 0.f;                                      // sum of dS: what delta lacks
-    static_for<ONE ? 2 : 2 * KeptKeys<T, D>::TILES>([&](auto j) {
+    static_for<TWICE ? kTwiceBlocks<D> : 2 * KeptKeys<T, D>::TILES>([&](auto j) {
       constexpr int row0 = 32 * j;
       if (j / 2 >= keys.nt) return;
       f32x16 x, y;
@@ -339,8 +378,14 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
       for (int e = 0; e < 16; e += 2) {
         s0 += y[e];
         s1 += y[e + 1];
-        w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
-        wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
+        if (SPLIT) {
+          uint32_t rest;
+          w[e >> 3][(e & 7) >> 1] = split_pair<T>(y[e], y[e + 1], rest);
+          wp[e >> 3][(e & 7) >> 1] = rest;
+        } else {
+          w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+          wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
+        }
       }
       more += s0 + s1;
 #pragma unroll
@@ -352,6 +397,7 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
           const u16* hi = keys.kcol[d][1] + (row0 + 16 * s + 8) * D;
           const typename T::x8 kf = read_cols<T>(lo, hi);
           acc[d] = T::mfma(kf, ds, acc[d]);
+          if (SPLIT) acc[d] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wp[s]), acc[d]);
           if (EXACT) pk[EXACT ? d : 0] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wp[s]), pk[EXACT ? d : 0]);
         }
       }
@@ -550,17 +596,19 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
       load(sQ, p.q + b * p.sq.b + h * p.sq.h, p.sq.t, p.Lq);
       load(sG, p.dout + b * p.sdo.b + h * p.sdo.h, p.sdo.t, p.Lq);
     }
+    const RowOf lower = {b, h, rw + (lane & 15)}, upper = {b, h, rw + (lane & 15) + 16};
+    const bool a_ok = lower.i < p.Lq, b_ok = upper.i < p.Lq;
+    typename T::x8 of[D / 16];
+    load_tile<T, D>(at((const u16*)p.out, p.so, lower), a_ok, at((const u16*)p.out, p.so, upper), b_ok, lane, of);
     if (BIAS) fill_bias<T, NT>(bt, start, p, h, tid);
     wait_vmem();
     __syncthreads();
 
-    // dq of rows rw .. rw + 31, in two walks over the keys: the first adds up
-    // delta as the sum of P dP, free of the output's rounding.
+    // dq of rows rw .. rw + 31, put right by sum_j P_ij k_j once the rows' exact
+    // delta is known, as in cross_dq_kernel.
     {
       const int i = rw + c32;
       const int64_t row = ((int64_t)b * p.H + h) * p.Lq + i;
-      const RowOf lower = {b, h, rw + (lane & 15)}, upper = {b, h, rw + (lane & 15) + 16};
-      const bool a_ok = lower.i < p.Lq, b_ok = upper.i < p.Lq;
       const int ra = fresh(ra0);
       typename T::x8 qf[D / 16], gf[D / 16];
       const float z = i < p.Lq ? p.lse[row] : -INFINITY;
@@ -570,10 +618,16 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
         qf[ks] = read_row<T>(sQ + (ra ^ (8 * row_chunk(ks))) + rw * D);
         gf[ks] = read_row<T>(sG + (ra ^ (8 * row_chunk(ks))) + rw * D);
       }
+      float delta = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[ks][e], (float)of[ks][e], delta);
+      delta = both_halves_sum(delta);
       int last = rw < p.Lq ? nkb : 0;                     // blocks of keys that some row sees
       if (BIAS && p.rb.causal && rw + 31 + off < 32 * last) last = rw + 31 + off < 0 ? 0 : (rw + 31 + off) / 32 + 1;
       // P and dP - delta of block j.
-      auto block = [&](int j, float delta, f32x16& x, f32x16& y) {
+      auto block = [&](int j, f32x16& x, f32x16& y) {
         const int ra = fresh(ra0);
         const u16* tK = sK + 32 * j * D;
         const u16* tV = sV + 32 * j * D;
@@ -597,35 +651,41 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = fast_exp2(x[e]);
       };
-      float delta = 0.f;
+      f32x16 acc[D / 32], pk[D / 32];
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) acc[d] = pk[d] = f32x16{};
+      float more = 0.f;
       for (int j = 0; j < last; ++j) {
         f32x16 x, y;
-        block(j, 0.f, x, y);
+        block(j, x, y);
+        const int ca = fresh(ca0);
         float s0 = 0.f, s1 = 0.f;
+        u32x4 w[2], wp[2];
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          s0 = fmaf(x[e], y[e], s0);
-          s1 = fmaf(x[e + 1], y[e + 1], s1);
+          y[e] *= x[e];
+          y[e + 1] *= x[e + 1];
+          s0 += y[e];
+          s1 += y[e + 1];
+          w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+          wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
         }
-        delta += s0 + s1;
-      }
-      delta = both_halves_sum(delta);
-      f32x16 acc[D / 32];
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) acc[d] = f32x16{};
-      for (int j = 0; j < last; ++j) {
-        f32x16 x, y;
-        block(j, delta, x, y);
-        const int ca = fresh(ca0);
-        u32x4 w[2];
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) w[e >> 3][(e & 7) >> 1] = T::pack(x[e] * y[e], x[e + 1] * y[e + 1]);
+        more += s0 + s1;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int d = 0; d < D / 32; ++d)
-            acc[d] = T::mfma(read_col<T, D>(sK + 32 * j * D, ca, d, 16 * s), __builtin_bit_cast(typename T::x8, w[s]), acc[d]);
+          for (int d = 0; d < D / 32; ++d) {
+            const typename T::x8 kf = read_col<T, D>(sK + 32 * j * D, ca, d, 16 * s);
+            acc[d] = T::mfma(kf, __builtin_bit_cast(typename T::x8, w[s]), acc[d]);
+            pk[d] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wp[s]), pk[d]);
+          }
       }
+      more = both_halves_sum(more);
+      delta += more;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] = fmaf(-more, pk[d][e], acc[d][e]);
       if (hw == 0) {
         st[0][i] = nlse2 / p.sl2;                         // past the last row -inf: weight 0
         st[1][i] = -delta;
@@ -717,8 +777,8 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
   const int hw = lane >> 5, c32 = lane & 31;
 
   const int n_kt = (p.Lk + 32 * NW - 1) / (32 * NW);
-  const int lid = xcd_remap(blockIdx.x, p.n_wg);
-  const int unit = unit_at(p, lid / (n_kt * p.kv_splits), p.Hk), split = lid / n_kt % p.kv_splits, j0 = lid % n_kt * 32 * NW;
+  const Place place = place_of<BIAS>(p, p.Hk, n_kt, p.kv_splits, false);
+  const int unit = place.unit, split = place.split, j0 = place.tile * 32 * NW;
   const int b = unit / p.Hk, hk = unit % p.Hk;
   const int n = key_count(p, b), off = query_offset(p, n);
   const int key = j0 + wave * 32 + c32;
@@ -1166,7 +1226,7 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   p.n_wg = (int)(units * (c.resident ? 1 : rt) * p.splits);
   if (c.resident) {
     const dim3 grid(p.n_wg), block(64 * kKeepWaves);
-    if (p.Lk <= 64) hipLaunchKernelGGL((cross_keep_dq_kernel<T, D, true>), grid, block, keep_lds_bytes(p.Lk), st, p);
+    if (p.Lk <= 32 * kTwiceBlocks<D>) hipLaunchKernelGGL((cross_keep_dq_kernel<T, D, true>), grid, block, keep_lds_bytes(p.Lk), st, p);
     else hipLaunchKernelGGL((cross_keep_dq_kernel<T, D, false>), grid, block, keep_lds_bytes(p.Lk), st, p);
   } else if (p.n_wg > 0) {
     if (p.splits > 1) {

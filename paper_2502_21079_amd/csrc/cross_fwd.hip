@@ -103,8 +103,8 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
   const int hw = lane >> 5, c32 = lane & 31;
 
   const int n_rows = BIAS ? p.Lq : p.G * p.Lq, n_rt = (n_rows + kRows - 1) / kRows;
-  const int lid = xcd_remap(blockIdx.x, p.n_wg);
-  const int unit = unit_at(p, lid / (n_rt * p.splits), BIAS ? p.H : p.Hk), split = lid / n_rt % p.splits, r0 = lid % n_rt * kRows;
+  const Place place = place_of<BIAS>(p, BIAS ? p.H : p.Hk, n_rt, p.splits, true);
+  const int unit = place.unit, split = place.split, r0 = place.tile * kRows;
   const int rw = r0 + wave * 32, r = rw + c32;           // first row of the wave, row of the lane
   const bool row_ok = r < n_rows;
   const RowOf ro = row_of<BIAS>(p, unit, row_ok ? r : 0);

@@ -19,6 +19,10 @@ struct BF16 {
     const bf16x2 r = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, r);
   }
+  __device__ __forceinline__ static void unpack(uint32_t v, float& a, float& b) {
+    a = __uint_as_float(v << 16);
+    b = __uint_as_float(v & 0xFFFF0000u);
+  }
   __device__ __forceinline__ static float load(const void* p, int64_t i) {
     return __uint_as_float((uint32_t)((const u16*)p)[i] << 16);
   }
@@ -36,6 +40,11 @@ struct FP16 {
   __device__ __forceinline__ static uint32_t pack(float a, float b) {
     const x2 r = {(_Float16)a, (_Float16)b};
     return __builtin_bit_cast(uint32_t, r);
+  }
+  __device__ __forceinline__ static void unpack(uint32_t v, float& a, float& b) {
+    const x2 r = __builtin_bit_cast(x2, v);
+    a = (float)r[0];
+    b = (float)r[1];
   }
   __device__ __forceinline__ static float load(const void* p, int64_t i) { return (float)((const _Float16*)p)[i]; }
   __device__ __forceinline__ static void store(void* p, int64_t i, float v) { ((_Float16*)p)[i] = (_Float16)v; }
@@ -393,6 +402,30 @@ struct RowOf {
 // samples change first, so that every XCD, which gets a run of that order, has
 // a share of the long samples and of the short ones.
 __device__ __forceinline__ int unit_at(const CrossParams& p, int u, int heads) { return u % p.B * heads + u / p.B; }
+// What a workgroup of a launch over units, ranges and tiles of rows or keys works
+// on.  Tiles of a unit run side by side on one XCD, whose L2 then holds what they
+// share; but under an order mask, where they differ in length, all units' longest
+// tiles come first and the short ones fill the gaps (last: the last tiles are the
+// longest, as with rows).
+struct Place {
+  int unit, split, tile;
+};
+template <bool BIAS>
+__device__ __forceinline__ Place place_of(const CrossParams& p, int heads, int tiles, int splits, bool last) {
+  Place w;
+  if (BIAS && p.rb.causal && tiles > 1) {
+    const int n = p.n_wg / tiles, u = xcd_remap(blockIdx.x % n, n), t = blockIdx.x / n;
+    w.unit = unit_at(p, u / splits, heads);
+    w.split = u % splits;
+    w.tile = last ? tiles - 1 - t : t;
+  } else {
+    const int lid = xcd_remap(blockIdx.x, p.n_wg);
+    w.unit = unit_at(p, lid / (tiles * splits), heads);
+    w.split = lid / tiles % splits;
+    w.tile = lid % tiles;
+  }
+  return w;
+}
 // Where the view with these strides has it.
 template <typename P>
 __device__ __forceinline__ P* at(P* base, const Strides& s, const RowOf& r) {

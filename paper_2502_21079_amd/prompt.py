@@ -25,6 +25,7 @@ from operator import index
 from typing import Optional, Union
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import AdaspaError, _check, _ptr, _stream, load_library
 
@@ -379,6 +380,7 @@ class _CrossAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse, key_lens, key_mask = ctx.saved_tensors
         dq, dk, dv = cross_attn_bwd(_rows(dout), q, k, v, out, lse, key_lens=key_lens, key_mask=key_mask,
@@ -395,6 +397,7 @@ class _RelBiasAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, table, out, lse, key_lens, key_mask = ctx.saved_tensors
         grads = rel_bias_attn_bwd(_rows(dout), q, k, v, table, out, lse, key_lens=key_lens, key_mask=key_mask, **ctx.kw)
@@ -402,13 +405,14 @@ class _RelBiasAttention(torch.autograd.Function):
 
 
 def cross_attention(q, k, v, *, key_lens=None, key_mask=None, scale: Optional[float] = None):
-    """The output of :func:`cross_attn`, differentiable in q, k and v."""
+    """The output of :func:`cross_attn`, differentiable (once) in q, k and v."""
     return _CrossAttention.apply(q, k, v, key_lens, key_mask, scale)
 
 
 def rel_bias_attention(q, k, v, table, *, max_distance: int = 128, bidirectional: bool = True, causal: bool = False,
                        q_offset: Union[int, str] = 0, key_lens=None, key_mask=None, scale: Optional[float] = None):
-    """The output of :func:`rel_bias_attn`, differentiable in q, k, v and the table."""
+    """The output of :func:`rel_bias_attn`, differentiable (once) in q, k, v and the
+    table."""
     kw = dict(max_distance=max_distance, bidirectional=bidirectional, causal=causal, q_offset=q_offset, scale=scale)
     return _RelBiasAttention.apply(q, k, v, table, key_lens, key_mask, kw)
 
