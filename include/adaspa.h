@@ -381,7 +381,9 @@ typedef struct {
  * holds the distances [bucket_start[m], bucket_start[m+1]), the last one all
  * from its start on.  Bidirectional: the first half of the table is for keys
  * at or before the query, the second for keys after it; otherwise keys after
- * the query have distance 0. */
+ * the query have distance 0.  A value past -2.3e38 (log2(e) times it leaves fp32)
+ * counts as minus infinity and hides its keys; where a row sees nothing but values of
+ * a large magnitude, its scores and lse hold 2^-24 of that. */
 typedef struct {
   int32_t num_buckets;            /* rows of the table, [num_buckets, H]; at most 256 a direction */
   int32_t bidirectional;

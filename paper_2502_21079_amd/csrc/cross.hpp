@@ -59,6 +59,7 @@ struct CrossParams {
 struct CrossPlan {
   bool resident;                       // the keys of a head stay in LDS, splits workgroups share its rows
   bool small;                          // backward: queries and keys of a head fit in LDS, one kernel does all
+  bool delta_first;                    // backward: a pass for delta, which dq then takes
   int splits, kv_splits;
   int64_t part_o, part_ml, part_d, row_ld, part_kv, part_t;   // byte offsets into the workspace
   int64_t bytes;

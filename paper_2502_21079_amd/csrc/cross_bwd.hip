@@ -18,7 +18,7 @@ namespace adaspa {
 namespace {
 constexpr int kDqRows = 128;           // query rows of a workgroup of cross_dq_kernel
 constexpr int kDkvWaves = 4;           // waves of 32 keys of a workgroup of cross_dkv_kernel
-// delta from the rounded output is off by about its rounding, which dq carries
+// delta from the rounded output is off by its rounding, which dq carries
 // times sum_j P_ij k_j.  Where registers allow that sum next to dq (d 64), dq is
 // put right by it once the row's exact delta is known: dq's error against 64 bits
 // falls from about 1.5 to 1.4 times that of the final rounding alone (the rest
@@ -38,8 +38,16 @@ __device__ __forceinline__ uint32_t split_pair(float a, float b, uint32_t& rest)
   return hi;
 }
 
+// fp16 weights for dv carry 2^14 (no weight is above 1): of 100,000 keys most have
+// weights below fp16's smallest normal number.
+template <class T>
+constexpr float kShift = T::kHalf ? 14.f : 0.f;
+template <class T>
+constexpr float kUnshift = T::kHalf ? 1.f / 16384.f : 1.f;
+
 // What a launch of cross_dq_kernel does.  Where few rows share many keys the
-// keys are split, and delta, which needs them all, comes first: DELTA leaves each
+// keys are split, and delta, which needs them all, comes first, as it does for long
+// walks at d 128: DELTA leaves each
 // range's sum of P dP, DQ adds these up and forms its range's dq.  (With delta
 // from the rounded output there, 25 queries over 18,266 keys had dq off by 5.4e-3
 // of its size where rounding dS and dq alone gives 2.4e-3.)
@@ -272,7 +280,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[d][e] = fmaf(-more, pk[EXACT ? d : 0][e], acc[d][e]);
   }
-  if (PASS == DQ) store_tile_f32<D>(acc, p.part_o + (split * all_rows + row) * D, row_ok, hw);
+  if (PASS == DQ && p.splits > 1) store_tile_f32<D>(acc, p.part_o + (split * all_rows + row) * D, row_ok, hw);
   else store_tile<T, D>(acc, p.scale, at(p.dq, p.sdq, two.a), two.a_ok, at(p.dq, p.sdq, two.b), two.b_ok, lane);
   // What cross_dkv_kernel takes as delta is free of the output's rounding: the
   // weights add up to 1, so the sum of P dP is delta and the sum of dS.
@@ -281,11 +289,15 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 }
 
 // dq with few keys: they stay in LDS, as in the forward pass, and each wave
-// walks row tiles of 32 on its own, without barriers.  ONE is for one tile of
-// keys: S and dP are formed twice, delta exactly from the first time, and the
-// output is not read, since there the rows' way through memory takes longer than
-// the products (24 x 110,080 rows over 64 keys, one walk and the output against
-// two walks: d 64 311 and 259 us, d 128 593 and 452).
+// walks row tiles of 32 on its own, without barriers.  TWICE is for the fewest:
+// S and dP are formed twice, delta exactly from the first time, and the output is
+// not read, since there the rows' way through memory takes longer than the products
+// (us, one walk and the output against two walks: 24 x 110,080 rows over 64 keys,
+// d 64 311 and 259, d 128 593 and 452; whole training passes at d 128, 24 x 50,000
+// rows over 128 keys 602 and 580, 48 x 20,000 over 100 479 and 474).  What bounds it
+// otherwise: the products beside the rows' way through memory (24 x 110,080 rows
+// over 256 keys, d 128: 2.7 GB, 565 us at a large copy's rate; four products, 692
+// GFLOP, 613 us at a large product's; KEEPDQ us).
 template <int D>
 constexpr int kTwiceBlocks = D == 64 ? 2 : 4;              // blocks of 32 keys that are walked twice
 template <class T, int D, bool TWICE>
@@ -526,9 +538,12 @@ struct TableSums {
 // The whole backward pass of one (sample, key head) whose queries and keys both
 // fit in LDS (256 of each at d 64, 128 at d 128), in one launch: a wave takes 32
 // rows for dq and delta, then, with the rows' statistics in LDS, 32 keys for dk
-// and dv.  A text encoder's prompts are of this size, and three launches one
-// after the other cost more than their work (8 x 24 heads x 226 tokens, d 64:
-// see the kernels' times in the design notes).
+// and dv.  A text encoder's prompts are of this size, and three launches one after
+// the other cost more than their work (8 x 24 heads x 226 tokens with a position
+// bias, d 64, forward and backward: 89 us with them, SMALLAB so).  What bounds it:
+// one workgroup's walk, 16 blocks of 32 keys or rows one after the other, in which
+// the vector units have more to do than the matrix pipe; 192 such workgroups have a
+// CU each.
 template <int D>
 constexpr int kSmallWaves = D == 64 ? 8 : 4;
 constexpr int kSmallFar = 256;         // the most far with which the sums by diagonal fit as well
@@ -940,7 +955,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
     auto stage_arg = [&](int u) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        arg[2 * u + k] = BIAS ? fmaf(x[2 * u + k], p.sl2, bias[2 * u + k]) : x[2 * u + k] * p.sl2;
+        arg[2 * u + k] = fmaf(x[2 * u + k], p.sl2, BIAS ? bias[2 * u + k] : kShift<T>);
         pin(arg[2 * u + k]);
       }
     };
@@ -955,6 +970,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         float v = arg[2 * u + k] * y[2 * u + k];
+        if (T::kHalf) v *= kUnshift<T>;
         pin(v);
         y[2 * u + k] = v;
       }
@@ -1008,7 +1024,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
   if (i0 < i1) issue(0);
   if (BIAS) {
     table.clear();
-    fill_bias<T, NT>(bt, start, p, hk * p.G, tid);
+    fill_bias<T, NT>(bt, start, p, hk * p.G, tid, kShift<T>);
   }
   int q0 = in_q, g_head = in_h - hk * p.G;                // of the current item
   if (i0 < i1) {
@@ -1026,7 +1042,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
     if (BIAS && g_head != head) {                         // another query head: its own bias
       __syncthreads();
       while (head < g_head) flush();
-      fill_bias<T, NT>(bt, start, p, hk * p.G + g_head, tid);
+      fill_bias<T, NT>(bt, start, p, hk * p.G + g_head, tid, kShift<T>);
       __syncthreads();
     }
     const int after = slot == 2 ? 0 : slot + 1, before = slot == 0 ? 2 : slot - 1;
@@ -1077,7 +1093,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
   u16* dvh = p.dv + b * p.sdv.b + hk * p.sdv.h;
   const bool a_in = key_a < p.Lk, b_in = key_b < p.Lk;
   store_tile<T, D>(dk, p.scale, dkh + (int64_t)key_a * p.sdk.t, a_in, dkh + (int64_t)key_b * p.sdk.t, b_in, lane);
-  store_tile<T, D>(dv, 1.f, dvh + (int64_t)key_a * p.sdv.t, a_in, dvh + (int64_t)key_b * p.sdv.t, b_in, lane);
+  store_tile<T, D>(dv, kUnshift<T>, dvh + (int64_t)key_a * p.sdv.t, a_in, dvh + (int64_t)key_b * p.sdv.t, b_in, lane);
 }
 
 // Rows of a result from the splits' partial rows, added in order.  Two results
@@ -1164,6 +1180,12 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   c.splits = tiles > 0 && tiles <= 96 && nt > 12 ? clamp_splits(512 / tiles, nt / 4) : 1;
   c.resident = keep_keys(p, D, bias, 1);
   if (c.resident) c.splits = keep_chunks(p, 1);
+  // dq shrinks with the square root of the number of keys, what an error of delta
+  // puts into it does not (sum_j P_ij k_j leans towards q_i): where no correction sum
+  // follows (d 128), long walks have their delta formed first as well.  dq's error, in
+  // units of its final rounding, with delta from the output: 1.3 at 2,245 keys, 3.6 at
+  // 49,836; 1.4 so, at one product in five more.
+  c.delta_first = !c.resident && (c.splits > 1 || (D == 128 && nt > (bias && p.rb.causal ? 64 : 32)));
   const int64_t ktiles = (int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves));
   const int64_t items = (int64_t)p.G * ((p.Lq + 63) / 64);
   // Ranges of the queries: rounds of as many workgroups as run at a time (two
@@ -1188,7 +1210,7 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   c.part_o = off;
   if (c.splits > 1 && !c.resident) off += up256(c.splits * rows * D * 4);
   c.part_d = off;
-  if (c.splits > 1 && !c.resident) off += up256(c.splits * rows * 4);
+  if (c.delta_first) off += up256(c.splits * rows * 4);
   c.part_kv = off;
   if (c.kv_splits > 1) off += up256((int64_t)c.kv_splits * 2 * p.B * p.Hk * p.Lk * D * 4);
   c.part_t = off;
@@ -1229,14 +1251,16 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
     if (p.Lk <= 32 * kTwiceBlocks<D>) hipLaunchKernelGGL((cross_keep_dq_kernel<T, D, true>), grid, block, keep_lds_bytes(p.Lk), st, p);
     else hipLaunchKernelGGL((cross_keep_dq_kernel<T, D, false>), grid, block, keep_lds_bytes(p.Lk), st, p);
   } else if (p.n_wg > 0) {
-    if (p.splits > 1) {
+    if (c.delta_first) {
       launch_dq<T, D, DELTA>(p, bias, lds, st);
       launch_dq<T, D, DQ>(p, bias, lds, st);
+    } else {
+      launch_dq<T, D, WHOLE>(p, bias, lds, st);
+    }
+    if (p.splits > 1) {
       const SumOf dq = {p.part_o, p.dq, p.sdq, p.scale};
       hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, st, dq, dq,
                          rows * D, p.splits, rows, p.H, p.Lq);
-    } else {
-      launch_dq<T, D, WHOLE>(p, bias, lds, st);
     }
   }
   p.n_wg = (int)((int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves)) * p.kv_splits);
@@ -1244,7 +1268,7 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
     if (bias) hipLaunchKernelGGL((cross_dkv_kernel<T, D, true>), dim3(p.n_wg), dim3(64 * kDkvWaves),
                                  lds + kDkvWaves * diag_entries(p.rb.far) * 4, st, p);
     else hipLaunchKernelGGL((cross_dkv_kernel<T, D, false>), dim3(p.n_wg), dim3(64 * kDkvWaves), 0, st, p);
-    const SumOf dk = {p.part_kv, p.dk, p.sdk, p.scale}, dv = {p.part_kv + keys * D, p.dv, p.sdv, 1.f};
+    const SumOf dk = {p.part_kv, p.dk, p.sdk, p.scale}, dv = {p.part_kv + keys * D, p.dv, p.sdv, kUnshift<T>};
     if (p.kv_splits > 1)
       hipLaunchKernelGGL((cross_sum_kernel<T, D>), dim3((uint32_t)((keys + per - 1) / per), 2), dim3(256), 0, st, dk, dv,
                          2 * keys * D, p.kv_splits, keys, p.Hk, p.Lk);

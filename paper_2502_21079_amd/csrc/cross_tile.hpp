@@ -204,9 +204,11 @@ __device__ __forceinline__ float table_value(const RelBias& rb, int64_t i) {
   return rb.table_f32 ? ((const float*)rb.table)[i] : T::load(rb.table, i);
 }
 // Fills bt (bias_entries floats) for head h; start: LDS room of side entries.
-// The caller has a barrier between this and the first read.
+// The caller has a barrier between this and the first read.  (shift: added to every
+// value.)
 template <class T, int NT>
-__device__ __forceinline__ void fill_bias(float* bt, uint16_t* start, const CrossParams& p, int h, int tid) {
+__device__ __forceinline__ void fill_bias(float* bt, uint16_t* start, const CrossParams& p, int h, int tid,
+                                          float shift = 0.f) {
   for (int i = tid; i < p.rb.side; i += NT) start[i] = p.rb.start[i];
   __syncthreads();
   const int n = bias_entries(p.rb.far);
@@ -214,7 +216,7 @@ __device__ __forceinline__ void fill_bias(float* bt, uint16_t* start, const Cros
     const int rel = i - p.rb.far - kPad;
     float v = -INFINITY;
     if (i < n - 32 && !(p.rb.causal && rel > 0))
-      v = table_value<T>(p.rb, (int64_t)bucket_of(start, p.rb, rel) * p.H + h) * kLog2e;
+      v = table_value<T>(p.rb, (int64_t)bucket_of(start, p.rb, rel) * p.H + h) * kLog2e + shift;
     bt[i] = v;
   }
 }
@@ -230,8 +232,7 @@ __device__ __forceinline__ int query_offset(const CrossParams& p, int n) { retur
 // follows it takes 32 bytes of each of 32 rows.  Here each access takes 64 bytes
 // of 16 rows (groups of 16 lanes take one chunk each), and two accesses, the
 // lower and the upper 16 rows, exchange groups (one v_permlane16_swap per
-// register).  (The long video's forward pass without any products, one key tile
-// of four: see the kernel.)
+// register).
 template <class T, int D>
 struct TileRegs {
   u32x4 w[D / 16];                                       // chunk 4 j + lane / 16 of rows (2 j: lower, 2 j + 1: upper)

@@ -270,8 +270,9 @@ def rel_bias_attn(q, k, v, table, *, max_distance: int = 128, bidirectional: boo
     the bucket being that of key position minus query position
     (:func:`relative_bucket_starts`): ``table`` is [num_buckets, H], fp32 or of
     q's type.  When ``bidirectional`` the second half of its rows is for keys
-    after the query; otherwise those count as distance 0.  ``causal`` masks
-    them.  Query i stands at position i + ``q_offset`` among the keys; "end"
+    after the query; otherwise those count as distance 0.  Values of minus
+    infinity, or past -2.3e38, hide their keys.  ``causal`` masks keys after the
+    query.  Query i stands at position i + ``q_offset`` among the keys; "end"
     puts a sample's queries at its last positions (decoding with a cache: one
     query over key_lens[b] keys).  Returns (out, lse)."""
     bias = _bias_key(q, k, table, max_distance, bidirectional, causal, q_offset)
