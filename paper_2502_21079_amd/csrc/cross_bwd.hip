@@ -54,6 +54,11 @@ constexpr float kUnshift = T::kHalf ? 1.f / 16384.f : 1.f;
 enum { WHOLE = 0, DELTA = 1, DQ = 2 };
 }  // namespace
 
+// dq of 128 query rows over one range of their keys: four waves of 32 rows, whose q
+// and dO stay in registers, tiles of 64 keys through two slots.  What bounds it: under
+// an order mask the last rows' walk (12 x 4,095 tokens at d 128: 167 us for 64 tiles
+// one after the other, the matrix pipe 26% busy); otherwise products and exponentials
+// that two waves per SIMD overlap only in part.
 template <class T, int D, bool BIAS, int PASS>
 __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
@@ -297,7 +302,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 // rows over 128 keys 602 and 580, 48 x 20,000 over 100 479 and 474).  What bounds it
 // otherwise: the products beside the rows' way through memory (24 x 110,080 rows
 // over 256 keys, d 128: 2.7 GB, 565 us at a large copy's rate; four products, 692
-// GFLOP, 613 us at a large product's; KEEPDQ us).
+// GFLOP, 613 us at a large product's; 785 us, the matrix pipe 45% busy).
 template <int D>
 constexpr int kTwiceBlocks = D == 64 ? 2 : 4;              // blocks of 32 keys that are walked twice
 template <class T, int D, bool TWICE>
@@ -540,7 +545,7 @@ struct TableSums {
 // rows for dq and delta, then, with the rows' statistics in LDS, 32 keys for dk
 // and dv.  A text encoder's prompts are of this size, and three launches one after
 // the other cost more than their work (8 x 24 heads x 226 tokens with a position
-// bias, d 64, forward and backward: 89 us with them, SMALLAB so).  What bounds it:
+// bias, d 64, forward and backward: 89 us with them, 51 so, 38 of them here).  What bounds it:
 // one workgroup's walk, 16 blocks of 32 keys or rows one after the other, in which
 // the vector units have more to do than the matrix pipe; 192 such workgroups have a
 // CU each.
@@ -779,7 +784,10 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
 // of the one before and the third of the one before that, so that the matrix
 // pipe has work while the VALU does: at d 128 the accumulators leave one wave
 // per SIMD, and no other wave would fill the gaps.  Tiles stay in a ring of
-// three for it.
+// three for it.  What bounds it: the matrix pipe at one wave's pace (24 heads x 110,080
+// rows over 256 keys, d 128: 692 GFLOP in 735 us, 942 TFLOP/s, the pipe 50% busy; a
+// large product reaches 1,136); under an order mask the first keys' walk, with the
+// table's sums by diagonal (12 x 4,095 tokens, d 128: 181 us).
 template <class T, int D, bool BIAS>
 __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_kernel(const CrossParams p) {
   constexpr int NW = kDkvWaves, NT = 64 * NW, KE = 64 * D;
@@ -1097,7 +1105,8 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
 }
 
 // Rows of a result from the splits' partial rows, added in order.  Two results
-// (dk and dv) side by side in one launch: blockIdx.y chooses.
+// (dk and dv) side by side in one launch: blockIdx.y chooses.  Bound by its bytes, of
+// which L2 holds a part (101 MB of dk's and dv's partial rows of the long video: 18 us).
 struct SumOf {
   const float* part;
   u16* out;
@@ -1127,7 +1136,8 @@ __global__ __launch_bounds__(256) void cross_sum_kernel(SumOf first, SumOf secon
 }
 
 // dtable[u, h]: the shares of head h over samples and workgroups, 64 runs of them
-// for four buckets at a time, each in order, then the runs' sums in order.
+// for four buckets at a time, each in order, then the runs' sums in order.  A chain of
+// loads: 4.6 us for 32 shares of 64 buckets as for 8 of 32.
 template <class T>
 __global__ __launch_bounds__(256) void cross_dtable_kernel(const CrossParams p, int per) {
   __shared__ float sum[64][4];

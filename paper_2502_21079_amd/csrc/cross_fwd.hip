@@ -92,7 +92,11 @@ struct Rows {
 
 // Workgroup: 128 query rows of one unit over one range of its keys, 64-key
 // tiles through a ring of RING slots in LDS, RING - 1 of them on their way while
-// one is used.
+// one is used.  What bounds it: one row over long keys, HBM (4 samples of 4 key
+// heads, 17,664 keys, d 128: 145 MB in 24 us, and the join 4); many rows, products
+// and weights that two or three waves per SIMD overlap only in part (24 x 256 rows
+// over 110,080 keys, d 128: 346 GFLOP in 430 us, matrix pipe 45% busy and vector
+// units 34%; 12 x 8,191 at d 64 with a bias: 206 GFLOP in 252 us, 38% and 62%).
 template <class T, int D, bool BIAS, int RING>
 __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
@@ -232,7 +236,10 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 
 // Few keys, many rows: the keys and values of one (sample, key head) stay in
 // LDS, and each wave walks row tiles on its own, without barriers; the next
-// tile's queries are loaded while one is worked on.
+// tile's queries are loaded while one is worked on.  What bounds it: the rows' way
+// through memory beside products and weights (24 x 110,080 rows over 256 keys, d 128:
+// 1.37 GB and 346 GFLOP in 425 us, 285 and 305 at a large copy's and product's rates;
+// streaming the keys instead takes 577).
 template <class T, int D>
 __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_kernel(const CrossParams p) {
   constexpr int NW = kKeepWaves, QR = keep_rows(D);
@@ -318,7 +325,8 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_ke
 // their sums, all in a fixed order.  Many ranges come with few rows and want a
 // workgroup per row (NG = 256 / (D / 4)); few ranges come with many rows, and one
 // group per row then leaves no thread without a range (24,776 rows of d 64 in two
-// ranges: 36 us with a workgroup per row, 5.7 so).
+// ranges: 36 us with a workgroup per row, 5.7 so).  A chain of loads where rows are
+// few (96 of 42 ranges: 4 us), else bound by its bytes.
 template <class T, int D, int NG>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossParams p) {
   constexpr int TPR = D / 4;
