@@ -30,12 +30,11 @@ constexpr bool kExactDq = D == 64;
 // into the product as a sum of two values, its upper bits and what they leave, so
 // that delta's error and the final rounding are all that is left.
 template <class T>
-__device__ __forceinline__ uint32_t split_pair(float a, float b, uint32_t& rest) {
+__device__ __forceinline__ uint2 split_pair(float a, float b) {
   const uint32_t hi = T::pack(a, b);
   float c, d;
   T::unpack(hi, c, d);
-  rest = T::pack(a - c, b - d);
-  return hi;
+  return make_uint2(hi, T::pack(a - c, b - d));
 }
 
 // fp16 weights for dv carry 2^14 (no weight is above 1): of 100,000 keys most have
@@ -247,9 +246,9 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
         s0 += y[e];
         s1 += y[e + 1];
         if (SPLIT) {
-          uint32_t rest;
-          w[e >> 3][(e & 7) >> 1] = split_pair<T>(y[e], y[e + 1], rest);
-          wp[e >> 3][(e & 7) >> 1] = rest;
+          const uint2 v = split_pair<T>(y[e], y[e + 1]);
+          w[e >> 3][(e & 7) >> 1] = v.x;
+          wp[e >> 3][(e & 7) >> 1] = v.y;
         } else {
           w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
           wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
@@ -396,9 +395,9 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
         s0 += y[e];
         s1 += y[e + 1];
         if (SPLIT) {
-          uint32_t rest;
-          w[e >> 3][(e & 7) >> 1] = split_pair<T>(y[e], y[e + 1], rest);
-          wp[e >> 3][(e & 7) >> 1] = rest;
+          const uint2 v = split_pair<T>(y[e], y[e + 1]);
+          w[e >> 3][(e & 7) >> 1] = v.x;
+          wp[e >> 3][(e & 7) >> 1] = v.y;
         } else {
           w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
           wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
@@ -545,17 +544,26 @@ struct TableSums {
 // rows for dq and delta, then, with the rows' statistics in LDS, 32 keys for dk
 // and dv.  A text encoder's prompts are of this size, and three launches one after
 // the other cost more than their work (8 x 24 heads x 226 tokens with a position
-// bias, d 64, forward and backward: 89 us with them, 51 so, 38 of them here).  What bounds it:
-// one workgroup's walk, 16 blocks of 32 keys or rows one after the other, in which
-// the vector units have more to do than the matrix pipe; 192 such workgroups have a
-// CU each.
+// bias, d 64, forward and backward: 89 us with them, 51 so, 38 of them here).  What
+// bounds it: one workgroup's walk, 16 blocks of 32 keys or rows one after the other,
+// in which the vector units have more to do than the matrix pipe; 192 such
+// workgroups have a CU each.
 template <int D>
 constexpr int kSmallWaves = D == 64 ? 8 : 4;
 constexpr int kSmallFar = 256;         // the most far with which the sums by diagonal fit as well
 
-template <class T, int D, bool BIAS>
-__global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_small_bwd_kernel(const CrossParams p) {
-  constexpr int NW = kSmallWaves<D>, NT = 64 * NW, L = 32 * NW, TILES = L / 64;
+// TINY is for up to 64 queries and keys: fewer waves, and P and dS go into their
+// products as two values each, since the gradients of a few rows and keys are a few
+// hundred values, whose rounding errors may by chance lie well above their mean
+// (6 x 8, d 128: dk's 1.7 times the final rounding alone).
+constexpr int kTiny = 64;
+template <int D>
+constexpr int kTinyWaves = D == 64 ? 2 : 4;               // waves load a tile in periods of its row order
+
+template <class T, int D, bool BIAS, bool TINY>
+__global__ __launch_bounds__(64 * (TINY ? kTinyWaves<D> : kSmallWaves<D>), D == 64 && !TINY ? 2 : 1) void cross_small_bwd_kernel(
+    const CrossParams p) {
+  constexpr int NW = TINY ? kTinyWaves<D> : kSmallWaves<D>, NT = 64 * NW, L = 32 * NW, TILES = L / 64;
   __shared__ __attribute__((aligned(1024))) u16 sQ[L * D], sG[L * D], sK[L * D], sV[L * D];
   __shared__ __attribute__((aligned(16))) float st[2][L]; // -LSE / scale and -delta of the rows
   __shared__ float mask[L];                               // 0 or -inf per key
@@ -680,14 +688,16 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
         block(j, x, y);
         const int ca = fresh(ca0);
         float s0 = 0.f, s1 = 0.f;
-        u32x4 w[2], wp[2];
+        u32x4 w[2], wp[2], wr[2];
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
           y[e] *= x[e];
           y[e + 1] *= x[e + 1];
           s0 += y[e];
           s1 += y[e + 1];
-          w[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+          const uint2 v = split_pair<T>(y[e], y[e + 1]);
+          w[e >> 3][(e & 7) >> 1] = v.x;
+          if (TINY) wr[e >> 3][(e & 7) >> 1] = v.y;
           wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
         }
         more += s0 + s1;
@@ -697,6 +707,7 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
           for (int d = 0; d < D / 32; ++d) {
             const typename T::x8 kf = read_col<T, D>(sK + 32 * j * D, ca, d, 16 * s);
             acc[d] = T::mfma(kf, __builtin_bit_cast(typename T::x8, w[s]), acc[d]);
+            if (TINY) acc[d] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wr[s]), acc[d]);
             pk[d] = T::mfma(kf, __builtin_bit_cast(typename T::x8, wp[s]), pk[d]);
           }
       }
@@ -742,7 +753,7 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
         }
         const float* at = bt + bias_entries(far) - 1;     // a masked key's: -inf
         if (BIAS && key_ok) at = bt + bias_from(lo, far) + far + kPad + 31 + c32 - 4 * hw;
-        u32x4 wp[2], ws[2];
+        u32x4 wp[2], ws[2], pr[2], sr[2];
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
           const int r = 8 * (e >> 2) + (e & 3);
@@ -750,16 +761,29 @@ __global__ __launch_bounds__(64 * kSmallWaves<D>, D == 64 ? 2 : 1) void cross_sm
           const float c = fast_exp2(BIAS ? fmaf(x[e + 1], p.sl2, at[-r - 1]) : x[e + 1] * p.sl2);
           y[e] *= a;
           y[e + 1] *= c;
-          wp[e >> 3][(e & 7) >> 1] = T::pack(a, c);
-          ws[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+          if (TINY) {
+            const uint2 v = split_pair<T>(a, c), t = split_pair<T>(y[e], y[e + 1]);
+            wp[e >> 3][(e & 7) >> 1] = v.x;
+            pr[e >> 3][(e & 7) >> 1] = v.y;
+            ws[e >> 3][(e & 7) >> 1] = t.x;
+            sr[e >> 3][(e & 7) >> 1] = t.y;
+          } else {
+            wp[e >> 3][(e & 7) >> 1] = T::pack(a, c);
+            ws[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
+          }
         }
         if (BIAS) table.add(y, lo);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int d = 0; d < D / 32; ++d) {
-            dv[d] = T::mfma(read_col<T, D>(tG, ca, d, 16 * s), __builtin_bit_cast(typename T::x8, wp[s]), dv[d]);
-            dk[d] = T::mfma(read_col<T, D>(tQ, ca, d, 16 * s), __builtin_bit_cast(typename T::x8, ws[s]), dk[d]);
+            const typename T::x8 gc = read_col<T, D>(tG, ca, d, 16 * s), qc = read_col<T, D>(tQ, ca, d, 16 * s);
+            dv[d] = T::mfma(gc, __builtin_bit_cast(typename T::x8, wp[s]), dv[d]);
+            dk[d] = T::mfma(qc, __builtin_bit_cast(typename T::x8, ws[s]), dk[d]);
+            if (TINY) {
+              dv[d] = T::mfma(gc, __builtin_bit_cast(typename T::x8, pr[s]), dv[d]);
+              dk[d] = T::mfma(qc, __builtin_bit_cast(typename T::x8, sr[s]), dk[d]);
+            }
           }
       }
     }
@@ -1235,6 +1259,14 @@ static void launch_dq(const CrossParams& p, bool bias, uint32_t lds, hipStream_t
   else hipLaunchKernelGGL((cross_dq_kernel<T, D, false, PASS>), dim3(p.n_wg), dim3(256), 0, st, p);
 }
 
+template <class T, int D, bool TINY>
+static void launch_small(const CrossParams& p, bool bias, uint32_t lds, hipStream_t st) {
+  constexpr int NW = TINY ? kTinyWaves<D> : kSmallWaves<D>;
+  if (bias) hipLaunchKernelGGL((cross_small_bwd_kernel<T, D, true, TINY>), dim3(p.n_wg), dim3(64 * NW),
+                               lds + NW * diag_entries(p.rb.far) * 4, st, p);
+  else hipLaunchKernelGGL((cross_small_bwd_kernel<T, D, false, TINY>), dim3(p.n_wg), dim3(64 * NW), 0, st, p);
+}
+
 template <class T, int D>
 static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStream_t st) {
   p.splits = c.splits;
@@ -1246,12 +1278,8 @@ static hipError_t run_bwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   const dim3 table(p.H, (buckets + 3) / 4);
   if (c.small) {
     p.n_wg = p.B * p.Hk;
-    constexpr int NW = kSmallWaves<D>;
-    if (p.n_wg > 0 && !bias)
-      hipLaunchKernelGGL((cross_small_bwd_kernel<T, D, false>), dim3(p.n_wg), dim3(64 * NW), 0, st, p);
-    if (p.n_wg > 0 && bias)
-      hipLaunchKernelGGL((cross_small_bwd_kernel<T, D, true>), dim3(p.n_wg), dim3(64 * NW),
-                         lds + NW * diag_entries(p.rb.far) * 4, st, p);
+    if (p.n_wg > 0 && p.Lq <= kTiny && p.Lk <= kTiny) launch_small<T, D, true>(p, bias, lds, st);
+    else if (p.n_wg > 0) launch_small<T, D, false>(p, bias, lds, st);
     if (bias) hipLaunchKernelGGL((cross_dtable_kernel<T>), table, dim3(256), 0, st, p, 1);
     return hipGetLastError();
   }

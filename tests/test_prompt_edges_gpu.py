@@ -129,3 +129,22 @@ def test_dq_over_very_many_keys(bias, Lq, Lk, dt):
     kw = dict(table=table[:, h], causal=True, q_offset=rows.start) if bias else {}
     ref = reference(q[:, h, rows], k, v, dout=g[:, h, rows], **kw)["dq"][0]
     assert off_by(dq[:, h, rows], ref) < 1.1 * math.sqrt(2) * off_by(ref.to(dt), ref)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Lq,Lk", [(1, 1), (8, 8), (6, 17), (64, 64), (33, 40), (64, 1), (65, 64), (1, 64)])
+def test_backward_of_tiny_problems(Lq, Lk, D):
+    """Up to 64 queries and keys, one of each more, with masks, shared heads and an
+    order mask; and every gradient within sqrt(2) times its final rounding: that, and
+    an error of delta or of the forward call's lse that is no larger."""
+    dt = HF if Lq % 2 else BF
+    q, k, v, g = make(3, 4, 2, Lq, Lk, D, dt, "blhd", seed=15)
+    table = table_of(8, 4, dt)
+    run_bias(q, k, v, g, table, max_distance=20, key_lens=lens_of(3, Lk, "empty"), key_mask=mask_of(3, Lk, "some"))
+    run_bias(q, k, v, g, table, max_distance=20, causal=True)
+    if min(Lq, Lk) > 5 and max(Lq, Lk) <= 64:
+        kw = dict(max_distance=20)
+        out, lse = ad.rel_bias_attn(q, k, v, table, **kw)
+        ref = reference(q, k, v, dout=g, table=table, **kw)
+        for name, x in zip(("dq", "dk", "dv"), ad.rel_bias_attn_bwd(g, q, k, v, table, out, lse, **kw)):
+            assert off_by(x, ref[name][0]) < math.sqrt(2) * off_by(ref[name][0].to(dt), ref[name][0]), name
