@@ -21,7 +21,7 @@ constexpr float kSumLimit = 256.f;     // a lane's weights of one tile add up to
 // is the maximum looked for, the reference moved there and the tile's weights
 // taken again.  So no weight exceeds 2^8, which fp16 holds too, and most tiles
 // need neither a maximum nor a rescaled accumulator.
-template <class T, int D>
+template <class T, int D, int G = 2>
 struct Rows {
   f32x16 o[D / 32];
   float m, l;
@@ -31,12 +31,12 @@ struct Rows {
     m = -INFINITY;
     l = 0.f;
   }
-  // Weights of 64 scores (sl2 x in log2 units), returns this lane's sum.
-  __device__ __forceinline__ float weights(const f32x16 (&x)[2], float sl2, typename T::x8 (&pb)[2][2]) const {
+  // Weights of G times 32 scores (sl2 x in log2 units), returns this lane's sum.
+  __device__ __forceinline__ float weights(const f32x16 (&x)[G], float sl2, typename T::x8 (&pb)[G][2]) const {
     const float ref = m == -INFINITY ? 0.f : -m;
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < G; ++g) {
       u32x4 w[2];
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
@@ -52,10 +52,10 @@ struct Rows {
   }
   // Moves the reference of the rows that need it to the maximum where that is
   // above it.  (In the first tile there is nothing yet to rescale.)
-  __device__ __forceinline__ void raise(const f32x16 (&x)[2], float sl2, bool first, bool need) {
+  __device__ __forceinline__ void raise(const f32x16 (&x)[G], float sl2, bool first, bool need) {
     float mt = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) mt = vmax(mt, vmax(x[g][e], x[g][e + 1]));
     mt = both_halves_max(mt) * sl2;
@@ -69,9 +69,9 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[d][e] *= a;
   }
-  // Scores of 64 keys: weights into pb, their fp32 sum into l.  first: of the
+  // Scores of the keys: weights into pb, their fp32 sum into l.  first: of the
   // first tile, whose rows have no reference yet.
-  __device__ __forceinline__ void weigh(const f32x16 (&x)[2], float sl2, typename T::x8 (&pb)[2][2], bool first) {
+  __device__ __forceinline__ void weigh(const f32x16 (&x)[G], float sl2, typename T::x8 (&pb)[G][2], bool first) {
     if (first) raise(x, sl2, true, true);
     float s = weights(x, sl2, pb);
     // A row that has seen no key yet has no reference either.  Whether a row
@@ -91,16 +91,16 @@ struct Rows {
 }  // namespace
 
 // Workgroup: 128 query rows of one unit over one range of its keys, 64-key
-// tiles through a ring of RING slots in LDS, RING - 1 of them on their way while
-// one is used.  What bounds it: one row over long keys, HBM (4 samples of 4 key
-// heads, 17,664 keys, d 128: 145 MB in 24 us, and the join 4); many rows, products
-// and weights that two or three waves per SIMD overlap only in part (24 x 256 rows
-// over 110,080 keys, d 128: 346 GFLOP in 430 us, matrix pipe 45% busy and vector
-// units 34%; 12 x 8,191 at d 64 with a bias: 206 GFLOP in 252 us, 38% and 62%).
-template <class T, int D, bool BIAS, int RING>
+// tiles through two slots in LDS, one on its way while the other is used.  What
+// bounds it: one row over long keys at d 128, HBM (4 samples of 4 key heads, 17,664
+// keys: 145 MB in 24 us, and the join 4); many rows, products and weights that two
+// or three waves per SIMD overlap only in part (24 x 256 rows over 110,080 keys,
+// d 128: 346 GFLOP in 430 us, matrix pipe 45% busy and vector units 34%; 12 x 8,191
+// at d 64 with a bias: 206 GFLOP in 252 us, 38% and 62%).
+template <class T, int D, bool BIAS>
 __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
-  __shared__ __attribute__((aligned(1024))) u16 ring[RING][2 * KE];
+  __shared__ __attribute__((aligned(1024))) u16 ring[2][2 * KE];
   __shared__ uint16_t start[BIAS ? kMaxBucketSide : 1];
   extern __shared__ __attribute__((aligned(16))) float bt[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -128,17 +128,14 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
   lv.init(wave, lane, p.sv.t);
   const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
   const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
-  int mb[RING];
+  int mb[2] = {1, 1};
   auto issue = [&](auto slot, int t) {
     const uint32_t dst = lds_addr(ring[0]) + slot * 4 * KE;
     lk.issue(dst, kh + (int64_t)t * 64 * p.sk.t, p.sk.t, n - t * 64);
     lv.issue(dst + KE * 2, vh + (int64_t)t * 64 * p.sv.t, p.sv.t, n - t * 64);
     if (p.key_mask) mb[slot] = mask_byte(p, b, t * 64, n, fresh(lane));
   };
-  static_for<RING>([&](auto u) {
-    mb[u] = 1;
-    if (u < RING - 1 && t0 + u < t1) issue(u, t0 + u);
-  });
+  if (t0 < t1) issue(integral_constant<int, 0>{}, t0);
   typename T::x8 qf[D / 16];
   const TwoRows two = two_rows<BIAS>(p, unit, rw, n_rows, lane);
   load_tile<T, D>(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane, qf);
@@ -159,14 +156,10 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
   const int rel0 = 4 * hw - (ro.i + off);
 
   auto tile = [&](auto u, int t) {
-    // This tile is there when no more than the younger ones' loads are left.
-    constexpr int YOUNGER = (RING - 2) * 2 * TileLoad<D, NW>::PER;
-    static_assert(YOUNGER < 16, "fits the wait's low bits");
-    if (RING > 2 && t + RING - 2 < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | YOUNGER);
-    else wait_vmem();
+    wait_vmem();
     const uint64_t keep = below(t * 64, n) & (p.key_mask ? __ballot(mb[u] != 0) : ~0ull);
     __syncthreads();
-    if (t + RING - 1 < t1) issue(integral_constant<int, (u + RING - 1) % RING>{}, t + RING - 1);
+    if (t + 1 < t1) issue(integral_constant<int, 1 - u>{}, t + 1);
     if (keep != ~0ull) {
       if (keep == 0) return;
       clear_rows<D, 256>(ring[u] + KE, keep, fresh(tid));
@@ -216,10 +209,10 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
         acc.o[d] = T::mfma(read_cols<T>(vp[d][0] + row * D, vp[d][1] + (row + 8) * D), pb[s >> 1][s & 1], acc.o[d]);
       }
   };
-  for (int t = t0; t < t1; t += RING)
-    static_for<RING>([&](auto u) {
-      if (t + u < t1) tile(u, t + u);
-    });
+  for (int t = t0; t < t1; t += 2) {
+    tile(integral_constant<int, 0>{}, t);
+    if (t + 1 < t1) tile(integral_constant<int, 1>{}, t + 1);
+  }
 
   const float l = both_halves_sum(acc.l);
   const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
@@ -232,6 +225,152 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
   store_tile<T, D>(acc.o, l == 0.f ? 0.f : 1.f / l, at(p.out, p.so, two.a), two.a_ok, at(p.out, p.so, two.b), two.b_ok,
                    lane);
   if (p.lse && row_ok && hw == 0) p.lse[row] = l == 0.f ? -INFINITY : (acc.m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Up to 32 rows at d 64: every wave takes the rows over blocks of 32 keys of its own,
+// every fourth, with slots of its own in LDS and no barrier before the waves' sums
+// are joined.  (With the tiles of cross_fwd_kernel one wave of four has the rows, and
+// its walk, not HBM, bounds the call: one token of 16 x 24 heads over up to 2,049 keys
+// with a bias, 143 MB, 40.0 us and so 28.4, a large copy's rate; 20 rows of 48 heads
+// over 100,000 keys 323 and 218.)  d 128 keeps cross_fwd_kernel: its slots would take
+// all of LDS, and it reads at 5.9 TB/s there.
+template <class T, int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void cross_few_kernel(const CrossParams p) {
+  constexpr int NW = 4, KE = 32 * D, CPR = D / 8, RPI = 64 / CPR;
+  static_assert(RPI == 8, "two loads a period of the row order");
+  __shared__ __attribute__((aligned(1024))) u16 ring[NW][2][2 * KE];   // per wave: slots [K | V]
+  __shared__ float sm[NW][32], sl[NW][32];
+  __shared__ uint16_t start[BIAS ? kMaxBucketSide : 1];
+  extern __shared__ __attribute__((aligned(16))) float bt[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+
+  const int n_rows = BIAS ? p.Lq : p.G * p.Lq;
+  const Place place = place_of<BIAS>(p, BIAS ? p.H : p.Hk, 1, p.splits, true);
+  const int unit = place.unit, split = place.split;
+  const int b = BIAS ? unit / p.H : unit / p.Hk, hk = BIAS ? (unit % p.H) / p.G : unit % p.Hk;
+  const int n = key_count(p, b), off = query_offset(p, n), far = BIAS ? p.rb.far : 0;
+  int kend = n;
+  if (BIAS && p.rb.causal) {
+    const int64_t last = (int64_t)n_rows + off;          // past the last visible key
+    kend = last < kend ? (last < 0 ? 0 : (int)last) : kend;
+  }
+  const int nb = (kend + 31) / 32;
+  const int b0 = (int)((int64_t)nb * split / p.splits) + wave, b1 = (int)((int64_t)nb * (split + 1) / p.splits);
+
+  const u16* kh = p.k + b * p.sk.b + hk * p.sk.h;
+  const u16* vh = p.v + b * p.sv.b + hk * p.sv.h;
+  uint32_t krel[2], vrel[2];                             // this lane's place in rows 0-7 and 8-15
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int row = 8 * j + lane / CPR, chunk = ((lane % CPR) ^ row_order<D>(row)) * 8;
+    krel[j] = (uint32_t)(row * p.sk.t + chunk) * 2u;
+    vrel[j] = (uint32_t)(row * p.sv.t + chunk) * 2u;
+  }
+  const uint32_t slots = lds_addr(ring[0][0]) + (uint32_t)wave * 8u * KE;
+  int mb = 1;
+  auto issue = [&](auto slot, int blk) {
+    const int left = n - blk * 32;
+    const u32x4 rk = TileLoad<D, 4, 32>::buffer(kh + (int64_t)blk * 32 * p.sk.t, p.sk.t, left);
+    const u32x4 rv = TileLoad<D, 4, 32>::buffer(vh + (int64_t)blk * 32 * p.sv.t, p.sv.t, left);
+    const uint32_t dst = slots + slot * 4 * KE;
+    static_for<4>([&](auto j) {
+      dma16<j * 1024>(rk, dst, krel[j & 1] + (uint32_t)(j / 2) * 32u * (uint32_t)p.sk.t, 0u);
+      dma16<j * 1024>(rv, dst + 2 * KE, vrel[j & 1] + (uint32_t)(j / 2) * 32u * (uint32_t)p.sv.t, 0u);
+    });
+    if (p.key_mask) mb = blk * 32 + c32 < n ? p.key_mask[b * p.mask_stride + blk * 32 + c32] : 1;
+  };
+  if (b0 < b1) issue(integral_constant<int, 0>{}, b0);
+  typename T::x8 qf[D / 16];
+  const TwoRows two = two_rows<BIAS>(p, unit, 0, n_rows, lane);
+  load_tile<T, D>(at(p.q, p.sq, two.a), two.a_ok, at(p.q, p.sq, two.b), two.b_ok, lane, qf);
+  if (BIAS) {
+    fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
+    __syncthreads();
+  }
+  Rows<T, D, 1> acc;
+  acc.init();
+  const int ra = row_lane<D>(c32, hw), ca = col_lane<D>(lane);
+  auto block = [&](auto u, int blk) {
+    // This block is there, and the other slot has been read.  (Both waits also keep
+    // the compiler from moving LDS accesses past them: there is no barrier here.)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    const uint32_t keep = (uint32_t)below(blk * 32, n) & (p.key_mask ? (uint32_t)__ballot(mb != 0) : ~0u);
+    u16* tK = ring[wave][u];
+    u16* tV = tK + KE;
+    if (blk + NW < b1) issue(integral_constant<int, 1 - u>{}, blk + NW);
+    if (keep != ~0u) {
+      if (keep == 0) return;
+      for (int c = lane; c < 32 * CPR; c += 64)
+        if (!((keep >> (c / CPR)) & 1)) *reinterpret_cast<u32x4*>(tV + c * 8) = u32x4{0, 0, 0, 0};
+    }
+    f32x16 x[1] = {f32x16{}};
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) x[0] = T::mfma(read_row<T>(tK + (ra ^ (8 * row_chunk(ks)))), qf[ks], x[0]);
+    if (BIAS) {
+      const float* at = bt + bias_from(blk * 32 - (31 + off), far) + far + kPad + 31 + 4 * hw - c32;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[0][e] = fmaf(x[0][e], p.sl2, at[8 * (e >> 2) + (e & 3)]);
+    }
+    if (keep != ~0u) {
+      const uint32_t mine = keep >> (4 * hw);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!((mine >> (8 * (e >> 2) + (e & 3))) & 1)) x[0][e] = -INFINITY;
+    }
+    typename T::x8 pb[1][2];
+    acc.weigh(x, BIAS ? 1.f : p.sl2, pb, blk == b0);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) acc.o[d] = T::mfma(read_col<T, D>(tV, ca, d, 16 * s), pb[0][s], acc.o[d]);
+  };
+  for (int blk = b0; blk < b1; blk += 2 * NW) {
+    block(integral_constant<int, 0>{}, blk);
+    if (blk + NW < b1) block(integral_constant<int, 1>{}, blk + NW);
+  }
+
+  // The waves' sums, through their slots: eight threads per row.
+  float* mine = reinterpret_cast<float*>(ring[wave][0]);
+  const float l = both_halves_sum(acc.l);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  store_tile_f32<D>(acc.o, mine + c32 * D, true, hw);
+  if (hw == 0) {
+    sm[wave][c32] = acc.m;
+    sl[wave][c32] = l;
+  }
+  __syncthreads();
+  const int r = tid >> 3, c = (tid & 7) * (D / 8);
+  if (r >= n_rows) return;
+  float m = sm[0][r], sum = 0.f, o[D / 8];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) m = vmax(m, sm[w][r]);
+#pragma unroll
+  for (int j = 0; j < D / 8; ++j) o[j] = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const float a = sm[w][r] == -INFINITY ? 0.f : fast_exp2(sm[w][r] - m);
+    const float* from = reinterpret_cast<const float*>(ring[w][0]) + r * D + c;
+    sum += a * sl[w][r];
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j) o[j] += a * from[j];
+  }
+  const RowOf ro = row_of<BIAS>(p, unit, r);
+  const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.Lq + ro.i;
+  if (p.splits > 1) {
+    const int64_t at = (int64_t)split * p.B * p.H * p.Lq + row;
+#pragma unroll
+    for (int j = 0; j < D / 8; j += 4)
+      *reinterpret_cast<f32x4*>(p.part_o + at * D + c + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
+    if (c == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(m, sum);
+    return;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  u32x4 v;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = T::pack(o[2 * j] * inv, o[2 * j + 1] * inv);
+  *reinterpret_cast<u32x4*>(at(p.out, p.so, ro) + c) = v;
+  if (p.lse && c == 0) p.lse[row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // Few keys, many rows: the keys and values of one (sample, key head) stay in
@@ -423,17 +562,15 @@ static hipError_t run_fwd(CrossParams p, bool bias, const CrossPlan& c, hipStrea
   }
   p.n_wg = (int)(units * ((rows + kRows - 1) / kRows) * p.splits);
   if (p.n_wg == 0) return hipSuccess;
-  // Few rows are a matter of bytes on their way: at d 64 three tiles per
-  // workgroup then, where one leaves room for a third workgroup per CU.
-  constexpr int DEEP = D == 64 ? 4 : 2;
   const uint32_t lds = bias ? bias_entries(p.rb.far) * 4 : 0;
-  if (rows <= 32) {
-    if (bias) hipLaunchKernelGGL((cross_fwd_kernel<T, D, true, DEEP>), dim3(p.n_wg), dim3(256), lds, st, p);
-    else hipLaunchKernelGGL((cross_fwd_kernel<T, D, false, DEEP>), dim3(p.n_wg), dim3(256), lds, st, p);
-  } else {
-    if (bias) hipLaunchKernelGGL((cross_fwd_kernel<T, D, true, 2>), dim3(p.n_wg), dim3(256), lds, st, p);
-    else hipLaunchKernelGGL((cross_fwd_kernel<T, D, false, 2>), dim3(p.n_wg), dim3(256), lds, st, p);
+  bool few = false;
+  if constexpr (D == 64) {
+    few = rows <= 32;
+    if (few && bias) hipLaunchKernelGGL((cross_few_kernel<T, D, true>), dim3(p.n_wg), dim3(256), lds, st, p);
+    if (few && !bias) hipLaunchKernelGGL((cross_few_kernel<T, D, false>), dim3(p.n_wg), dim3(256), lds, st, p);
   }
+  if (!few && bias) hipLaunchKernelGGL((cross_fwd_kernel<T, D, true>), dim3(p.n_wg), dim3(256), lds, st, p);
+  if (!few && !bias) hipLaunchKernelGGL((cross_fwd_kernel<T, D, false>), dim3(p.n_wg), dim3(256), lds, st, p);
   if (p.splits > 1) {
     const int64_t all = (int64_t)p.B * p.H * p.Lq;
     constexpr int NG = 1024 / D;                           // a workgroup's groups
