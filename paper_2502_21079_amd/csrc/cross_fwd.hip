@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) 
 // every fourth, with slots of its own in LDS and no barrier before the waves' sums
 // are joined.  (With the tiles of cross_fwd_kernel one wave of four has the rows, and
 // its walk, not HBM, bounds the call: one token of 16 x 24 heads over up to 2,049 keys
-// with a bias, 143 MB, 40.0 us and so 28.4, a large copy's rate; 20 rows of 48 heads
+// with a bias, 143 MB, 40.5 us and so 33.6, new inputs each call; 20 rows of 48 heads
 // over 100,000 keys 323 and 218.)  d 128 keeps cross_fwd_kernel: its slots would take
 // all of LDS, and it reads at 5.9 TB/s there.
 template <class T, int D, bool BIAS>
@@ -531,8 +531,7 @@ CrossPlan plan_fwd(const CrossParams& p, int D, bool bias) {
   // Keys are split where the row tiles alone leave CUs without work, into
   // ranges of no less than four tiles; below 1,024 keys the join's launch and
   // scratch cost more than the shorter walk gains (us a call, whole and split: one
-  // query over 512 keys, 32 heads, d 128 9 and 17.5, over 1,000 keys, 48 units,
-  // d 64 17.6 and 15.4).  And where all row tiles run at once but end apart, under
+  // query over 512 keys, 32 heads, d 128 9 and 17.5).  And where all row tiles run at once but end apart, under
   // an order mask or at d 64 with one workgroup on some CUs and two on others
   // (causal 12 x 4,095 of d 128 113 and 101, 6 x 6,199 of d 64 118 and 73,
   // 12 x 8,191 194 and 175, but 32 x 4,096, 1,024 tiles, 126 and 138, and
