@@ -24,7 +24,7 @@ struct RelBias {
   int table_f32;
   int side;                            // buckets of one direction
   int both;                            // keys after the query have buckets of their own
-  int far;                             // start[side - 1]
+  int far;                             // start[side - 1], at least 1
   int causal;
   int q_offset;                        // position of query 0 among the keys
   int at_end;                          // instead of q_offset: the queries end with their sample's keys

@@ -106,7 +106,11 @@ CrossParams params(const adaspa_cross_problem* p, const adaspa_rel_bias* r) {
     c.rb.table_f32 = r->table_fp32;
     c.rb.both = r->bidirectional != 0;
     c.rb.side = c.rb.both ? r->num_buckets / 2 : r->num_buckets;
-    c.rb.far = r->bucket_start[c.rb.side - 1];
+    // At least 1: the kernels take every distance from far on as one bucket on either
+    // side, and distance 0, the key at the query's own place, belongs to neither side
+    // alone (with one bucket a direction its value is the first direction's, and an
+    // order mask leaves it visible).
+    c.rb.far = r->bucket_start[c.rb.side - 1] > 1 ? r->bucket_start[c.rb.side - 1] : 1;
     c.rb.causal = r->causal != 0;
     c.rb.at_end = r->queries_at_end != 0;
     c.rb.q_offset = r->q_offset;
