@@ -524,14 +524,17 @@ struct TableSums {
       int d = start[m];
       const int d1 = last ? mid + 1 : start[m + 1];
       if (ahead && d == 0) d = 1;
+      // One direction: every key after the query is in the bucket of distance 0, the last
+      // that begins there.
+      const bool after = !p.rb.both && d == 0 && d1 > 0;
       float s = 0.f;
       for (d += lane; d < d1; d += 64) s += bt[ahead ? mid + d : mid - d];
-      if (!p.rb.both && u == 0)                           // one direction: every key after the query
+      if (after)
         for (int i = mid + 1 + lane; i < nd; i += 64) s += bt[i];
       s = wave_sum(s);
       if (last)
         for (int w = 0; w < NW; ++w) s += far_sum[ahead][w];
-      if (!p.rb.both && u == 0)
+      if (after)
         for (int w = 0; w < NW; ++w) s += far_sum[1][w];
       if (lane == 0) share[u] = s;
     }

@@ -1,5 +1,5 @@
 """Bucket plans that only the C ABI can name, on the GPU: one bucket a direction,
-whose last one begins at distance 0, against the plain 64-bit form with the
+whose last one begins at distance 0, and buckets that hold no distance, against the plain 64-bit form with the
 gradients, at offsets where a block of scores begins on the diagonal."""
 import ctypes
 
@@ -64,3 +64,12 @@ def test_one_bucket_a_direction(Lq, Lk, D, both, causal, offset, monkeypatch):
 def test_one_bucket_a_direction_with_masks_and_shared_heads(both, monkeypatch):
     for Lq, Lk in ((70, 65), (400, 290)):
         run(monkeypatch, 3, 4, 2, Lq, Lk, 64, HF, (0, 0) if both else (0,), both, not both, 1, "empty", "some")
+
+
+@pytest.mark.parametrize("both,causal", [(True, False), (False, False), (False, True)])
+@pytest.mark.parametrize("starts", [(0, 0), (0, 0, 0, 5), (0, 0, 3, 3, 3, 40, 40), (0, 1, 1)])
+@pytest.mark.parametrize("Lq,Lk", [(50, 60), (200, 210), (400, 500)])
+def test_buckets_without_a_distance(Lq, Lk, starts, both, causal, monkeypatch):
+    """Where several buckets begin at one distance the last of them holds it, and in
+    one direction the keys after the query, whose distance is 0."""
+    run(monkeypatch, 2, 2, 2, Lq, Lk, 64, BF, starts, both, causal, 7, "some")
