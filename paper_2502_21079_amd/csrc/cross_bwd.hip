@@ -44,6 +44,67 @@ constexpr float kShift = T::kHalf ? 14.f : 0.f;
 template <class T>
 constexpr float kUnshift = T::kHalf ? 1.f / 16384.f : 1.f;
 
+// fp16 ends at 65504 and has its 11 bits down to 2^-14 only, while dS goes with the
+// sizes of dO (a loss's mean over many elements, or its scale) and of v and with one
+// over the number of keys.  So in fp16 dS enters its products times a power of two, and
+// the sums are divided by it where they are stored: one per row for dq, one per key for
+// dk, which are lanes of the accumulators, so that a lane changes its own alone.  The
+// first values other than 0 bring their largest to [2^6, 2^7); a later one that would
+// pass 2^15 brings the factor, and what has been added up, down again.  All of it is
+// exact, and what still falls below fp16's smallest step is 2^-31 of the largest.
+// (Without it output gradients of 1e-4 over 200 to 9,000 keys left dq off by 2e-3 to
+// 9e-2 of its size, those of 1e-5 by up to 0.6, and some of 12,000 gave infinities.)
+// A maximum per pair of values and a product per value: training passes in fp16 take 3
+// to 5% longer (24 x 50,000 rows over 256 keys, d 128: 975 and 1,013 us; 12 x 4,095
+// tokens under an order mask 404 and 423).  bf16 has fp32's range and needs none.
+template <class T>
+struct Spread {
+  float up = T::kHalf ? 0x1p64f : 1.f, down = T::kHalf ? 0x1p-64f : 1.f;
+  __device__ __forceinline__ static bool over(float most) { return !(most <= 0x1p15f); }   // also NaN
+  // A new factor where `most`, the largest magnitude of this lane's values with the
+  // present one, or its other half's is over; returns what it changed by.
+  template <int N>
+  __device__ __forceinline__ float lower(float most, f32x16 (&acc)[N]) {
+    const float was = down;
+    most = both_halves_max(most);
+    if (over(most)) {
+      // 2^e <= most < 2^(e + 1), without the factor; the new one is 2^(6 - e), at most 2^64.
+      const uint32_t e = __float_as_uint(most * down) >> 23, b = 254 + 6 - e;
+      up = __uint_as_float((b < 191 ? b : 191) << 23);
+      down = 1.f / up;
+    }
+    const float by = up * was;
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[d][i] *= by;
+    return by;
+  }
+  // dS as it enters the product that is summed up in acc.
+  template <int N>
+  __device__ __forceinline__ void apply(f32x16& y, f32x16 (&acc)[N]) {
+    if constexpr (T::kHalf) {
+      float m[2] = {0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 16; e += 2)
+        m[(e >> 1) & 1] = vmax(m[(e >> 1) & 1], vmax(__builtin_fabsf(y[e]), __builtin_fabsf(y[e + 1])));
+      const float most = vmax(m[0], m[1]) * up;
+      if (__any(over(most))) lower(most, acc);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] *= up;
+    }
+  }
+  template <int N>
+  __device__ __forceinline__ void undo(f32x16 (&acc)[N]) const {
+    if constexpr (T::kHalf) {
+#pragma unroll
+      for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= down;
+    }
+  }
+};
+
 // What a launch of cross_dq_kernel does.  Where few rows share many keys the
 // keys are split, and delta, which needs them all, comes first, as it does for long
 // walks at d 128: DELTA leaves each
@@ -130,6 +191,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
   }
   if (BIAS) fill_bias<T, 256>(bt, start, p, unit % p.H, tid);
   float more = 0.f;                                        // sum of dS: what delta lacks (DELTA: of P dP)
+  Spread<T> spread;
 
   f32x16 acc[D / 32], pk[EXACT ? D / 32 : 1];
 #pragma unroll
@@ -245,6 +307,10 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
       for (int e = 0; e < 16; e += 2) {
         s0 += y[e];
         s1 += y[e + 1];
+      }
+      spread.apply(y, acc);
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
         if (SPLIT) {
           const uint2 v = split_pair<T>(y[e], y[e + 1]);
           w[e >> 3][(e & 7) >> 1] = v.x;
@@ -278,6 +344,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
     if (row_ok && hw == 0) p.part_d[split * all_rows + row] = more;
     return;
   }
+  spread.undo(acc);
   if (EXACT) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -381,6 +448,7 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
 #pragma unroll
     for (int e = 0; e < 16; ++e) from[e] = -delta;
     float more = 0.f;                                      // sum of dS: what delta lacks
+    Spread<T> spread;
     static_for<TWICE ? kTwiceBlocks<D> : 2 * KeptKeys<T, D>::TILES>([&](auto j) {
       constexpr int row0 = 32 * j;
       if (j / 2 >= keys.nt) return;
@@ -394,6 +462,10 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
       for (int e = 0; e < 16; e += 2) {
         s0 += y[e];
         s1 += y[e + 1];
+      }
+      spread.apply(y, acc);
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
         if (SPLIT) {
           const uint2 v = split_pair<T>(y[e], y[e + 1]);
           w[e >> 3][(e & 7) >> 1] = v.x;
@@ -422,6 +494,7 @@ __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_dq
     // weights add up to 1, so the sum of P dP is delta and the sum of dS.
     more = both_halves_sum(more);
     const float exact = delta + more;
+    spread.undo(acc);
     if (EXACT) {
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
@@ -620,6 +693,7 @@ __global__ __launch_bounds__(64 * (TINY ? kTinyWaves<D> : kSmallWaves<D>), D == 
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f32x16{};
+  Spread<T> spread_k;
 
   for (int g = 0; g < p.G; ++g) {
     const int h = hk * p.G + g;
@@ -686,22 +760,31 @@ __global__ __launch_bounds__(64 * (TINY ? kTinyWaves<D> : kSmallWaves<D>), D == 
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) acc[d] = pk[d] = f32x16{};
       float more = 0.f;
+      Spread<T> spread;
       for (int j = 0; j < last; ++j) {
         f32x16 x, y;
         block(j, x, y);
         const int ca = fresh(ca0);
         float s0 = 0.f, s1 = 0.f;
         u32x4 w[2], wp[2], wr[2];
+        auto put = [&](int e) {
+          const uint2 v = split_pair<T>(y[e], y[e + 1]);
+          w[e >> 3][(e & 7) >> 1] = v.x;
+          if (TINY) wr[e >> 3][(e & 7) >> 1] = v.y;
+          wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
+        };
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
           y[e] *= x[e];
           y[e + 1] *= x[e + 1];
           s0 += y[e];
           s1 += y[e + 1];
-          const uint2 v = split_pair<T>(y[e], y[e + 1]);
-          w[e >> 3][(e & 7) >> 1] = v.x;
-          if (TINY) wr[e >> 3][(e & 7) >> 1] = v.y;
-          wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
+          if (!T::kHalf) put(e);
+        }
+        if (T::kHalf) {
+          spread.apply(y, acc);
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) put(e);
         }
         more += s0 + s1;
 #pragma unroll
@@ -716,6 +799,7 @@ __global__ __launch_bounds__(64 * (TINY ? kTinyWaves<D> : kSmallWaves<D>), D == 
       }
       more = both_halves_sum(more);
       delta += more;
+      spread.undo(acc);
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -757,25 +841,33 @@ __global__ __launch_bounds__(64 * (TINY ? kTinyWaves<D> : kSmallWaves<D>), D == 
         const float* at = bt + bias_entries(far) - 1;     // a masked key's: -inf
         if (BIAS && key_ok) at = bt + bias_from(lo, far) + far + kPad + 31 + c32 - 4 * hw;
         u32x4 wp[2], ws[2], pr[2], sr[2];
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const int r = 8 * (e >> 2) + (e & 3);
-          const float a = fast_exp2(BIAS ? fmaf(x[e], p.sl2, at[-r]) : x[e] * p.sl2);
-          const float c = fast_exp2(BIAS ? fmaf(x[e + 1], p.sl2, at[-r - 1]) : x[e + 1] * p.sl2);
-          y[e] *= a;
-          y[e + 1] *= c;
+        auto put = [&](int e) {
           if (TINY) {
-            const uint2 v = split_pair<T>(a, c), t = split_pair<T>(y[e], y[e + 1]);
+            const uint2 v = split_pair<T>(x[e], x[e + 1]), t = split_pair<T>(y[e], y[e + 1]);
             wp[e >> 3][(e & 7) >> 1] = v.x;
             pr[e >> 3][(e & 7) >> 1] = v.y;
             ws[e >> 3][(e & 7) >> 1] = t.x;
             sr[e >> 3][(e & 7) >> 1] = t.y;
           } else {
-            wp[e >> 3][(e & 7) >> 1] = T::pack(a, c);
+            wp[e >> 3][(e & 7) >> 1] = T::pack(x[e], x[e + 1]);
             ws[e >> 3][(e & 7) >> 1] = T::pack(y[e], y[e + 1]);
           }
+        };
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const int r = 8 * (e >> 2) + (e & 3);
+          x[e] = fast_exp2(BIAS ? fmaf(x[e], p.sl2, at[-r]) : x[e] * p.sl2);
+          x[e + 1] = fast_exp2(BIAS ? fmaf(x[e + 1], p.sl2, at[-r - 1]) : x[e + 1] * p.sl2);
+          y[e] *= x[e];
+          y[e + 1] *= x[e + 1];
+          if (!T::kHalf) put(e);
         }
         if (BIAS) table.add(y, lo);
+        if (T::kHalf) {
+          spread_k.apply(y, dk);
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) put(e);
+        }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -799,7 +891,7 @@ __global__ __launch_bounds__(64 * (TINY ? kTinyWaves<D> : kSmallWaves<D>), D == 
   }
   const RowOf lower = {b, hk, rw + (lane & 15)}, upper = {b, hk, rw + (lane & 15) + 16};
   const bool a_ok = lower.i < p.Lk, b_ok = upper.i < p.Lk;
-  store_tile<T, D>(dk, p.scale, at(p.dk, p.sdk, lower), a_ok, at(p.dk, p.sdk, upper), b_ok, lane);
+  store_tile<T, D>(dk, p.scale * spread_k.down, at(p.dk, p.sdk, lower), a_ok, at(p.dk, p.sdk, upper), b_ok, lane);
   store_tile<T, D>(dv, 1.f, at(p.dv, p.sdv, lower), a_ok, at(p.dv, p.sdv, upper), b_ok, lane);
 }
 
@@ -909,6 +1001,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
     ++head;
   };
   f32x16 x, y;                                            // S and dP of the block in the second stage
+  Spread<T> spread;
   typename T::x8 pf[2], sf[2];                            // P and dS of the one in the third
 #pragma unroll
   for (int s = 0; s < 2; ++s) pf[s] = sf[s] = typename T::x8{};
@@ -1001,20 +1094,27 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
         pin(arg[2 * u + k]);
       }
     };
+    // fp16: y becomes dS with the factor that it enters its product with, or, where the
+    // table's gradient takes it too, without.
+    const float factor = kUnshift<T> * (BIAS ? 1.f : spread.up), later = BIAS ? spread.up : 1.f;
+    float most = 0.f;
     auto stage_ds = [&](int u) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         float v = arg[2 * u + k] * y[2 * u + k];
-        if (T::kHalf) v *= kUnshift<T>;
+        if (T::kHalf) v *= factor;
         pin(v);
         y[2 * u + k] = v;
       }
     };
     auto stage_pack = [&](int u) {
-      uint32_t a = T::pack(arg[2 * u], arg[2 * u + 1]), c = T::pack(y[2 * u], y[2 * u + 1]);
+      uint32_t a = T::pack(arg[2 * u], arg[2 * u + 1]), c;
+      if constexpr (T::kHalf && BIAS) c = T::pack(y[2 * u] * later, y[2 * u + 1] * later);
+      else c = T::pack(y[2 * u], y[2 * u + 1]);
       asm volatile("" : "+v"(a), "+v"(c));
       wp[u >> 2][u & 3] = a;
       ws[u >> 2][u & 3] = c;
+      if (T::kHalf) most = vmax(most, vmax(__builtin_fabsf(y[2 * u]), __builtin_fabsf(y[2 * u + 1])));
     };
     biases(0);
 #pragma unroll
@@ -1039,8 +1139,15 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
       stage_ds(7);
       stage_pack(7);
     }
-    if (BIAS) {
-      table.add(y, lo);
+    if (BIAS) table.add(y, lo);
+    if constexpr (T::kHalf) {
+      // The third stage has by now added up all that was packed with the factor so far.
+      most *= later;
+      if (__any(spread.over(most))) {
+        const float by = spread.lower(most, dk) * later;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) ws[u >> 2][u & 3] = T::pack(y[2 * u] * by, y[2 * u + 1] * by);
+      }
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -1117,6 +1224,7 @@ __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_ker
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f32x16{};
   }
+  spread.undo(dk);
   const bool ok = key < p.Lk;
   if (p.kv_splits > 1) {
     const int64_t all = (int64_t)p.B * p.Hk * p.Lk, at = (int64_t)unit * p.Lk + key;
