@@ -12,14 +12,25 @@ namespace adaspa {
 namespace {
 
 constexpr int kRows = 128;             // query rows of a workgroup: four waves of 32
-constexpr float kSumLimit = 256.f;     // a lane's weights of one tile add up to no more, or the reference moves
+// Weights against a row's maximum go down to e^-18 and less where one key stands out,
+// and fp16's smallest step is 2^-24.  So in fp16 they carry 2^kLift (the reference is
+// that far below the maximum), which leaves a factor of 32 up to kSumLimit: 100,000 keys
+// of unit-variance scores beside one at 16 whose value is 0 had an output off by 2.5e-3
+// of its size, and with one at 18 by 0.23; now by the roundings alone.  It is divided out
+// with the sum of the weights.  References move more often, which costs 2.5% under a bias
+// (12 x 8,191 tokens, d 64: 266 and 272 us) and nothing measurable without.
+template <class T>
+constexpr float kLift = T::kHalf ? 10.f : 0.f;
+// A lane's weights of one tile add up to no more, or the reference moves.
+template <class T>
+constexpr float kSumLimit = T::kHalf ? 32768.f : 256.f;
 
 // Running softmax of the rows of a wave (lane = row c32, the two half-waves
 // hold its keys between them).  Weights are taken against a reference m (log2
-// units): the maximum of a row's first tile, then whatever it is until the
+// units): the maximum of a row's first tile (less kLift), then whatever it is until the
 // weights of a tile, summed over one lane's 32 keys, pass kSumLimit; only then
 // is the maximum looked for, the reference moved there and the tile's weights
-// taken again.  So no weight exceeds 2^8, which fp16 holds too, and most tiles
+// taken again.  So no weight exceeds kSumLimit, which fp16 holds too, and most tiles
 // need neither a maximum nor a rescaled accumulator.
 template <class T, int D, int G = 2>
 struct Rows {
@@ -59,6 +70,7 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 16; e += 2) mt = vmax(mt, vmax(x[g][e], x[g][e + 1]));
     mt = both_halves_max(mt) * sl2;
+    if (T::kHalf) mt -= kLift<T>;
     const bool move = need && !(mt <= m);                  // also where it is NaN: the row becomes NaN
     const float a = move ? fast_exp2(m - mt) : 1.f;
     if (move) m = mt;
@@ -78,7 +90,7 @@ struct Rows {
     // moves is its own matter, so that its bits do not follow its neighbours.
     if (!first) {
       const float most = both_halves_max(s);
-      const bool need = !(most <= kSumLimit) || m == -INFINITY;
+      const bool need = !(most <= kSumLimit<T>) || m == -INFINITY;
       if (__any(need)) {
         raise(x, sl2, false, need);
         s = weights(x, sl2, pb);
