@@ -1329,8 +1329,13 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   // puts into it does not (sum_j P_ij k_j leans towards q_i): where no correction sum
   // follows (d 128), long walks have their delta formed first as well.  dq's error, in
   // units of its final rounding, with delta from the output: 1.3 at 2,245 keys, 3.6 at
-  // 49,836; 1.4 so, at one product in five more.
-  c.delta_first = !c.resident && (c.splits > 1 || (D == 128 && nt > (bias && p.rb.causal ? 64 : 32)));
+  // 49,836; 1.4 so, at one product in five more.  What counts is how many keys a row can
+  // see, the last row's where there is an order: 110 heads of 5 rows that end with 4,095
+  // keys, values with a mean of half their spread, 1.9 and 1.4.
+  int64_t seen = p.Lk;
+  if (bias && p.rb.causal && !p.rb.at_end) seen = (int64_t)p.Lq + p.rb.q_offset < seen ? (int64_t)p.Lq + p.rb.q_offset : seen;
+  constexpr int64_t kLong = 32 * 64;
+  c.delta_first = !c.resident && (c.splits > 1 || (D == 128 && seen > kLong));
   const int64_t ktiles = (int64_t)p.B * p.Hk * ((p.Lk + 32 * kDkvWaves - 1) / (32 * kDkvWaves));
   const int64_t items = (int64_t)p.G * ((p.Lq + 63) / 64);
   // Ranges of the queries: rounds of as many workgroups as run at a time (two
@@ -1355,7 +1360,8 @@ CrossPlan plan_bwd(const CrossParams& p, int D, bool bias) {
   c.part_o = off;
   if (c.splits > 1 && !c.resident) off += up256(c.splits * rows * D * 4);
   c.part_d = off;
-  if (c.delta_first) off += up256(c.splits * rows * 4);
+  // (Room by the keys alone: sizes are asked for without an offset.)
+  if (!c.resident && (c.splits > 1 || (D == 128 && p.Lk > kLong))) off += up256(c.splits * rows * 4);
   c.part_kv = off;
   if (c.kv_splits > 1) off += up256((int64_t)c.kv_splits * 2 * p.B * p.Hk * p.Lk * D * 4);
   c.part_t = off;
