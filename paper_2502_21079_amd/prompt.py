@@ -366,10 +366,10 @@ def rel_bias_attn_bwd_workspace(q_shape, k_shape, num_buckets: int, *, max_dista
 def _rows(t):
     """t itself where the kernels can read it as it lies, else a copy."""
     try:
-        _steps(t.shape, t.stride())
+        readable = _steps(t.shape, t.stride())[2] < 1 << 23 and t.data_ptr() % 16 == 0
     except AdaspaError:
-        return t.contiguous()
-    return t if t.data_ptr() % 16 == 0 else t.contiguous()
+        readable = False
+    return t if readable else t.clone(memory_format=torch.contiguous_format)
 
 
 class _CrossAttention(torch.autograd.Function):
