@@ -82,6 +82,8 @@ def _bias_ref(num_buckets, max_distance, bidirectional, causal, q_offset, table_
     starts = relative_bucket_starts(num_buckets, max_distance, bidirectional)
     arr = (ctypes.c_int32 * len(starts))(*starts)
     end = q_offset == "end"
+    if not end and not -(1 << 28) < q_offset < 1 << 28:
+        raise AdaspaError(f"q_offset must be below 2^28 in magnitude, got {q_offset}")
     r = _RelBias(num_buckets, int(bidirectional), ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32)), int(causal),
                  0 if end else q_offset, int(end), int(table_fp32))
     r._starts = arr                       # lives as long as the structure that points to it
@@ -109,6 +111,8 @@ def _plan(bwd, dtype, shapes, strides, outs, scale, mask_stride, bias) -> _Plan:
     like = ((qs, strides[0]), (qs, strides[0]), (ks, strides[1]), (ks, strides[2]))
     res = [_steps(n, _new_strides(n, t) if o is None else o) for (n, t), o in zip(like, outs)]
     B, H, Lq, D = qs
+    if max(*qs, *ks) >= 1 << 31:                 # the structure's numbers would wrap
+        raise AdaspaError(f"sizes must be below 2^31, got q {tuple(qs)} and k {tuple(ks)}")
     p = _CrossProblem(B, H, ks[1], Lq, ks[2], D, dtype, scale)
     for name, s in zip(("q", "k", "v", "dout", "out", "dq", "dk", "dv"), ins + [ins[0]] * (4 - len(ins)) + res):
         setattr(p, name + "_stride", _I64x3(*s))
