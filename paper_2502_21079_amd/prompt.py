@@ -69,18 +69,23 @@ def relative_bucket_starts(num_buckets: int, max_distance: int, bidirectional: b
     e = n // 2
     if max_distance <= e:
         raise AdaspaError(f"max_distance must be more than {e}, the distances with a bucket of their own")
-    starts, d = list(range(e)), e
-    for m in range(n - e):
-        while d ** (n - e) * e ** m < max_distance ** m * e ** (n - e):
-            d += 1
-        starts.append(d)
+    starts = list(range(e)) + [e]
+    for m in range(1, n - e):
+        low, high = starts[-1], max_distance          # the condition holds at max_distance
+        while low < high:
+            d = (low + high) // 2
+            if d ** (n - e) * e ** m < max_distance ** m * e ** (n - e):
+                low = d + 1
+            else:
+                high = d
+        starts.append(low)
     return tuple(starts)
 
 
 @functools.lru_cache(maxsize=512, typed=True)
 def _bias_ref(num_buckets, max_distance, bidirectional, causal, q_offset, table_fp32):
     starts = relative_bucket_starts(num_buckets, max_distance, bidirectional)
-    arr = (ctypes.c_int32 * len(starts))(*starts)
+    arr = (ctypes.c_int32 * len(starts))(*(min(d, (1 << 31) - 1) for d in starts))
     end = q_offset == "end"
     if not end and not -(1 << 28) < q_offset < 1 << 28:
         raise AdaspaError(f"q_offset must be below 2^28 in magnitude, got {q_offset}")
