@@ -358,7 +358,9 @@ adaspa_status adaspa_block_sparse_attn_noalloc(const adaspa_problem* prob, const
  * not overlap themselves.  H query heads share Hk key heads, H % Hk == 0, in
  * runs of H / Hk.  Lengths may be 0.  lse: fp32 [B, H, Lq], contiguous.
  * Scores, softmax, sums and gradients are accumulated in fp32; the weights and
- * dS are rounded to the inputs' type for the second products, results once.
+ * dS are rounded to the inputs' type for the second products, results once.  In
+ * fp16 both are rounded times powers of two that are taken back in fp32, so that
+ * neither many keys nor small or large output gradients cost bits.
  * The workspace is scratch, 256-byte aligned, of the size that the matching
  * _workspace call names (0: invalid arguments; 16: the call takes none, NULL
  * will do), not shared by calls that may overlap.  Ownership, streams, errors and
@@ -378,8 +380,8 @@ typedef struct {
 } adaspa_cross_problem;
 
 /* Buckets of the distance between a key and a query.  Bucket m of a direction
- * holds the distances [bucket_start[m], bucket_start[m+1]), the last one all
- * from its start on.  Bidirectional: the first half of the table is for keys
+ * holds the distances [bucket_start[m], bucket_start[m+1]) (none where the two are
+ * equal), the last one all from its start on.  Bidirectional: the first half of the table is for keys
  * at or before the query, the second for keys after it; otherwise keys after
  * the query have distance 0.  A value past -2.3e38 (log2(e) times it leaves fp32)
  * counts as minus infinity and hides its keys; where a row sees nothing but values of

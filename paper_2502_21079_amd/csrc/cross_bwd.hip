@@ -11,6 +11,13 @@
 // its delta is the exact one.  No sum is added
 // to memory by more than one workgroup: partial sums go to the workspace and
 // are added in a fixed order, so results are the same from call to call.
+//
+// P and dS enter the second products in the inputs' type, which is what the matrix
+// pipe takes; all sums are fp32.  Either is off by half a step of its own, so dv, dk and
+// dq are within 1.4 to 1.5 times their final rounding.  A value is split in two
+// (split_pair), at one product more, only where something else would come on top: delta
+// from the rounded output (dq at d 128), or chance among a few values (problems of up to
+// 64 queries and keys).  The table's gradient takes dS in fp32.
 #include "cross_tile.hpp"
 
 namespace adaspa {
@@ -28,7 +35,8 @@ constexpr bool kExactDq = D == 64;
 // At d 128 they do not, and delta's error can be as large as dS's rounding (162
 // rows over 2,245 keys: 1.6 times the final rounding together).  There dS goes
 // into the product as a sum of two values, its upper bits and what they leave, so
-// that delta's error and the final rounding are all that is left.
+// that delta's error and the final rounding are all that is left: 1.3 times the latter
+// for scores of unit variance, 1.7 for scores that spread three times as far.
 template <class T>
 __device__ __forceinline__ uint2 split_pair(float a, float b) {
   const uint32_t hi = T::pack(a, b);
@@ -106,8 +114,8 @@ struct Spread {
 };
 
 // What a launch of cross_dq_kernel does.  Where few rows share many keys the
-// keys are split, and delta, which needs them all, comes first, as it does for long
-// walks at d 128: DELTA leaves each
+// keys are split, and delta, which needs them all, comes first, as it does at d 128
+// wherever a row can see more than 2,048 keys: DELTA leaves each
 // range's sum of P dP, DQ adds these up and forms its range's dq.  (With delta
 // from the rounded output there, 25 queries over 18,266 keys had dq off by 5.4e-3
 // of its size where rounding dS and dq alone gives 2.4e-3.)
@@ -116,8 +124,8 @@ enum { WHOLE = 0, DELTA = 1, DQ = 2 };
 
 // dq of 128 query rows over one range of their keys: four waves of 32 rows, whose q
 // and dO stay in registers, tiles of 64 keys through two slots.  What bounds it: under
-// an order mask the last rows' walk (12 x 4,095 tokens at d 128: 167 us for 64 tiles
-// one after the other, the matrix pipe 26% busy); otherwise products and exponentials
+// an order mask the last rows' walk (12 x 4,095 tokens at d 128, fp16: 64 tiles one after
+// the other, 101 us for delta and 127 for dq, the matrix pipe 19 and 23% busy); otherwise products and exponentials
 // that two waves per SIMD overlap only in part.
 template <class T, int D, bool BIAS, int PASS>
 __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
@@ -368,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(const CrossParams p) {
 // rows over 128 keys 602 and 580, 48 x 20,000 over 100 479 and 474).  What bounds it
 // otherwise: the products beside the rows' way through memory (24 x 110,080 rows
 // over 256 keys, d 128: 2.7 GB, 565 us at a large copy's rate; four products, 692
-// GFLOP, 613 us at a large product's; 785 us, the matrix pipe 45% busy).
+// GFLOP, 600 us at a large product's; 772 us, the matrix pipe 45% busy).
 template <int D>
 constexpr int kTwiceBlocks = D == 64 ? 2 : 4;              // blocks of 32 keys that are walked twice
 template <class T, int D, bool TWICE>
@@ -620,9 +628,9 @@ struct TableSums {
 // rows for dq and delta, then, with the rows' statistics in LDS, 32 keys for dk
 // and dv.  A text encoder's prompts are of this size, and three launches one after
 // the other cost more than their work (8 x 24 heads x 226 tokens with a position
-// bias, d 64, forward and backward: 89 us with them, 51 so, 38 of them here).  What
+// bias, d 64, forward and backward: 89 us with them, 51 so, 36 of them here).  What
 // bounds it: one workgroup's walk, 16 blocks of 32 keys or rows one after the other
-// (waves wait 58% of their time; the vector units issue in 19% of it, the matrix pipe
+// (waves wait 57% of their time; the vector units issue in 19% of it, the matrix pipe
 // works in 8%); 192 such workgroups have a CU each.
 template <int D>
 constexpr int kSmallWaves = D == 64 ? 8 : 4;
@@ -904,9 +912,9 @@ __global__ __launch_bounds__(64 * (TINY ? kTinyWaves<D> : kSmallWaves<D>), D == 
 // pipe has work while the VALU does: at d 128 the accumulators leave one wave
 // per SIMD, and no other wave would fill the gaps.  Tiles stay in a ring of
 // three for it.  What bounds it: the matrix pipe at one wave's pace (24 heads x 110,080
-// rows over 256 keys, d 128: 692 GFLOP in 735 us, 942 TFLOP/s, the pipe 50% busy; a
-// large product reaches 1,136); under an order mask the first keys' walk, with the
-// table's sums by diagonal (12 x 4,095 tokens, d 128: 181 us).
+// rows over 256 keys, d 128: 692 GFLOP in 713 us, 971 TFLOP/s, the pipe 50% busy; a
+// large product reaches 1,154); under an order mask the first keys' walk, with the
+// table's sums by diagonal (12 x 4,095 tokens, d 128, fp16: 170 us).
 template <class T, int D, bool BIAS>
 __global__ __launch_bounds__(64 * kDkvWaves, D == 64 ? 2 : 1) void cross_dkv_kernel(const CrossParams p) {
   constexpr int NW = kDkvWaves, NT = 64 * NW, KE = 64 * D;

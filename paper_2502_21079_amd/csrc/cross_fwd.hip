@@ -32,6 +32,11 @@ constexpr float kSumLimit = T::kHalf ? 32768.f : 256.f;
 // is the maximum looked for, the reference moved there and the tile's weights
 // taken again.  So no weight exceeds kSumLimit, which fp16 holds too, and most tiles
 // need neither a maximum nor a rescaled accumulator.
+// They enter the product with V in the inputs' type, which is what the matrix pipe
+// takes, and their fp32 sum before that.  Each is off by half a step of its own, so the
+// output's error is between its final rounding alone (values with a mean) and 1.4 times
+// that (values without one, weights that hardly differ); two values per weight would
+// take the product twice.
 template <class T, int D, int G = 2>
 struct Rows {
   f32x16 o[D / 32];
@@ -107,8 +112,8 @@ struct Rows {
 // bounds it: one row over long keys at d 128, HBM (4 samples of 4 key heads, 17,664
 // keys: 145 MB in 24 us, and the join 4); many rows, products and weights that two
 // or three waves per SIMD overlap only in part (24 x 256 rows over 110,080 keys,
-// d 128: 346 GFLOP in 430 us, matrix pipe 45% busy and vector units 34%; 12 x 8,191
-// at d 64 with a bias: 206 GFLOP in 252 us, 38% and 62%).
+// d 128: 346 GFLOP in 399 us, matrix pipe 46% busy and vector units 34%; 12 x 8,191
+// at d 64 with a bias: 206 GFLOP in 237 us, 38% and 63%).
 template <class T, int D, bool BIAS>
 __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(const CrossParams p) {
   constexpr int NW = 4, KE = 64 * D;
@@ -389,8 +394,9 @@ __global__ __launch_bounds__(256, 2) void cross_few_kernel(const CrossParams p) 
 // LDS, and each wave walks row tiles on its own, without barriers; the next
 // tile's queries are loaded while one is worked on.  What bounds it: the rows' way
 // through memory beside products and weights (24 x 110,080 rows over 256 keys, d 128:
-// 1.37 GB and 346 GFLOP in 425 us, 285 and 305 at a large copy's and product's rates;
-// streaming the keys instead takes 577).
+// 1.37 GB and 346 GFLOP in 409 us, 287 and 300 at a large copy's and product's rates;
+// streaming the keys instead takes 577, and the first length that does not fit, 257,
+// 582).
 template <class T, int D>
 __global__ __launch_bounds__(64 * kKeepWaves, kKeepWaves / 4) void cross_keep_kernel(const CrossParams p) {
   constexpr int NW = kKeepWaves, QR = keep_rows(D);

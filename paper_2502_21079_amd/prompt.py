@@ -15,7 +15,8 @@ the HIP kernels of ``libadaspa.so`` (the C ABI is in ``include/adaspa.h``).
 
 Tensors are bf16 or fp16 views [B, heads, tokens, D] with D contiguous; other
 strides are the caller's (a projection's [B, tokens, heads, D] output is passed
-as its transpose).
+as its transpose).  ``scale`` multiplies the scores; None, and every value that is not
+above 0 in fp32, stands for 1 / sqrt(D).
 """
 from __future__ import annotations
 
@@ -266,7 +267,8 @@ def cross_attn(q, k, v, *, key_lens=None, key_mask=None, scale: Optional[float] 
     ``key_lens`` (int32 [B]) leaves sample b its first key_lens[b] keys,
     ``key_mask`` (bool or uint8 [B, Lk], 0 = masked) takes single ones away.  A
     row that sees no key gives 0 and an lse of -inf; what masked keys hold
-    takes no part.  ``workspace`` (at least :func:`cross_attn_workspace` bytes,
+    takes no part.  ``scale`` defaults to 1 / sqrt(D), which values up to 0 stand for
+    too.  ``workspace`` (at least :func:`cross_attn_workspace` bytes,
     any type) is allocated here when not given and needed: few query rows
     split their keys over workgroups."""
     return _forward(q, k, v, None, None, key_lens, key_mask, scale, out, lse, want_lse, workspace)
@@ -281,7 +283,8 @@ def rel_bias_attn(q, k, v, table, *, max_distance: int = 128, bidirectional: boo
     q's type.  When ``bidirectional`` the second half of its rows is for keys
     after the query; otherwise those count as distance 0.  Values of minus
     infinity, or past -2.3e38, hide their keys.  ``causal`` masks keys after the
-    query.  Query i stands at position i + ``q_offset`` among the keys; "end"
+    query.  ``scale`` as there: 0 is not "no scores" but 1 / sqrt(D).  Query i stands at
+    position i + ``q_offset`` among the keys; "end"
     puts a sample's queries at its last positions (decoding with a cache: one
     query over key_lens[b] keys).  Returns (out, lse)."""
     bias = _bias_key(q, k, table, max_distance, bidirectional, causal, q_offset)
