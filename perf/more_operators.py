@@ -241,7 +241,8 @@ def prepare(case, seed):
 def _scale(amax):
     """The least power of two of which 448 times is amax or more."""
     m, e = torch.frexp(amax.float())
-    return ((e - 9 + (m > 0.875).int()).clamp(min=-126) + 127 << 23).view(torch.float32)     # 2^e by its bits
+    e = torch.where(m == 0, -126, (e - 9 + (m > 0.875).int()).clamp(min=-126))
+    return (e + 127 << 23).view(torch.float32)                         # 2^e by its bits
 
 
 # --- the plain form ----------------------------------------------------------
@@ -424,7 +425,7 @@ def _nearest(x):
 
 def _least_scale(amax):
     """By trial: 2^e - 1 of which is too little."""
-    e = torch.floor(torch.log2(amax.clamp(min=2.0 ** -118) / 448.0))
+    e = torch.floor(torch.log2(amax.clamp(min=2.0 ** -140) / 448.0))
     e = torch.where(torch.exp2(e) * 448.0 < amax, e + 1, e)
     return torch.exp2(torch.where(torch.exp2(e - 1) * 448.0 >= amax, e - 1, e).clamp(min=-126))
 
