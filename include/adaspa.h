@@ -24,9 +24,10 @@
  * Beside it stand the attentions of the prompt side, with their gradients:
  * adaspa_cross_attn (video tokens over a text encoder's states) and
  * adaspa_rel_bias_attn (the encoder's own, with a learned relative position
- * bias).  Their tensors, strides and masks are described at their declarations;
- * what is said below of ownership, streams, errors and determinism holds for
- * them too.
+ * bias), rotary positions of queries and keys (adaspa_rotary), and a
+ * key/value cache in 8 bits with the attention that reads it (adaspa_cache_*).  Their
+ * tensors, strides and masks are described at their declarations; what is said
+ * below of ownership, streams, errors and determinism holds for them too.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -439,6 +440,119 @@ adaspa_status adaspa_rel_bias_attn_bwd(const adaspa_cross_problem* prob,
                                        const uint8_t* key_mask, const void* out, const float* lse,
                                        void* dq, void* dk, void* dv, void* dtable,
                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Rotary positions of queries and keys, in one call.  Pair i of a head, (u, w), becomes
+ *
+ *   magnitude * (u cos a - w sin a, u sin a + w cos a),   a = position * freq[i],
+ *
+ * the elements behind the `pairs` pairs are copied.  The position of token t of
+ * sample b is positions[b, t, axis] (without positions, on one axis: t) plus `offset`,
+ * plus offsets[b] where that is given; the pairs go by the axes in turn,
+ * axis_pairs[a] by axis a.  Angles are formed in fp64, products in fp32, results
+ * rounded once.
+ *
+ * Tensors are bf16 or fp16 views [B, heads, len, D] as those of the prompt side
+ * (D contiguous, strides multiples of 8, 16-byte aligned data), D a multiple of 8 up to
+ * 256.  kv_heads may be 0 (no keys: k and k_out are not read).  An output may
+ * be its input, at the same strides; other overlaps are not allowed, nor is an output
+ * that overlaps itself. */
+enum { ADASPA_ROTARY_HALF = 0,           /* pair i: elements i and i + pairs */
+       ADASPA_ROTARY_INTERLEAVED = 1 };  /* elements 2 i and 2 i + 1 */
+
+typedef struct {
+  int32_t batch, heads, kv_heads, len, head_dim;
+  int32_t dtype;                  /* ADASPA_BF16 / ADASPA_FP16 */
+  int32_t pairs;                  /* 1 to D / 2 */
+  int32_t layout;                 /* ADASPA_ROTARY_* */
+  int32_t axes;                   /* 1 to 4 */
+  int32_t axis_pairs[4];          /* pairs of each axis, `pairs` in all */
+  float magnitude;
+  const double* freq;             /* HOST array [pairs], radians per position */
+  /* (batch, head, token) strides in elements */
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
+  int64_t position_stride[2];     /* (batch, token) strides of positions; axes lie side by side */
+} adaspa_rotary_problem;
+
+/* positions: device int32 or NULL; offset: below 2^40 in magnitude; offsets:
+ * device int32 [B] or NULL. */
+adaspa_status adaspa_rotary(const adaspa_rotary_problem* prob, const void* q, const void* k,
+                            const int32_t* positions, int64_t offset, const int32_t* offsets,
+                            void* q_out, void* k_out, void* stream);
+
+/* Its backward pass: the results' gradients turned the other way, by the same
+ * magnitude.  The strides of q and k are those of the given gradients, q_out's and
+ * k_out's those of dq and dk. */
+adaspa_status adaspa_rotary_bwd(const adaspa_rotary_problem* prob, const void* dq_out,
+                                const void* dk_out, const int32_t* positions, int64_t offset,
+                                const int32_t* offsets, void* dq, void* dk, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * A key/value cache in 8 bits: a pool of pages, each `page` tokens of one sequence
+ * for every key head.
+ *
+ *   k        e4m3 (OCP) [pages, Hk, page, D]
+ *   v        e4m3 [pages, Hk, page / 16, D, 16]: sixteen tokens of a channel side by
+ *            side, the order in which attention takes them
+ *   k_scale, v_scale   fp32 [pages, Hk], powers of two (2^-126 to 2^127): a value is its
+ *            code times its page's and head's scale
+ *   page_table         int32 [B, max_pages] (row stride table_stride): the pages of each
+ *            sequence in order.  Entries outside [0, pages) name no page: what would be
+ *            written there is dropped, what would be read there is not there.
+ *
+ * All are device memory of the caller's; k and v 16-byte aligned.  New keys and values,
+ * queries and outputs are bf16 or fp16 views [B, heads, len, D] as those of the prompt
+ * side (D in {64, 128}, strides multiples of 8, 16-byte aligned data, outputs that do not
+ * overlap themselves).  H query heads share Hk key heads in runs; read and write have
+ * H = Hk.  Lengths are device int32 [B]. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  const int32_t* page_table;
+} adaspa_cache;
+
+typedef struct {
+  int32_t batch, heads, kv_heads;
+  int32_t len;                    /* new tokens, rows to read, or queries, of a sample */
+  int32_t head_dim, dtype;        /* ADASPA_BF16 / ADASPA_FP16 */
+  int32_t pages, page, max_pages; /* page in {16, 32, 64, 128}; max_pages * page < 2^28 */
+  int32_t causal;                 /* attention: a query sees the tokens up to its own place */
+  float softmax_scale;            /* attention: <= 0 selects 1/sqrt(D) */
+  int64_t table_stride;
+  /* (batch, head, token) strides in elements; attention reads the first two, read and
+   * write the last two */
+  int64_t q_stride[3], out_stride[3], k_stride[3], v_stride[3];
+} adaspa_cache_problem;
+
+/* Quantises k and v [B, Hk, len, D] into the pages behind the lens[b] tokens that a
+ * sequence has; new_lens (may be NULL: len) leaves sample b its first new_lens[b] tokens.
+ * A page and head gets the least power of two s >= 2^-126 with amax <= 448 s over the
+ * finite values, values the nearest code, ties to even; infinities and NaN are kept as NaN.  A
+ * page that holds tokens before lens[b] keeps the larger of its scale and the new tokens', and
+ * where that grows their codes are brought to it.  What lies behind the last token stays as it
+ * was.  A sample with lens[b] < 0 is left out.  No two sequences may write the same page. */
+adaspa_status adaspa_cache_write(const adaspa_cache_problem* prob, const adaspa_cache* cache,
+                                 const void* k, const void* v, const int32_t* lens,
+                                 const int32_t* new_lens, void* stream);
+
+/* Rows t of k and v [B, Hk, len, D] are the tokens at positions starts[b] + t (starts may be
+ * NULL: t) of sequences of lens[b] tokens; rows that are no token's are zeros. */
+adaspa_status adaspa_cache_read(const adaspa_cache_problem* prob, const adaspa_cache* cache,
+                                const int32_t* lens, const int32_t* starts, void* k, void* v,
+                                void* stream);
+
+/* Attention of q [B, H, len, D] over the first lens[b] tokens of each sequence (clamped to
+ * [0, max_pages * page]):
+ *   out_i = sum_j exp(S_ij - lse_i) v_j,  lse_i = log sum_j exp(S_ij),  S_ij = scale q_i . k_j
+ * The queries are their sequence's last tokens: sample b has q_lens[b] of them (NULL: len;
+ * clamped to [0, len]), query i stands at lens[b] - q_lens[b] + i and, with `causal`, sees no
+ * token behind that.  Rows without a token, and those from q_lens[b] on, give 0 and -inf.  lse:
+ * fp32 [B, H, len] or NULL.  The workspace is that of the prompt side's calls: scratch, 256-byte
+ * aligned, of the size that the _workspace call names. */
+size_t adaspa_cache_attn_workspace(const adaspa_cache_problem* prob);
+adaspa_status adaspa_cache_attn(const adaspa_cache_problem* prob, const adaspa_cache* cache,
+                                const void* q, const int32_t* lens, const int32_t* q_lens, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

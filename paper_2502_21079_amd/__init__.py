@@ -17,12 +17,14 @@ The three calls mirror the C ABI in ``include/adaspa.h``:
 
 The prompt side (cross attention to an encoder's states, attention with a
 learned relative position bias, each with its backward pass) is in
-``prompt.py`` and exported here.
+``prompt.py`` and exported here, rotary positions are in ``positions.py``, a
+key/value cache in 8 bits and attention over it in ``cache.py``.
 
 There is no CPU fallback: if the library is missing, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -39,7 +41,9 @@ __all__ = ["dense_attn_lse", "dense_attn_workspace", "block_search", "block_spar
            "single_pass_online_search", "single_pass_online_search_workspace",
            "single_pass_online_search_min_workspace", "cross_attn", "cross_attn_workspace", "cross_attn_bwd",
            "cross_attn_bwd_workspace", "cross_attention", "rel_bias_attn", "rel_bias_attn_workspace",
-           "rel_bias_attn_bwd", "rel_bias_attn_bwd_workspace", "rel_bias_attention", "relative_bucket_starts"]
+           "rel_bias_attn_bwd", "rel_bias_attn_bwd_workspace", "rel_bias_attention", "relative_bucket_starts",
+           "rotary", "rotary_bwd", "rotary_embedding", "rotary_frequencies", "rotary_magnitude", "KVCache", "kv_cache",
+           "cache_write", "cache_read", "cache_attn", "cache_attn_workspace"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libadaspa.so"
@@ -52,7 +56,9 @@ EXPORTED_SYMBOLS = ("adaspa_status_string", "adaspa_dense_attn_workspace", "adas
                     "adaspa_single_pass_online_search_min_workspace", "adaspa_single_pass_online_search",
                     "adaspa_cross_attn_workspace", "adaspa_cross_attn", "adaspa_cross_attn_bwd_workspace",
                     "adaspa_cross_attn_bwd", "adaspa_rel_bias_attn_workspace", "adaspa_rel_bias_attn",
-                    "adaspa_rel_bias_attn_bwd_workspace", "adaspa_rel_bias_attn_bwd")
+                    "adaspa_rel_bias_attn_bwd_workspace", "adaspa_rel_bias_attn_bwd", "adaspa_rotary",
+                    "adaspa_rotary_bwd", "adaspa_cache_write", "adaspa_cache_read", "adaspa_cache_attn_workspace",
+                    "adaspa_cache_attn")
 
 SELECT_TOPK = 0
 SELECT_COVERAGE = 1
@@ -128,7 +134,8 @@ def load_library():
     lib.adaspa_block_sparse_attn_noalloc.restype = ctypes.c_int
     lib.adaspa_block_sparse_attn_noalloc.argtypes = [P, vp, vp, vp, i32p, i32p, ctypes.c_int64,
                                                      vp, f32p, vp]
-    _prompt._declare(lib)
+    for part in (_prompt, _positions, _cache):
+        part._declare(lib)
     _lib = lib
     return lib
 
@@ -152,6 +159,14 @@ def _stream(device):
     if _raw_stream is not None and device.index is not None:
         return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
+
+
+# A launch goes to the current device: the calls below make that the tensors' own.
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _on(index: int):
+    return _SAME_DEVICE if torch.cuda.current_device() == index else torch.cuda.device(index)
 
 
 # The argument structures of a call are made once per set of values (sizes and
@@ -539,7 +554,10 @@ def block_sparse_attn_noalloc(q, k, v, row_ptr, col_idx, *, block: int, out, lse
 
 
 
-from . import prompt as _prompt  # noqa: E402  (it uses the helpers above)
+# They use the helpers above.
+from . import cache as _cache, positions as _positions, prompt as _prompt  # noqa: E402
+from .cache import KVCache, cache_attn, cache_attn_workspace, cache_read, cache_write, kv_cache  # noqa: E402
 from .prompt import (cross_attention, cross_attn, cross_attn_bwd, cross_attn_bwd_workspace,  # noqa: E402
                      cross_attn_workspace, rel_bias_attention, rel_bias_attn, rel_bias_attn_bwd,
                      rel_bias_attn_bwd_workspace, rel_bias_attn_workspace, relative_bucket_starts)
+from .positions import rotary, rotary_bwd, rotary_embedding, rotary_frequencies, rotary_magnitude  # noqa: E402

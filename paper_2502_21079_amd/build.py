@@ -17,7 +17,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libadaspa.so")
-SOURCES = ["api.hip", "attn.hip", "select.hip", "cross_api.hip", "cross_fwd.hip", "cross_bwd.hip"]
+SOURCES = ["api.hip", "attn.hip", "select.hip", "cross_api.hip", "cross_fwd.hip", "cross_bwd.hip",
+           "rotary_api.hip", "rotary.hip", "cache_api.hip", "cache_rw.hip", "cache_attn.hip"]
 ARCH = os.environ.get("ADASPA_OFFLOAD_ARCH", "gfx950")
 
 FLAGS = [

@@ -1,0 +1,570 @@
+// Attention over a key/value cache in 8 bits (gfx950).
+//
+//   out_i = sum_j exp(S_ij - lse_i) v_j,  lse_i = log sum_j exp(S_ij),  S_ij = scale q_i . k_j
+//
+// over a sequence's keys j < n and, with an order, j <= n - queries + i; a row
+// without any gives 0 and -inf.  Query heads that share a key head are rows of
+// one problem: row r of a key head is query r / G of head hk G + r % G, so that
+// neighbouring rows see almost the same keys.
+//
+// Keys enter the first product as codes, which 16 bits hold exactly, and their
+// scale is part of the factor that the scores get anyway.  Values enter the second
+// as code times scale in bf16, whose exponents hold every scale; so do the
+// weights, with fp16 inputs as two values each (the second what the first leaves),
+// so that no output type loses to their rounding.
+#include "cache_tile.hpp"
+
+namespace adaspa {
+
+namespace {
+
+// Weights are taken against a reference m (log2 units) that moves to a row's
+// maximum only where a score is further above it: no weight exceeds 2^8, and most
+// tiles rescale nothing.
+constexpr float kAbove = 8.f;
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Two weights as bf16, and what that leaves, as bf16 again.
+__device__ __forceinline__ uint32_t split2(float a, float b, uint32_t& rest) {
+  const uint32_t hi = BF16::pack(a, b);
+  float ha, hb;
+  BF16::unpack(hi, ha, hb);
+  rest = BF16::pack(a - ha, b - hb);
+  return hi;
+}
+
+// The query and head of a key head's row.
+__device__ __forceinline__ RowOf cache_row(const CacheParams& p, int unit, int r) {
+  RowOf o;
+  o.b = unit / p.Hk;
+  o.i = r / p.G;
+  o.h = unit % p.Hk * p.G + (r - o.i * p.G);
+  return o;
+}
+
+// Keys and queries of sequence b.
+struct Lens {
+  int n, q;                                              // keys; queries, the last q of the positions
+  __device__ __forceinline__ Lens(const CacheParams& p, int b) {
+    n = clamp_len(__builtin_amdgcn_readfirstlane(p.lens[b]), (int)((int64_t)p.c.max_pages * p.c.page));
+    q = p.new_lens ? clamp_len(__builtin_amdgcn_readfirstlane(p.new_lens[b]), p.L) : p.L;
+  }
+  // How many keys query i sees.
+  __device__ __forceinline__ int seen(const CacheParams& p, int i) const {
+    if (i >= q) return 0;
+    if (!p.causal) return n;
+    const int m = n - q + i + 1;
+    return m < 0 ? 0 : m;
+  }
+};
+
+}  // namespace
+
+// Up to 16 NQ rows of a key head.  Every wave walks blocks of 64 keys of its own,
+// from memory to registers in the places that the matrix instructions want: rows of
+// the first product are keys ordered so that a lane's scores are those of 16
+// neighbouring tokens, whose values of one channel lie side by side in the cache.
+// So neither operand passes through LDS, and a block's loads are 16 bytes a lane.
+// The waves' sums are joined in LDS, ranges of the keys by cache_join_kernel.
+template <class T, int D, int NQ>
+__global__ __launch_bounds__(256, 2) void cache_few_kernel(const CacheParams p) {
+  constexpr int NW = 4, DT = D / 16, KJ = D / 64;          // channel tiles; 16-byte pieces of a key a lane
+  __shared__ __attribute__((aligned(16))) float so[NW][NQ * 16 * D];
+  __shared__ float sm[NW][NQ * 16], sl[NW][NQ * 16];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int g = lane >> 4, c16 = lane & 15;
+  const int unit = blockIdx.x / p.chunks, range = blockIdx.x % p.chunks;
+  const int b = unit / p.Hk, hk = unit % p.Hk, n_rows = p.G * p.L;
+  const Lens len(p, b);
+  const int k0 = range * p.chunk, k1 = len.n - k0 < p.chunk ? len.n : k0 + p.chunk;   // keys of this range
+  if (k0 >= len.n && range > 0) return;
+
+  typename T::x8 qf[NQ][KJ][2];
+  int seen[NQ];
+  float m[NQ], l[NQ];
+  f32x4 o[NQ][DT];
+#pragma unroll
+  for (int r = 0; r < NQ; ++r) {
+    const bool ok = r * 16 + c16 < n_rows;
+    const RowOf ro = cache_row(p, unit, ok ? r * 16 + c16 : 0);
+    const u16* q = at(p.q, p.sq, ro);
+    seen[r] = ok ? len.seen(p, ro.i) : 0;
+#pragma unroll
+    for (int j = 0; j < KJ; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 w = {0, 0, 0, 0};
+        if (ok) w = *reinterpret_cast<const u32x4*>(q + 64 * j + 16 * g + 8 * h);
+        qf[r][j][h] = __builtin_bit_cast(typename T::x8, w);
+      }
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[r][d] = f32x4{};
+  }
+  const int fewest = len.q < p.L ? 0 : len.seen(p, 0);     // keys that every row sees
+  const int shift = 31 - __builtin_clz(p.c.page);
+
+  struct Block {
+    u32x4 k[4][KJ], v[DT];
+    float ks, vs;
+    int live;                                              // tokens of this lane's 16 that are there
+  };
+  auto load = [&](Block& x, int k) {
+    // Keys: 16 rows of an instruction are tokens 4 t + c16 % 4 of sixteen number c16 / 4.
+    const int kp = k + (c16 >> 2) * 16, vp = k + g * 16;
+    const int ki = kp < len.n ? page_at(p.c, b, kp >> shift) : -1, vi = vp < len.n ? page_at(p.c, b, vp >> shift) : -1;
+    const int64_t ka = (int64_t)(ki < 0 ? 0 : ki) * p.Hk + hk, va = (int64_t)(vi < 0 ? 0 : vi) * p.Hk + hk;
+    const int mask = p.c.page - 1;
+    const uint8_t* kt = p.c.k + (ka << shift) * D + ((kp & mask) + (c16 & 3)) * D + 16 * g;
+    const uint8_t* vt = p.c.v + (va << shift) * D + (vp & mask) * D + 16 * c16;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) {
+        x.k[t][j] = u32x4{0, 0, 0, 0};
+        if (ki >= 0) x.k[t][j] = *reinterpret_cast<const u32x4*>(kt + 4 * t * D + 64 * j);
+      }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      x.v[d] = u32x4{0, 0, 0, 0};
+      if (vi >= 0) x.v[d] = *reinterpret_cast<const u32x4*>(vt + 256 * d);
+    }
+    x.ks = x.vs = 1.f;
+    if (vi >= 0) {
+      x.ks = p.c.k_scale[va];
+      x.vs = p.c.v_scale[va];
+    }
+    const int left = len.n - vp;
+    x.live = vi < 0 ? 0 : (left < 16 ? left : 16);
+  };
+  auto work = [&](Block& x, int k) {
+    const bool edge = k + 64 > fewest || __any(x.live < 16);
+    if (edge) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.v[d][i] &= first_bytes(x.live - 4 * i);
+    }
+    f32x4 s[NQ][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) s[r][t] = f32x4{};
+#pragma unroll
+      for (int j = 0; j < KJ; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const typename T::x8 kf = decode8<T>(x.k[t][j][2 * h], x.k[t][j][2 * h + 1], 1.f);
+#pragma unroll
+          for (int r = 0; r < NQ; ++r) s[r][t] = mfma16(kf, qf[r][j][h], s[r][t]);
+        }
+    }
+    const float a = x.ks * p.sl2;
+    bf16x8 w[NQ][2], rest[NQ][2];
+#pragma unroll
+    for (int r = 0; r < NQ; ++r) {
+      float top = -INFINITY;
+      const int see = seen[r] - (k + 16 * g) < x.live ? seen[r] - (k + 16 * g) : x.live;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[r][t][e] *= a;
+          if (edge && 4 * t + e >= see) s[r][t][e] = -INFINITY;
+          top = vmax(top, s[r][t][e]);
+        }
+      const auto u = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = both_halves_max(vmax(__uint_as_float(u[0]), __uint_as_float(u[1])));
+      if (__any(!(top <= m[r] + kAbove))) {                // NaN too: the row becomes NaN
+        const float to = top <= m[r] ? m[r] : top;
+        const float by = to == -INFINITY ? 1.f : fast_exp2(m[r] - to);
+        m[r] = to;
+        l[r] *= by;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[r][d][e] *= by;
+      }
+      const float ref = m[r] == -INFINITY ? 0.f : m[r];
+      float sum = 0.f;
+      u32x4 hi[2], lo[2];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const float c = fast_exp2(s[r][t][e] - ref), d = fast_exp2(s[r][t][e + 1] - ref);
+          sum += c + d;
+          uint32_t left = 0;
+          hi[t >> 1][(t & 1) * 2 + e / 2] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
+          lo[t >> 1][(t & 1) * 2 + e / 2] = left;
+        }
+      l[r] += sum;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        w[r][h] = __builtin_bit_cast(bf16x8, hi[h]);
+        rest[r][h] = __builtin_bit_cast(bf16x8, lo[h]);
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 vf = decode8<BF16>(x.v[d][2 * h], x.v[d][2 * h + 1], x.vs);
+#pragma unroll
+        for (int r = 0; r < NQ; ++r) {
+          o[r][d] = mfma16(vf, w[r][h], o[r][d]);
+          if (T::kHalf) o[r][d] = mfma16(vf, rest[r][h], o[r][d]);
+        }
+      }
+  };
+  Block x[2];
+  int k = k0 + wave * 64;
+  if (k < k1) load(x[0], k);
+  for (; k < k1; k += 2 * 64 * NW) {
+    if (k + 64 * NW < k1) load(x[1], k + 64 * NW);
+    work(x[0], k);
+    if (k + 64 * NW >= k1) break;
+    if (k + 2 * 64 * NW < k1) load(x[0], k + 2 * 64 * NW);
+    work(x[1], k + 64 * NW);
+  }
+
+  // The waves' sums: lane c16 of a group of 16 has row c16, channels 16 d + 4 g on.
+#pragma unroll
+  for (int r = 0; r < NQ; ++r) {
+    const auto u = __builtin_amdgcn_permlane16_swap(__float_as_uint(l[r]), __float_as_uint(l[r]), false, false);
+    l[r] = both_halves_sum(__uint_as_float(u[0]) + __uint_as_float(u[1]));
+    if (g == 0) {
+      sm[wave][r * 16 + c16] = m[r];
+      sl[wave][r * 16 + c16] = l[r];
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(&so[wave][(r * 16 + c16) * D + 16 * d + 4 * g]) = o[r][d];
+  }
+  __syncthreads();
+  constexpr int TPR = D / 4;
+  for (int i = tid; i < n_rows * TPR; i += 256) {
+    const int r = i / TPR, c = i % TPR * 4;
+    float top = sm[0][r], sum = 0.f;
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = sm[w][r] <= top ? top : sm[w][r];
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float by = sm[w][r] == -INFINITY ? 0.f : fast_exp2(sm[w][r] - top);
+      const f32x4 y = *reinterpret_cast<const f32x4*>(&so[w][r * D + c]);
+      sum += by * sl[w][r];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += by * y[e];
+    }
+    const RowOf ro = cache_row(p, unit, r);
+    const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.L + ro.i;
+    if (p.chunks > 1) {
+      const int64_t to = (int64_t)range * p.B * p.H * p.L + row;
+      *reinterpret_cast<f32x4*>(p.part_o + to * D + c) = v;
+      if (c == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * to) = make_float2(top, sum);
+      continue;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    *reinterpret_cast<uint2*>(at(p.out, p.so, ro) + c) =
+        make_uint2(T::pack(v[0] * inv, v[1] * inv), T::pack(v[2] * inv, v[3] * inv));
+    if (p.lse && c == 0) p.lse[row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  }
+}
+
+// Many rows: 128 of a key head, four waves of 32, over tiles of 64 keys that are
+// turned into 16 bits once for all of them on their way to LDS: raw codes of the
+// next tile are loaded into registers while this one is worked on.
+//   keys: 16-byte pieces (8 channels) of the tile's 64 keys side by side, a piece
+//   and one further apart each time, so that neither way meets a bank twice;
+//   values: pieces of 8 tokens of a channel, in the order of the weights' places
+//   in the second product, channels side by side.
+template <class T, int D>
+__global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p) {
+  constexpr int KP = 64 * 8 + 8;                           // elements from a piece of the keys to the next
+  constexpr int PER = D / 64;                              // 16-byte loads of a thread, for keys and for values
+  __shared__ __attribute__((aligned(16))) u16 sk[2][D / 8 * KP];
+  __shared__ __attribute__((aligned(16))) u16 sv[2][64 * D];
+  __shared__ __attribute__((aligned(16))) float scale[2][4];   // of the keys' sixteens; below 0: not there
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hw = lane >> 5, c32 = lane & 31;
+  const int n_rows = p.G * p.L, n_rt = (n_rows + 127) / 128;
+  const int lid = xcd_remap(blockIdx.x, p.n_wg);
+  const int unit = lid / (n_rt * p.chunks), range = lid / n_rt % p.chunks, rt = n_rt - 1 - lid % n_rt;
+  const int b = unit / p.Hk, hk = unit % p.Hk;
+  const Lens len(p, b);
+  if (range > 0 && range * p.chunk >= len.n) return;
+  const int rw = rt * 128 + wave * 32, r = rw + c32;
+  const RowOf ro = cache_row(p, unit, r < n_rows ? r : 0);
+  const int seen = r < n_rows ? len.seen(p, ro.i) : 0;
+  // The most keys that a row of this tile, and of this wave, sees; the fewest of this wave.
+  const int last = rt * 128 + 127 < n_rows ? rt * 128 + 127 : n_rows - 1;
+  auto most_of = [&](int from, int to) {                   // rows [from, to]
+    const int i = to / p.G < len.q ? to / p.G : len.q - 1;
+    return from > to || i < from / p.G ? 0 : len.seen(p, i);
+  };
+  const int end = most_of(rt * 128, last);
+  const int rl = rw + 31 < n_rows ? rw + 31 : n_rows - 1;
+  const int most = most_of(rw, rl);
+  const int fewest = rw + 31 < n_rows && rl / p.G < len.q ? len.seen(p, rw / p.G) : 0;
+  const int k0 = range * p.chunk, k1 = end - k0 < p.chunk ? end : k0 + p.chunk;
+  const int nt = k1 > k0 ? (k1 - k0 + 63) / 64 : 0;
+
+  const int shift = 31 - __builtin_clz(p.c.page), mask = p.c.page - 1;
+  // Thread's piece j is of sixteen number (tid + 256 j) / D of the tile, for keys and values.
+  u32x4 rk[PER], rv[PER];
+  float ks[PER], vs[PER];
+  int live[PER];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int piece = tid + 256 * j, pos = k0 + t * 64 + __builtin_amdgcn_readfirstlane(piece / D) * 16;
+      const int id = pos < len.n ? page_at(p.c, b, pos >> shift) : -1;
+      rk[j] = rv[j] = u32x4{0, 0, 0, 0};
+      ks[j] = -1.f;
+      vs[j] = 1.f;
+      live[j] = 0;
+      if (id < 0) continue;
+      const int64_t a = (int64_t)id * p.Hk + hk, base = (a << shift) * D + (pos & mask) * D + piece % D * 16;
+      rk[j] = *reinterpret_cast<const u32x4*>(p.c.k + base);
+      rv[j] = *reinterpret_cast<const u32x4*>(p.c.v + base);
+      ks[j] = p.c.k_scale[a];
+      vs[j] = p.c.v_scale[a];
+      live[j] = len.n - pos < 16 ? len.n - pos : 16;
+    }
+  };
+  auto put = [&](int slot) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int piece = tid + 256 * j, six = piece / D, in = piece % D;
+      const int key = six * 16 + in / (D / 16), c = in % (D / 16) * 2;
+      u16* k = sk[slot] + c * KP + key * 8;
+      *reinterpret_cast<typename T::x8*>(k) = decode8<T>(rk[j][0], rk[j][1], 1.f);
+      *reinterpret_cast<typename T::x8*>(k + KP) = decode8<T>(rk[j][2], rk[j][3], 1.f);
+      if (live[j] < 16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rv[j][i] &= first_bytes(live[j] - 4 * i);
+      }
+      u16* v = sv[slot] + (six * 2 * D + in) * 8;
+      *reinterpret_cast<bf16x8*>(v) = decode8<BF16>(rv[j][0], rv[j][2], vs[j]);
+      *reinterpret_cast<bf16x8*>(v + D * 8) = decode8<BF16>(rv[j][1], rv[j][3], vs[j]);
+      if (in == 0) scale[slot][six] = ks[j];
+    }
+  };
+
+  typename T::x8 qf[D / 16];
+  auto two = [&](int ln) {
+    TwoRows w;
+    const int x = rw + (ln & 15);
+    w.a_ok = x < n_rows;
+    w.b_ok = x + 16 < n_rows;
+    w.a = cache_row(p, unit, w.a_ok ? x : 0);
+    w.b = cache_row(p, unit, w.b_ok ? x + 16 : 0);
+    return w;
+  };
+  if (nt > 0) fetch(0);
+  {
+    const TwoRows w = two(lane);
+    load_tile<T, D>(at(p.q, p.sq, w.a), w.a_ok, at(p.q, p.sq, w.b), w.b_ok, lane, qf);
+  }
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
+  float m = -INFINITY, l = 0.f;
+  if (nt > 0) put(0);
+  __syncthreads();
+
+  for (int t = 0; t < nt; ++t) {
+    const int slot = t & 1, key0 = k0 + t * 64;
+    if (t + 1 < nt) fetch(t + 1);
+    if (key0 < most) {
+      const f32x4 a4 = *reinterpret_cast<const f32x4*>(scale[slot]);
+      f32x16 x[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        x[h] = f32x16{};
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+          x[h] = T::mfma(*reinterpret_cast<const typename T::x8*>(sk[slot] + (row_chunk(s) + 2 * hw) * KP +
+                                                                  (32 * h + c32) * 8), qf[s], x[h]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[h][e] *= a4[2 * h + (e >> 3)] * p.sl2;
+      const bool gone = !(a4[0] >= 0.f && a4[1] >= 0.f && a4[2] >= 0.f && a4[3] >= 0.f);
+      if (key0 + 64 > fewest || gone) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (key0 + 32 * h + 8 * (e >> 2) + 4 * hw + (e & 3) >= seen || a4[2 * h + (e >> 3)] < 0.f) x[h][e] = -INFINITY;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = vmax(top, x[h][e]);
+      top = both_halves_max(top);
+      if (__any(!(top <= m + kAbove))) {
+        const float to = top <= m ? m : top;
+        const float by = to == -INFINITY ? 1.f : fast_exp2(m - to);
+        m = to;
+        l *= by;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] *= by;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      float s0 = 0.f, s1 = 0.f;
+      bf16x8 w[4], rest[4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 hi[2], lo[2];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const float c = fast_exp2(x[h][e] - ref), d = fast_exp2(x[h][e + 1] - ref);
+          s0 += c;
+          s1 += d;
+          uint32_t left = 0;
+          hi[e >> 3][(e & 7) >> 1] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
+          lo[e >> 3][(e & 7) >> 1] = left;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          w[2 * h + i] = __builtin_bit_cast(bf16x8, hi[i]);
+          rest[2 * h + i] = __builtin_bit_cast(bf16x8, lo[i]);
+        }
+      }
+      l += s0 + s1;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sv[slot] + ((2 * s + hw) * D + 32 * d + c32) * 8);
+          o[d] = mfma32(vf, w[s], o[d]);
+          if (T::kHalf) o[d] = mfma32(vf, rest[s], o[d]);
+        }
+    }
+    if (t + 1 < nt) put(1 - slot);
+    __syncthreads();
+  }
+
+  l = both_halves_sum(l);
+  const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.L + ro.i;
+  const bool ok = r < n_rows;
+  if (p.chunks > 1) {
+    const int64_t to = (int64_t)range * p.B * p.H * p.L + row;
+    store_tile_f32<D>(o, p.part_o + to * D, ok, hw);
+    if (ok && hw == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * to) = make_float2(m, l);
+    return;
+  }
+  const TwoRows w = two(lane);
+  store_tile<T, D>(o, l == 0.f ? 0.f : 1.f / l, at(p.out, p.so, w.a), w.a_ok, at(p.out, p.so, w.b), w.b_ok, lane);
+  if (p.lse && ok && hw == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Joins the ranges of a sequence's keys: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s,
+// in a fixed order.  A workgroup per row, NG groups of D / 4 threads that take every
+// NG-th range each.
+template <class T, int D>
+__global__ __launch_bounds__(256) void cache_join_kernel(const CacheParams p) {
+  constexpr int TPR = D / 4, NG = 256 / TPR;
+  __shared__ f32x4 so[NG][TPR];
+  __shared__ float sm[NG], sl[NG];
+  const int64_t rows = (int64_t)p.B * p.H * p.L, row = blockIdx.x;
+  const int i = (int)(row % p.L), h = (int)(row / p.L % p.H), b = (int)(row / p.L / p.H);
+  const Lens len(p, b);
+  int used = (len.n + p.chunk - 1) / p.chunk;
+  used = used < 1 ? 1 : used;                              // the first range is always there
+  const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+  float m = -INFINITY, l = 0.f;
+  for (int s = grp; s < used; s += NG) {
+    const float x = p.part_ml[2 * (s * rows + row)];
+    m = x <= m ? m : x;
+  }
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = grp; s < used; s += NG) {
+    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * (s * rows + row));
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (s * rows + row) * D + 4 * t);
+    const float w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+    l += w * ml.y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += w * v[j];
+  }
+  so[grp][t] = o;
+  if (t == 0) {
+    sm[grp] = m;
+    sl[grp] = l;
+  }
+  __syncthreads();
+  if (grp != 0) return;
+#pragma unroll
+  for (int x = 1; x < NG; ++x) m = sm[x] <= m ? m : sm[x];
+  l = 0.f;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int x = 0; x < NG; ++x) {
+    const float w = sm[x] == -INFINITY ? 0.f : fast_exp2(sm[x] - m);
+    const f32x4 v = so[x][t];
+    l += w * sl[x];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += w * v[j];
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  *reinterpret_cast<uint2*>(p.out + b * p.so.b + h * p.so.h + i * p.so.t + 4 * t) =
+      make_uint2(T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv));
+  if (p.lse && t == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+CachePlan plan_cache_attn(const CacheParams& p) {
+  CachePlan c{};
+  const int64_t units = (int64_t)p.B * p.Hk, rows = (int64_t)p.G * p.L, keys = (int64_t)p.c.max_pages * p.c.page;
+  c.few = rows <= kFewRows;
+  const int64_t tiles = units * (c.few ? 1 : (rows + 127) / 128);
+  const int64_t step = c.few ? 256 : 64;                   // keys of a workgroup's turn
+  const int64_t turns = (keys + step - 1) / step;
+  int64_t n = tiles > 0 ? (c.few ? 1024 : 512) / tiles : 1;    // ranges that fill the chip
+  if (!c.few && n < 2) n = 1;
+  const int64_t least = c.few ? 1 : 4;                     // turns of a range
+  n = n < turns / least ? n : turns / least;
+  n = n < 1 ? 1 : n;
+  const int64_t each = turns == 0 ? 1 : (turns + n - 1) / n;
+  c.chunk = (int)(each * step < 0x7FFFFF00 ? each * step : 0x7FFFFF00);
+  c.chunks = turns == 0 ? 1 : (int)((turns + each - 1) / each);
+  if (c.chunks > 1) {
+    const int64_t all = (int64_t)c.chunks * p.B * p.H * p.L;
+    c.part_ml = (all * p.D * 4 + 255) / 256 * 256;
+    c.bytes = c.part_ml + (all * 8 + 255) / 256 * 256;
+  }
+  return c;
+}
+
+template <class T, int D>
+static hipError_t run_attn(CacheParams p, const CachePlan& c, hipStream_t st) {
+  const int64_t rows = (int64_t)p.G * p.L, units = (int64_t)p.B * p.Hk;
+  p.chunk = c.chunk;
+  p.chunks = c.chunks;
+  p.n_wg = (int)(units * p.chunks * (c.few ? 1 : (rows + 127) / 128));
+  if (!c.few) hipLaunchKernelGGL((cache_rows_kernel<T, D>), dim3(p.n_wg), dim3(256), 0, st, p);
+  else if (rows <= 16) hipLaunchKernelGGL((cache_few_kernel<T, D, 1>), dim3(p.n_wg), dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((cache_few_kernel<T, D, 2>), dim3(p.n_wg), dim3(256), 0, st, p);
+  if (p.chunks > 1)
+    hipLaunchKernelGGL((cache_join_kernel<T, D>), dim3((uint32_t)(units * rows)), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_attn(CacheParams p, bool f16, const CachePlan& c, hipStream_t st) {
+  if (p.D == 64) return f16 ? run_attn<FP16, 64>(p, c, st) : run_attn<BF16, 64>(p, c, st);
+  return f16 ? run_attn<FP16, 128>(p, c, st) : run_attn<BF16, 128>(p, c, st);
+}
+
+}  // namespace adaspa

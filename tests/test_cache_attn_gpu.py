@@ -1,0 +1,214 @@
+"""Attention over an 8-bit cache against the definition in 64 bits: rows from one to
+many, lengths from none to long, pages that end inside tiles, shared heads, strides."""
+import itertools
+import math
+import random
+
+import pytest
+import torch
+
+import paper_2502_21079_amd as ad
+from _cache_ref import attn_reference, random_pool, within
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def queries(B, H, Lq, D, dt, seed, layout="bhld"):
+    g = torch.Generator().manual_seed(seed)
+    q = torch.randn(B, Lq, H, D, generator=g).to(dt).to(DEV).transpose(1, 2)
+    return q if layout == "blhd" else q.contiguous()
+
+
+def run(B, H, Hk, Lq, lens, page, D, dt, *, q_lens=None, causal=True, scale=None, seed=1, layout="bhld", spare=0, **kw):
+    cap = max(1, -(-max(lens) // page)) + spare
+    cache, table, ks, vs = random_pool(ad, B, lens, Hk, page, D, cap, seed)
+    q = queries(B, H, Lq, D, dt, seed + 1, layout)
+    out, lse = ad.cache_attn(q, cache, table, i32(lens), q_lens=None if q_lens is None else i32(q_lens), causal=causal,
+                             scale=scale, **kw)
+    ref = attn_reference(q, ks, vs, lens, q_lens=q_lens, causal=causal, scale=scale)
+    what = f"B{B} H{H}/{Hk} Lq{Lq} lens{lens} page{page} D{D} {dt} q{q_lens} c{causal}"
+    print(what, flush=True)
+    assert out.stride() == q.stride() or not q.numel()
+    within(out, ref["out"], "out " + what)
+    within(lse, ref["lse"], "lse " + what)
+    return q, cache, table, out, lse
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_single_tokens(page, D, dt):
+    """One token of each sequence, from no key to many."""
+    run(5, 4, 2, 1, [1, 0, 63, 300, 65], page, D, dt, seed=page)
+    run(3, 6, 1, 1, [16, 17, 1500], page, D, dt, seed=page + 1, spare=2)
+
+
+@pytest.mark.parametrize("Lq,H,Hk", [(2, 2, 2), (5, 6, 2), (16, 1, 1), (16, 2, 1), (17, 2, 1), (33, 3, 3), (128, 2, 1), (129, 1, 1),
+                                     (43, 6, 2), (300, 2, 2)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows(Lq, H, Hk, D, causal):
+    """Rows below, at and past the sizes at which a wave's or a workgroup's tiles end."""
+    dt = torch.bfloat16 if (Lq + D) % 2 else torch.float16
+    run(2, H, Hk, Lq, [max(Lq, 333), Lq], 32, D, dt, causal=causal, seed=Lq, layout="blhd")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_padded_batches(D, dt):
+    """Samples with fewer queries than the batch is wide, with none, with more queries than
+    tokens (the first see nothing), without tokens."""
+    for Lq in (4, 40, 150):
+        run(6, 4, 2, Lq, [200, 200, 200, 2, 0, 5], 16, D, dt, q_lens=[Lq, 1, 0, Lq, Lq, 3], seed=Lq)
+        run(3, 4, 2, Lq, [200, 70, 0], 64, D, dt, q_lens=[Lq, 2, Lq], causal=False, seed=Lq + 1)
+
+
+@pytest.mark.parametrize("n", [1, 15, 16, 17, 31, 33, 47, 48, 49, 63, 64, 65, 127, 128, 129, 255, 256, 257])
+def test_lengths_around_tiles(n):
+    for page, Lq in ((16, 1), (128, 1), (16, 40), (64, 40)):
+        run(1, 2, 1, Lq, [n], page, 64, torch.bfloat16, seed=n)
+
+
+def test_large_scores_and_scales():
+    """Scores of hundreds either way, scales from 2^-126 to 2^100 beside each other."""
+    for Lq in (1, 70):
+        run(2, 2, 1, Lq, [400, 130], 16, 64, torch.float16, scale=3.0, seed=Lq)
+        run(2, 2, 1, Lq, [400, 130], 16, 128, torch.bfloat16, scale=-1.0, seed=Lq + 1)
+        for dt in (torch.bfloat16, torch.float16):
+            B, H, page, D, lens = 1, 2, 16, 64, [200]
+            cache, table, ks, vs = random_pool(ad, B, lens, 1, page, D, 13, Lq)
+            ids = table[0].long().cpu()
+            by = torch.ones(13, dtype=torch.float64)
+            # One page of values thousands of times larger whose keys hardly count, one of zeros of the least scale.
+            by[2], by[5] = 2.0 ** 10, 2.0 ** -117
+            at = torch.arange(200) // page
+            cache.v_scale[ids.to(DEV)] *= by.float().to(DEV)[:, None]
+            vs[0] = vs[0] * by[at][None, :, None]
+            ks[0][:, at == 2] = 0
+            cache.k[ids[2].item()] = torch.zeros_like(cache.k[ids[2].item()].float()).to(cache.k.dtype)
+            q = queries(B, H, Lq, D, dt, 9) * 4
+            out, lse = ad.cache_attn(q, cache, table, i32(lens))
+            ref = attn_reference(q, ks, vs, lens)
+            within(out, ref["out"], "out")
+            within(lse, ref["lse"], "lse")
+
+
+def test_pages_that_are_not_there():
+    """Entries outside the pool take no part, nor do their tokens' places."""
+    B, H, Hk, page, D = 1, 4, 2, 16, 64
+    for Lq in (1, 50):
+        lens = [200]
+        cache, table, ks, vs = random_pool(ad, B, lens, Hk, page, D, 13, 3)
+        q = queries(B, H, Lq, D, torch.bfloat16, 4)
+        bad = table.clone()
+        bad[0, 1], bad[0, 6], bad[0, 7] = -1, cache.k.shape[0], 1 << 30
+        keep = torch.ones(200, dtype=torch.bool)
+        keep[16:32] = keep[96:128] = False
+        out, lse = ad.cache_attn(q, cache, bad, i32(lens), causal=False)
+        ref = attn_reference(q, [ks[0][:, keep]], [vs[0][:, keep]], [int(keep.sum())], causal=False)
+        within(out, ref["out"], "out")
+        within(lse, ref["lse"], "lse")
+        out, lse = ad.cache_attn(q, cache, torch.full_like(bad, -1), i32(lens))
+        assert not out.any() and (lse == -math.inf).all()
+        # Lengths past the table end with it, below 0 count as 0.
+        full = [13 * page]
+        cache, table, ks, vs = random_pool(ad, B, full, Hk, page, D, 13, 5)
+        out, lse = ad.cache_attn(q, cache, table, i32([1 << 30]))
+        ref = attn_reference(q, ks, vs, full)
+        within(out, ref["out"], "out")
+        out, lse = ad.cache_attn(q, cache, table, i32([-4]))
+        assert not out.any() and (lse == -math.inf).all()
+        none = table[:, :0]
+        out, lse = ad.cache_attn(q, cache, none, i32([10]))
+        assert not out.any() and (lse == -math.inf).all()
+
+
+def test_nan_of_a_token_reaches_its_rows_alone():
+    """A sequence with a NaN among its keys, or values, gives NaN there; others do not."""
+    for Lq in (1, 60):
+        cache, table, ks, vs = random_pool(ad, 2, [100, 100], 1, 16, 64, 7, 8)
+        q = queries(2, 2, Lq, 64, torch.bfloat16, 9)
+        cache.k.view(torch.uint8)[table[0, 2].long(), 0, 3, 5] = 0x7F
+        out, lse = ad.cache_attn(q, cache, table, i32([100, 100]))
+        assert out[0].isnan().all() and lse[0].isnan().all()
+        ref = attn_reference(q[1:], ks[1:], vs[1:], [100])
+        within(out[1:], ref["out"], "out")
+        within(lse[1:], ref["lse"], "lse")
+
+
+def test_outputs_workspace_and_repeats():
+    """Outputs and workspace of the caller's; the same bits each time, whatever the workspace
+    held; no lse; one device call per stream."""
+    B, H, Hk, page, D = 3, 8, 2, 64, 128
+    lens = [900, 1200, 64]
+    cache, table, ks, vs = random_pool(ad, B, lens, Hk, page, D, 19, 6)
+    for Lq in (1, 4, 30):
+        q = queries(B, H, Lq, D, torch.bfloat16, Lq, "blhd")
+        out, lse = ad.cache_attn(q, cache, table, i32(lens))
+        need = ad.cache_attn_workspace(q.shape, cache, 19)
+        for byte in (0, 255):
+            ws = torch.full((need,), byte, dtype=torch.uint8, device=DEV)
+            room = torch.full((B, Lq + 1, H + 1, D), 3.0, dtype=q.dtype, device=DEV)
+            o = room[:, :Lq, :H].transpose(1, 2)
+            z = torch.empty_like(lse)
+            ad.cache_attn(q, cache, table, i32(lens), out=o, lse=z, workspace=ws)
+            assert torch.equal(o, out) and torch.equal(z, lse)
+            assert (room[:, Lq:] == 3).all() and (room[:, :, H:] == 3).all()
+        o, none = ad.cache_attn(q, cache, table, i32(lens), want_lse=False)
+        assert none is None and torch.equal(o, out)
+        if need > 16:
+            with pytest.raises(ad.AdaspaError):
+                ad.cache_attn(q, cache, table, i32(lens), workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            o, z = ad.cache_attn(q, cache, table, i32(lens))
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(o, out) and torch.equal(z, lse)
+
+
+def test_shared_pages():
+    """Two sequences over the same beginning, read alike."""
+    cache, table, ks, vs = random_pool(ad, 1, [256], 2, 32, 64, 8, 7)
+    both = table.expand(2, -1)                           # a table of one row, read twice
+    q = queries(2, 4, 3, 64, torch.bfloat16, 1)
+    out, lse = ad.cache_attn(q, cache, both, i32([256, 100]))
+    ref = attn_reference(q, [ks[0], ks[0][:, :100]], [vs[0], vs[0][:, :100]], [256, 100])
+    within(out, ref["out"], "out")
+    within(lse, ref["lse"], "lse")
+
+
+def test_long_sequences():
+    """Tens of thousands of tokens, split over workgroups, in both kernels."""
+    run(2, 4, 1, 1, [20011, 9000], 64, 64, torch.bfloat16, seed=1)
+    run(1, 6, 2, 3, [30000], 16, 128, torch.float16, seed=2)
+    run(1, 2, 1, 130, [12345], 128, 128, torch.bfloat16, seed=3)
+
+
+def test_random_cases():
+    rng = random.Random(11)
+    for trial in range(60):
+        page, D, dt = rng.choice([16, 32, 64, 128]), rng.choice([64, 128]), rng.choice([torch.bfloat16, torch.float16])
+        Hk, G, B = rng.choice([1, 2, 3]), rng.choice([1, 2, 3, 5, 8, 12]), rng.choice([1, 2, 4])
+        Lq = rng.choice([1, 1, 2, 3, 7, 20, 65, 140])
+        lens = [rng.choice([0, 1, rng.randrange(700)]) for _ in range(B)]
+        q_lens = [rng.randrange(-1, Lq + 2) for _ in range(B)] if rng.random() < 0.5 else None
+        run(B, Hk * G, Hk, Lq, lens, page, D, dt, q_lens=q_lens, causal=rng.random() < 0.7, seed=trial,
+            layout=rng.choice(["bhld", "blhd"]), spare=rng.randrange(20), scale=rng.choice([None, 0.3]))
+
+
+def test_sizes_of_nothing():
+    for B, Lq in itertools.product((0, 2), (0, 1)):
+        if B and Lq:
+            continue
+        cache = ad.kv_cache(4, 2, 16, 64)
+        q = torch.zeros(B, 4, Lq, 64, dtype=torch.bfloat16, device=DEV)
+        out, lse = ad.cache_attn(q, cache, torch.zeros(B, 3, dtype=torch.int32, device=DEV),
+                                 torch.zeros(B, dtype=torch.int32, device=DEV))
+        assert out.shape == q.shape and lse.shape == q.shape[:3]
