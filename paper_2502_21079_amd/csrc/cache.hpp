@@ -34,17 +34,21 @@ struct CacheParams {
   float* lse;                          // [B, H, L], may be null
   float sl2;                           // softmax scale * log2(e)
   int causal;
-  int chunk, chunks;                   // keys of a range, ranges of a sequence at most
-  float* part_o;                       // [chunks, B * H * L, D]
-  float* part_ml;                      // [chunks, B * H * L, 2] reference and sum
+  int shares;                          // few rows: workgroups of a key head that share all samples' keys, 0: one a
+                                       // sample
+  int64_t* before;                     // few rows: [B + 1] turns before each sample
+  int chunk, chunks;                   // many rows: keys of a range, ranges of a sequence at most
+  float* part_o;                       // [2 * shares, Hk, G * L, D], or [chunks, B * H * L, D]
+  float* part_ml;                      // the same with 2 in place of D: reference and sum
   int n_wg;
 };
 
 // Ranges and scratch of an attention call, by its shape alone.
 struct CachePlan {
   bool few;                            // the rows of a key head fit in a wave's tiles
-  int chunk, chunks;
-  int64_t part_ml, bytes;
+  bool bypass;                         // few rows: keys and values are read past the last-level cache
+  int shares, chunk, chunks;
+  int64_t part_ml, before, bytes;      // byte offsets into the workspace
 };
 constexpr int kFewRows = 32;
 

@@ -151,6 +151,7 @@ adaspa_status adaspa_cache_attn(const adaspa_cache_problem* prob, const adaspa_c
   p.new_lens = q_lens;
   p.part_o = (float*)workspace;
   p.part_ml = (float*)((char*)workspace + plan.part_ml);
+  p.before = (int64_t*)((char*)workspace + plan.before);
   return done(launch_cache_attn(p, prob->dtype == ADASPA_FP16, plan, (hipStream_t)stream));
 }
 

@@ -22,6 +22,8 @@ namespace {
 // maximum only where a score is further above it: no weight exceeds 2^8, and most
 // tiles rescale nothing.
 constexpr float kAbove = 8.f;
+// The same by sums: a lane's weights of one tile add up to no more.
+constexpr float kSumLimit = 256.f;
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -52,7 +54,7 @@ __device__ __forceinline__ RowOf cache_row(const CacheParams& p, int unit, int r
 struct Lens {
   int n, q;                                              // keys; queries, the last q of the positions
   __device__ __forceinline__ Lens(const CacheParams& p, int b) {
-    n = clamp_len(__builtin_amdgcn_readfirstlane(p.lens[b]), (int)((int64_t)p.c.max_pages * p.c.page));
+    n = p.c.pages ? clamp_len(__builtin_amdgcn_readfirstlane(p.lens[b]), p.c.max_pages * p.c.page) : 0;
     q = p.new_lens ? clamp_len(__builtin_amdgcn_readfirstlane(p.new_lens[b]), p.L) : p.L;
   }
   // How many keys query i sees.
@@ -64,6 +66,63 @@ struct Lens {
   }
 };
 
+template <bool BYPASS>
+__device__ __forceinline__ u32x4 read16(const uint8_t* p) {
+  const u32x4* from = reinterpret_cast<const u32x4*>(p);
+  if constexpr (BYPASS) return __builtin_nontemporal_load(from);
+  return *from;
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32) |
+                   (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x));
+}
+
+// The turns of all samples, and where share w of them begins (in LDS: sample, turn of
+// that).  Share 0 also leaves the turns before each sample for the join.
+struct Turns {
+  int64_t total;
+  int shares;                                            // no more than turns
+  __device__ __forceinline__ Turns(const CacheParams& p, int tid, int wave, int lane, int w, int* place) {
+    __shared__ int64_t sums[4];
+    const int each = (p.B + 255) / 256, b0 = tid * each, b1 = b0 + each < p.B ? b0 + each : p.B;
+    auto turns = [&](int b) { return (clamp_len(p.lens[b], p.c.max_pages * p.c.page) + 255) / 256; };
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) mine += turns(b);
+    int64_t upto = mine;                                   // of this wave's lanes up to this one
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const int64_t x = __shfl_up(upto, s);
+      if (lane >= s) upto += x;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (x < wave) upto += sums[x];
+      total += sums[x];
+    }
+    total = uniform(total);
+    int64_t before = upto - mine;
+    shares = (int)(total < p.shares ? total : p.shares);
+    const int64_t from = shares == 0 ? 0 : total * w / shares;
+    if (w == 0 || (from >= before && from < upto)) {
+      for (int b = b0; b < b1; ++b) {
+        const int t = turns(b);
+        if (w == 0) p.before[b] = before;
+        if (from >= before && from < before + t) {
+          place[0] = b;
+          place[1] = (int)(from - before);
+        }
+        before += t;
+      }
+      if (w == 0 && tid == 255) p.before[p.B] = total;
+    }
+    __syncthreads();
+  }
+};
+
 }  // namespace
 
 // Up to 16 NQ rows of a key head.  Every wave walks blocks of 64 keys of its own,
@@ -71,211 +130,325 @@ struct Lens {
 // the first product are keys ordered so that a lane's scores are those of 16
 // neighbouring tokens, whose values of one channel lie side by side in the cache.
 // So neither operand passes through LDS, and a block's loads are 16 bytes a lane.
-// The waves' sums are joined in LDS, ranges of the keys by cache_join_kernel.
-template <class T, int D, int NQ>
-__global__ __launch_bounds__(256, 2) void cache_few_kernel(const CacheParams p) {
+//
+// Work is counted in turns, 256 keys, a block for each wave.  With p.shares, workgroup
+// (w, key head) takes an equal share of the turns of all samples in their order, whatever their
+// lengths; where a share ends inside a sequence, its sums go to the workspace (place 2 w for
+// what begins inside one, 2 w + 1 for what begins with one) and cache_few_join_kernel joins
+// them.  Without, a workgroup takes a sequence.
+//
+// Workgroups are few (one a CU with p.shares) and every wave has one or two blocks, 16 to 32 KB, on
+// their way: more of them only spread the reads over memory.  The key heads of a
+// share run side by side, since they lie side by side in a page.  BYPASS: keys and values that the
+// last-level cache could not keep until the next call are read past it.  16 sequences of up to
+// 17,664 tokens, 4 key heads of d 128 under 24, and 110,080 tokens of 24 heads, us a call: shares in
+// the order samples, key heads, turns, 512 workgroups 53 and 129; key heads side by side 51 and 128;
+// 256 workgroups 48 and 124; past the cache 46 and 113 (6.0 TB/s).
+template <class T, int D, int NQ, bool BYPASS>
+__global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_few_kernel(const CacheParams p) {
   constexpr int NW = 4, DT = D / 16, KJ = D / 64;          // channel tiles; 16-byte pieces of a key a lane
   __shared__ __attribute__((aligned(16))) float so[NW][NQ * 16 * D];
   __shared__ float sm[NW][NQ * 16], sl[NW][NQ * 16];
+  __shared__ int place[2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int g = lane >> 4, c16 = lane & 15;
-  const int unit = blockIdx.x / p.chunks, range = blockIdx.x % p.chunks;
-  const int b = unit / p.Hk, hk = unit % p.Hk, n_rows = p.G * p.L;
-  const Lens len(p, b);
-  const int k0 = range * p.chunk, k1 = len.n - k0 < p.chunk ? len.n : k0 + p.chunk;   // keys of this range
-  if (k0 >= len.n && range > 0) return;
-
-  typename T::x8 qf[NQ][KJ][2];
-  int seen[NQ];
-  float m[NQ], l[NQ];
-  f32x4 o[NQ][DT];
-#pragma unroll
-  for (int r = 0; r < NQ; ++r) {
-    const bool ok = r * 16 + c16 < n_rows;
-    const RowOf ro = cache_row(p, unit, ok ? r * 16 + c16 : 0);
-    const u16* q = at(p.q, p.sq, ro);
-    seen[r] = ok ? len.seen(p, ro.i) : 0;
-#pragma unroll
-    for (int j = 0; j < KJ; ++j)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4 w = {0, 0, 0, 0};
-        if (ok) w = *reinterpret_cast<const u32x4*>(q + 64 * j + 16 * g + 8 * h);
-        qf[r][j][h] = __builtin_bit_cast(typename T::x8, w);
-      }
-    m[r] = -INFINITY;
-    l[r] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[r][d] = f32x4{};
+  const int n_rows = p.G * p.L, shift = 31 - __builtin_clz(p.c.page);
+  const int hk = blockIdx.x % p.Hk, w = blockIdx.x / p.Hk;
+  int b = w, left = 0;                                     // sample; turns of it before this share
+  int64_t turn = 0, end = 1;                               // this workgroup's share of all turns
+  if (p.shares) {
+    const Turns all(p, tid, wave, lane, w, place);
+    if (w >= all.shares) return;
+    turn = all.total * w / all.shares;
+    end = all.total * (w + 1) / all.shares;
+    b = __builtin_amdgcn_readfirstlane(place[0]);
+    left = __builtin_amdgcn_readfirstlane(place[1]);
   }
-  const int fewest = len.q < p.L ? 0 : len.seen(p, 0);     // keys that every row sees
-  const int shift = 31 - __builtin_clz(p.c.page);
+  for (bool first = true;; first = false) {
+    const Lens len(p, b);
+    const int turns = (len.n + 255) / 256;
+    if (p.shares && turns == 0) {                            // the next sample with keys (there is one)
+      ++b;
+      continue;
+    }
+    const int upto = !p.shares || turns - left <= end - turn ? turns : left + (int)(end - turn);
+    const int k0 = left * 256, k1 = upto * 256 < len.n ? upto * 256 : len.n;     // keys of this part of the share
+    const int unit = b * p.Hk + hk;
 
-  struct Block {
-    u32x4 k[4][KJ], v[DT];
-    float ks, vs;
-    int live;                                              // tokens of this lane's 16 that are there
-  };
-  auto load = [&](Block& x, int k) {
-    // Keys: 16 rows of an instruction are tokens 4 t + c16 % 4 of sixteen number c16 / 4.
-    const int kp = k + (c16 >> 2) * 16, vp = k + g * 16;
-    const int ki = kp < len.n ? page_at(p.c, b, kp >> shift) : -1, vi = vp < len.n ? page_at(p.c, b, vp >> shift) : -1;
-    const int64_t ka = (int64_t)(ki < 0 ? 0 : ki) * p.Hk + hk, va = (int64_t)(vi < 0 ? 0 : vi) * p.Hk + hk;
-    const int mask = p.c.page - 1;
-    const uint8_t* kt = p.c.k + (ka << shift) * D + ((kp & mask) + (c16 & 3)) * D + 16 * g;
-    const uint8_t* vt = p.c.v + (va << shift) * D + (vp & mask) * D + 16 * c16;
+    typename T::x8 qf[NQ][KJ][2];
+    int seen[NQ];
+    float m[NQ], l[NQ];
+    f32x4 o[NQ][DT];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < KJ; ++j) {
-        x.k[t][j] = u32x4{0, 0, 0, 0};
-        if (ki >= 0) x.k[t][j] = *reinterpret_cast<const u32x4*>(kt + 4 * t * D + 64 * j);
-      }
-#pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      x.v[d] = u32x4{0, 0, 0, 0};
-      if (vi >= 0) x.v[d] = *reinterpret_cast<const u32x4*>(vt + 256 * d);
-    }
-    x.ks = x.vs = 1.f;
-    if (vi >= 0) {
-      x.ks = p.c.k_scale[va];
-      x.vs = p.c.v_scale[va];
-    }
-    const int left = len.n - vp;
-    x.live = vi < 0 ? 0 : (left < 16 ? left : 16);
-  };
-  auto work = [&](Block& x, int k) {
-    const bool edge = k + 64 > fewest || __any(x.live < 16);
-    if (edge) {
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x.v[d][i] &= first_bytes(x.live - 4 * i);
-    }
-    f32x4 s[NQ][4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-#pragma unroll
-      for (int r = 0; r < NQ; ++r) s[r][t] = f32x4{};
+    for (int r = 0; r < NQ; ++r) {
+      const bool ok = r * 16 + c16 < n_rows;
+      const RowOf ro = cache_row(p, unit, ok ? r * 16 + c16 : 0);
+      const u16* q = at(p.q, p.sq, ro);
+      seen[r] = ok ? len.seen(p, ro.i) : 0;
 #pragma unroll
       for (int j = 0; j < KJ; ++j)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const typename T::x8 kf = decode8<T>(x.k[t][j][2 * h], x.k[t][j][2 * h + 1], 1.f);
-#pragma unroll
-          for (int r = 0; r < NQ; ++r) s[r][t] = mfma16(kf, qf[r][j][h], s[r][t]);
+          u32x4 w = {0, 0, 0, 0};
+          if (ok) w = *reinterpret_cast<const u32x4*>(q + 64 * j + 16 * g + 8 * h);
+          qf[r][j][h] = __builtin_bit_cast(typename T::x8, w);
         }
-    }
-    const float a = x.ks * p.sl2;
-    bf16x8 w[NQ][2], rest[NQ][2];
+      m[r] = -INFINITY;
+      l[r] = 0.f;
 #pragma unroll
-    for (int r = 0; r < NQ; ++r) {
-      float top = -INFINITY;
-      const int see = seen[r] - (k + 16 * g) < x.live ? seen[r] - (k + 16 * g) : x.live;
+      for (int d = 0; d < DT; ++d) o[r][d] = f32x4{};
+    }
+    const int fewest = len.q < p.L ? 0 : len.seen(p, 0);     // keys that every row sees
+
+    struct Block {
+      u32x4 k[4][KJ], v[DT];
+      float ks, vs;
+      int live;                                              // tokens of this lane's 16 that are there
+    };
+    // What the table says of this wave's next 16 blocks (lane 4 i + j: sixteen j of block
+    // i) and of the 16 after them, so that no load waits for another.  n > 0; behind the last
+    // token the last one's page stands.
+    constexpr int STEP = 64 * NW;
+    auto look = [&](int k) {
+      const int pos = k + (lane >> 2) * STEP + (lane & 3) * 16;
+      return p.c.table[b * p.c.table_stride + ((pos < len.n - 1 ? pos : len.n - 1) >> shift)];
+    };
+    int pages = 0, later = 0, at_page = 0;
+    // What is not there is read from the pool's first page and masked.
+    auto load = [&](Block& x, int k) {
+      if (at_page == 64) {
+        pages = later;
+        later = look(k + 16 * STEP);
+        at_page = 0;
+      }
+      const int i0 = __builtin_amdgcn_readlane(pages, at_page), i1 = __builtin_amdgcn_readlane(pages, at_page + 1);
+      const int i2 = __builtin_amdgcn_readlane(pages, at_page + 2), i3 = __builtin_amdgcn_readlane(pages, at_page + 3);
+      at_page += 4;
+      auto of = [&](int i) {                                 // (by bits: a choice would put them in memory)
+        const int odd = -(i & 1), lo = i0 ^ ((i0 ^ i1) & odd), hi = i2 ^ ((i2 ^ i3) & odd);
+        return (uint32_t)(lo ^ ((lo ^ hi) & -(i >> 1)));
+      };
+      // Keys: 16 rows of an instruction are tokens 4 t + c16 % 4 of sixteen number c16 / 4.
+      const uint32_t kp = of(c16 >> 2), vp = of(g), all = p.c.pages, mask = p.c.page - 1;
+      const int64_t ka = (int64_t)(kp < all ? kp : 0) * p.Hk + hk, va = (int64_t)(vp < all ? vp : 0) * p.Hk + hk;
+      const uint8_t* kt = p.c.k + (ka << shift) * D + (((k + (c16 >> 2) * 16) & mask) + (c16 & 3)) * D + 16 * g;
+      const uint8_t* vt = p.c.v + (va << shift) * D + ((k + g * 16) & mask) * D + 16 * c16;
+      x.ks = p.c.k_scale[va];
+      x.vs = p.c.v_scale[va];
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[r][t][e] *= a;
-          if (edge && 4 * t + e >= see) s[r][t][e] = -INFINITY;
-          top = vmax(top, s[r][t][e]);
-        }
-      const auto u = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-      top = both_halves_max(vmax(__uint_as_float(u[0]), __uint_as_float(u[1])));
-      if (__any(!(top <= m[r] + kAbove))) {                // NaN too: the row becomes NaN
-        const float to = top <= m[r] ? m[r] : top;
-        const float by = to == -INFINITY ? 1.f : fast_exp2(m[r] - to);
-        m[r] = to;
-        l[r] *= by;
+        for (int j = 0; j < KJ; ++j) x.k[t][j] = read16<BYPASS>(kt + 4 * t * D + 64 * j);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) x.v[d] = read16<BYPASS>(vt + 256 * d);
+      const int left = len.n - (k + g * 16);
+      x.live = vp < all ? (left < 16 ? left : 16) : 0;
+    };
+    auto work = [&](Block& x, int k) {
+      const bool edge = k + 64 > fewest || __any(x.live < 16);
+      if (edge) {
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[r][d][e] *= by;
+          for (int i = 0; i < 4; ++i) x.v[d][i] &= first_bytes(x.live - 4 * i);
+        if (x.live <= 0) x.vs = 1.f;                         // no page's scale, and zeros
       }
-      const float ref = m[r] == -INFINITY ? 0.f : m[r];
-      float sum = 0.f;
-      u32x4 hi[2], lo[2];
+      f32x4 s[NQ][4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 4; ++t) {
 #pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          const float c = fast_exp2(s[r][t][e] - ref), d = fast_exp2(s[r][t][e + 1] - ref);
-          sum += c + d;
-          uint32_t left = 0;
-          hi[t >> 1][(t & 1) * 2 + e / 2] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
-          lo[t >> 1][(t & 1) * 2 + e / 2] = left;
+        for (int r = 0; r < NQ; ++r) s[r][t] = f32x4{};
+#pragma unroll
+        for (int j = 0; j < KJ; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const typename T::x8 kf = decode8<T>(x.k[t][j][2 * h], x.k[t][j][2 * h + 1], 1.f);
+#pragma unroll
+            for (int r = 0; r < NQ; ++r) s[r][t] = mfma16(kf, qf[r][j][h], s[r][t]);
+          }
+      }
+      const float a = x.ks * p.sl2;
+      bf16x8 w[NQ][2], rest[NQ][2];
+#pragma unroll
+      for (int r = 0; r < NQ; ++r) {
+        float top = -INFINITY;
+        const int see = seen[r] - (k + 16 * g) < x.live ? seen[r] - (k + 16 * g) : x.live;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[r][t][e] *= a;
+            if (edge && 4 * t + e >= see) s[r][t][e] = -INFINITY;
+            top = vmax(top, s[r][t][e]);
+          }
+        const auto u = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = both_halves_max(vmax(__uint_as_float(u[0]), __uint_as_float(u[1])));
+        if (__any(!(top <= m[r] + kAbove))) {                // NaN too: the row becomes NaN
+          const float to = top <= m[r] ? m[r] : top;
+          const float by = to == -INFINITY ? 1.f : fast_exp2(m[r] - to);
+          m[r] = to;
+          l[r] *= by;
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[r][d][e] *= by;
         }
-      l[r] += sum;
+        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+        float sum = 0.f;
+        u32x4 hi[2], lo[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        w[r][h] = __builtin_bit_cast(bf16x8, hi[h]);
-        rest[r][h] = __builtin_bit_cast(bf16x8, lo[h]);
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const float c = fast_exp2(s[r][t][e] - ref), d = fast_exp2(s[r][t][e + 1] - ref);
+            sum += c + d;
+            uint32_t left = 0;
+            hi[t >> 1][(t & 1) * 2 + e / 2] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
+            lo[t >> 1][(t & 1) * 2 + e / 2] = left;
+          }
+        l[r] += sum;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          w[r][h] = __builtin_bit_cast(bf16x8, hi[h]);
+          rest[r][h] = __builtin_bit_cast(bf16x8, lo[h]);
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8 vf = decode8<BF16>(x.v[d][2 * h], x.v[d][2 * h + 1], x.vs);
+#pragma unroll
+          for (int r = 0; r < NQ; ++r) {
+            o[r][d] = mfma16(vf, w[r][h], o[r][d]);
+            if (T::kHalf) o[r][d] = mfma16(vf, rest[r][h], o[r][d]);
+          }
+        }
+    };
+    Block x[2];
+    int k = k0 + wave * 64;
+    if (k < k1) {
+      // A block's loads go out before the one before it is worked on, also where it is past the
+      // range (it is not worked on): behind a branch the compiler would wait for the newest.
+      pages = look(k);
+      later = look(k + 16 * STEP);
+      load(x[0], k);
+      // The queries are there (all but the newest 2 + 4 KJ + DT loads): left to the first product,
+      // inside the loop, their wait would hold up every turn.
+      constexpr int newest = 2 + 4 * KJ + DT;
+      __builtin_amdgcn_s_waitcnt(0x0F70 | (newest & 15) | (newest >> 4 << 14));
+      for (;; k += 2 * STEP) {
+        load(x[1], k + STEP);
+        work(x[0], k);
+        if (k + STEP >= k1) break;
+        load(x[0], k + 2 * STEP);
+        work(x[1], k + STEP);
+        if (k + 2 * STEP >= k1) break;
       }
     }
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8 vf = decode8<BF16>(x.v[d][2 * h], x.v[d][2 * h + 1], x.vs);
-#pragma unroll
-        for (int r = 0; r < NQ; ++r) {
-          o[r][d] = mfma16(vf, w[r][h], o[r][d]);
-          if (T::kHalf) o[r][d] = mfma16(vf, rest[r][h], o[r][d]);
-        }
-      }
-  };
-  Block x[2];
-  int k = k0 + wave * 64;
-  if (k < k1) load(x[0], k);
-  for (; k < k1; k += 2 * 64 * NW) {
-    if (k + 64 * NW < k1) load(x[1], k + 64 * NW);
-    work(x[0], k);
-    if (k + 64 * NW >= k1) break;
-    if (k + 2 * 64 * NW < k1) load(x[0], k + 2 * 64 * NW);
-    work(x[1], k + 64 * NW);
-  }
 
-  // The waves' sums: lane c16 of a group of 16 has row c16, channels 16 d + 4 g on.
+    // The waves' sums: lane c16 of a group of 16 has row c16, channels 16 d + 4 g on.
 #pragma unroll
-  for (int r = 0; r < NQ; ++r) {
-    const auto u = __builtin_amdgcn_permlane16_swap(__float_as_uint(l[r]), __float_as_uint(l[r]), false, false);
-    l[r] = both_halves_sum(__uint_as_float(u[0]) + __uint_as_float(u[1]));
-    if (g == 0) {
-      sm[wave][r * 16 + c16] = m[r];
-      sl[wave][r * 16 + c16] = l[r];
+    for (int r = 0; r < NQ; ++r) {
+      const auto u = __builtin_amdgcn_permlane16_swap(__float_as_uint(l[r]), __float_as_uint(l[r]), false, false);
+      l[r] = both_halves_sum(__uint_as_float(u[0]) + __uint_as_float(u[1]));
+      if (g == 0) {
+        sm[wave][r * 16 + c16] = m[r];
+        sl[wave][r * 16 + c16] = l[r];
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(&so[wave][(r * 16 + c16) * D + 16 * d + 4 * g]) = o[r][d];
     }
+    __syncthreads();
+    constexpr int TPR = D / 4;
+    for (int i = tid; i < n_rows * TPR; i += 256) {
+      const int r = i / TPR, c = i % TPR * 4;
+      float top = sm[0][r], sum = 0.f;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(&so[wave][(r * 16 + c16) * D + 16 * d + 4 * g]) = o[r][d];
+      for (int w = 1; w < NW; ++w) top = sm[w][r] <= top ? top : sm[w][r];
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float by = sm[w][r] == -INFINITY ? 0.f : fast_exp2(sm[w][r] - top);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(&so[w][r * D + c]);
+        sum += by * sl[w][r];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += by * y[e];
+      }
+      if (left > 0 || upto < turns) {
+        const int64_t to = ((2 * w + (first && left > 0 ? 0 : 1)) * (int64_t)p.Hk + hk) * n_rows + r;
+        *reinterpret_cast<f32x4*>(p.part_o + to * D + c) = v;
+        if (c == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * to) = make_float2(top, sum);
+        continue;
+      }
+      const RowOf ro = cache_row(p, unit, r);
+      const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.L + ro.i;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      *reinterpret_cast<uint2*>(at(p.out, p.so, ro) + c) =
+          make_uint2(T::pack(v[0] * inv, v[1] * inv), T::pack(v[2] * inv, v[3] * inv));
+      if (p.lse && c == 0) p.lse[row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+    turn += upto - left;
+    if (!p.shares || turn >= end) return;
+    left = 0;
+    ++b;
+    __syncthreads();                                         // the waves' sums have been read
+  }
+}
+
+// Joins the shares of key heads that several workgroups had, in their order, and writes
+// the rows of sequences without tokens; the others were written already.  A workgroup per row.
+template <class T, int D>
+__global__ __launch_bounds__(256) void cache_few_join_kernel(const CacheParams p) {
+  constexpr int TPR = D / 4, NG = 256 / TPR;
+  __shared__ f32x4 so[NG][TPR];
+  __shared__ float sm[NG], sl[NG];
+  const int n_rows = p.G * p.L, unit = blockIdx.x / n_rows, r = blockIdx.x % n_rows;
+  const RowOf ro = cache_row(p, unit, r);
+  const int64_t from = p.before[ro.b], to = p.before[ro.b + 1], total = p.before[p.B];
+  // Turn x is in share ((x + 1) shares - 1) / total.
+  const int64_t shares = total < p.shares ? total : p.shares;
+  const int w0 = from == to ? 0 : (int)(((from + 1) * shares - 1) / total);
+  const int w1 = from == to ? -1 : (int)((to * shares - 1) / total);
+  if (w0 == w1) return;
+  const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+  auto slot = [&](int w) { return ((2 * w + (w == w0 ? 1 : 0)) * (int64_t)p.Hk + unit % p.Hk) * n_rows + r; };
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int w = w0 + grp; w <= w1; w += NG) {
+    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * slot(w));
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + slot(w) * D + 4 * t);
+    const float top = ml.x <= m ? m : ml.x;
+    const float old = m == -INFINITY ? 0.f : fast_exp2(m - top), by = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top);
+    m = top;
+    l = l * old + by * ml.y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = o[j] * old + by * v[j];
+  }
+  so[grp][t] = o;
+  if (t == 0) {
+    sm[grp] = m;
+    sl[grp] = l;
   }
   __syncthreads();
-  constexpr int TPR = D / 4;
-  for (int i = tid; i < n_rows * TPR; i += 256) {
-    const int r = i / TPR, c = i % TPR * 4;
-    float top = sm[0][r], sum = 0.f;
+  if (grp != 0) return;
 #pragma unroll
-    for (int w = 1; w < NW; ++w) top = sm[w][r] <= top ? top : sm[w][r];
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int x = 1; x < NG; ++x) m = sm[x] <= m ? m : sm[x];
+  l = 0.f;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float by = sm[w][r] == -INFINITY ? 0.f : fast_exp2(sm[w][r] - top);
-      const f32x4 y = *reinterpret_cast<const f32x4*>(&so[w][r * D + c]);
-      sum += by * sl[w][r];
+  for (int x = 0; x < NG; ++x) {
+    const float w = sm[x] == -INFINITY ? 0.f : fast_exp2(sm[x] - m);
+    const f32x4 v = so[x][t];
+    l += w * sl[x];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += by * y[e];
-    }
-    const RowOf ro = cache_row(p, unit, r);
-    const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.L + ro.i;
-    if (p.chunks > 1) {
-      const int64_t to = (int64_t)range * p.B * p.H * p.L + row;
-      *reinterpret_cast<f32x4*>(p.part_o + to * D + c) = v;
-      if (c == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * to) = make_float2(top, sum);
-      continue;
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    *reinterpret_cast<uint2*>(at(p.out, p.so, ro) + c) =
-        make_uint2(T::pack(v[0] * inv, v[1] * inv), T::pack(v[2] * inv, v[3] * inv));
-    if (p.lse && c == 0) p.lse[row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    for (int j = 0; j < 4; ++j) o[j] += w * v[j];
   }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  *reinterpret_cast<uint2*>(at(p.out, p.so, ro) + 4 * t) =
+      make_uint2(T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv));
+  if (p.lse && t == 0) p.lse[((int64_t)ro.b * p.H + ro.h) * p.L + ro.i] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // Many rows: 128 of a key head, four waves of 32, over tiles of 64 keys that are
@@ -291,7 +464,7 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
   constexpr int PER = D / 64;                              // 16-byte loads of a thread, for keys and for values
   __shared__ __attribute__((aligned(16))) u16 sk[2][D / 8 * KP];
   __shared__ __attribute__((aligned(16))) u16 sv[2][64 * D];
-  __shared__ __attribute__((aligned(16))) float scale[2][4];   // of the keys' sixteens; below 0: not there
+  __shared__ __attribute__((aligned(16))) float scale[2][4];   // factors on the scores of the keys' sixteens; below 0: not there
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
   const int n_rows = p.G * p.L, n_rt = (n_rows + 127) / 128;
@@ -320,23 +493,28 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
   // Thread's piece j is of sixteen number (tid + 256 j) / D of the tile, for keys and values.
   u32x4 rk[PER], rv[PER];
   float ks[PER], vs[PER];
-  int live[PER];
+  int live[PER], id[PER];
+  const int six0 = wave * 64 / D;
+  auto look = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int pos = k0 + t * 64 + (six0 + 256 * j / D) * 16;
+      id[j] = p.c.table[b * p.c.table_stride + ((pos < len.n - 1 ? pos : len.n - 1) >> shift)];
+    }
+  };
+  // What is not there is read from the pool's first page and masked.
   auto fetch = [&](int t) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const int piece = tid + 256 * j, pos = k0 + t * 64 + __builtin_amdgcn_readfirstlane(piece / D) * 16;
-      const int id = pos < len.n ? page_at(p.c, b, pos >> shift) : -1;
-      rk[j] = rv[j] = u32x4{0, 0, 0, 0};
-      ks[j] = -1.f;
-      vs[j] = 1.f;
-      live[j] = 0;
-      if (id < 0) continue;
-      const int64_t a = (int64_t)id * p.Hk + hk, base = (a << shift) * D + (pos & mask) * D + piece % D * 16;
+      const int pos = k0 + t * 64 + (six0 + 256 * j / D) * 16;
+      const bool there = pos < len.n && (uint32_t)id[j] < (uint32_t)p.c.pages;
+      const int64_t a = (int64_t)(there ? id[j] : 0) * p.Hk + hk;
+      const int64_t base = (a << shift) * D + (pos & mask) * D + (tid + 256 * j) % D * 16;
       rk[j] = *reinterpret_cast<const u32x4*>(p.c.k + base);
       rv[j] = *reinterpret_cast<const u32x4*>(p.c.v + base);
       ks[j] = p.c.k_scale[a];
       vs[j] = p.c.v_scale[a];
-      live[j] = len.n - pos < 16 ? len.n - pos : 16;
+      live[j] = there ? (len.n - pos < 16 ? len.n - pos : 16) : 0;
     }
   };
   auto put = [&](int slot) {
@@ -350,11 +528,13 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
       if (live[j] < 16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) rv[j][i] &= first_bytes(live[j] - 4 * i);
+        if (live[j] <= 0) vs[j] = 1.f;                     // no page's scale, and zeros
       }
       u16* v = sv[slot] + (six * 2 * D + in) * 8;
       *reinterpret_cast<bf16x8*>(v) = decode8<BF16>(rv[j][0], rv[j][2], vs[j]);
       *reinterpret_cast<bf16x8*>(v + D * 8) = decode8<BF16>(rv[j][1], rv[j][3], vs[j]);
-      if (in == 0) scale[slot][six] = ks[j];
+      // At least 2^-126, so that times minus infinity it hides.
+      if (in == 0) scale[slot][six] = live[j] > 0 ? fmaxf(ks[j] * p.sl2, 0x1p-126f) : -1.f;
     }
   };
 
@@ -368,7 +548,11 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
     w.b = cache_row(p, unit, w.b_ok ? x + 16 : 0);
     return w;
   };
-  if (nt > 0) fetch(0);
+  if (nt > 0) {
+    look(0);
+    fetch(0);
+    look(1);
+  }
   {
     const TwoRows w = two(lane);
     load_tile<T, D>(at(p.q, p.sq, w.a), w.a_ok, at(p.q, p.sq, w.b), w.b_ok, lane, qf);
@@ -382,7 +566,10 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
 
   for (int t = 0; t < nt; ++t) {
     const int slot = t & 1, key0 = k0 + t * 64;
-    if (t + 1 < nt) fetch(t + 1);
+    if (t + 1 < nt) {
+      fetch(t + 1);
+      look(t + 2);
+    }
     if (key0 < most) {
       const f32x4 a4 = *reinterpret_cast<const f32x4*>(scale[slot]);
       f32x16 x[2];
@@ -394,56 +581,61 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
           x[h] = T::mfma(*reinterpret_cast<const typename T::x8*>(sk[slot] + (row_chunk(s) + 2 * hw) * KP +
                                                                   (32 * h + c32) * 8), qf[s], x[h]);
       }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[h][e] *= a4[2 * h + (e >> 3)] * p.sl2;
       const bool gone = !(a4[0] >= 0.f && a4[1] >= 0.f && a4[2] >= 0.f && a4[3] >= 0.f);
       if (key0 + 64 > fewest || gone) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (key0 + 32 * h + 8 * (e >> 2) + 4 * hw + (e & 3) >= seen || a4[2 * h + (e >> 3)] < 0.f) x[h][e] = -INFINITY;
+            // Minus infinity, once times the factor.
+            if (key0 + 32 * h + 8 * (e >> 2) + 4 * hw + (e & 3) >= seen || a4[2 * h + (e >> 3)] < 0.f)
+              x[h][e] = a4[2 * h + (e >> 3)] < 0.f ? INFINITY : -INFINITY;
       }
-      float top = -INFINITY;
+      bf16x8 w[4], rest[4];
+      auto weigh = [&]() {
+        const float ref = m == -INFINITY ? 0.f : -m;
+        float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int i = 0; i < 4; ++i) {
+          u32x4 hi, lo;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = vmax(top, x[h][e]);
-      top = both_halves_max(top);
-      if (__any(!(top <= m + kAbove))) {
-        const float to = top <= m ? m : top;
-        const float by = to == -INFINITY ? 1.f : fast_exp2(m - to);
-        m = to;
+          for (int e = 0; e < 8; e += 2) {
+            const float c = fast_exp2(fmaf(x[i >> 1][(i & 1) * 8 + e], a4[i], ref));
+            const float d = fast_exp2(fmaf(x[i >> 1][(i & 1) * 8 + e + 1], a4[i], ref));
+            s0 += c;
+            s1 += d;
+            uint32_t left = 0;
+            hi[e >> 1] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
+            lo[e >> 1] = left;
+          }
+          w[i] = __builtin_bit_cast(bf16x8, hi);
+          rest[i] = __builtin_bit_cast(bf16x8, lo);
+        }
+        return s0 + s1;
+      };
+      float sum = weigh();
+      const bool need = !(both_halves_max(sum) <= kSumLimit) || (m == -INFINITY && key0 < seen);
+      if (__any(need)) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float six = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) six = vmax(six, x[i >> 1][(i & 1) * 8 + e] * a4[i]);
+          top = vmax(top, six);
+        }
+        top = both_halves_max(top);
+        const bool move = need && !(top <= m);             // NaN too: the row becomes NaN
+        const float by = move ? fast_exp2(m - top) : 1.f;
+        if (move) m = top;
         l *= by;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[d][e] *= by;
+        sum = weigh();
       }
-      const float ref = m == -INFINITY ? 0.f : m;
-      float s0 = 0.f, s1 = 0.f;
-      bf16x8 w[4], rest[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4 hi[2], lo[2];
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const float c = fast_exp2(x[h][e] - ref), d = fast_exp2(x[h][e + 1] - ref);
-          s0 += c;
-          s1 += d;
-          uint32_t left = 0;
-          hi[e >> 3][(e & 7) >> 1] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
-          lo[e >> 3][(e & 7) >> 1] = left;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          w[2 * h + i] = __builtin_bit_cast(bf16x8, hi[i]);
-          rest[2 * h + i] = __builtin_bit_cast(bf16x8, lo[i]);
-        }
-      }
-      l += s0 + s1;
+      l += sum;
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -525,27 +717,48 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheParams p) {
   if (p.lse && t == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+namespace {
+int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
+}  // namespace
+
 CachePlan plan_cache_attn(const CacheParams& p) {
   CachePlan c{};
   const int64_t units = (int64_t)p.B * p.Hk, rows = (int64_t)p.G * p.L, keys = (int64_t)p.c.max_pages * p.c.page;
   c.few = rows <= kFewRows;
-  const int64_t tiles = units * (c.few ? 1 : (rows + 127) / 128);
-  const int64_t step = c.few ? 256 : 64;                   // keys of a workgroup's turn
-  const int64_t turns = (keys + step - 1) / step;
-  int64_t n = tiles > 0 ? (c.few ? 1024 : 512) / tiles : 1;    // ranges that fill the chip
-  if (!c.few && n < 2) n = 1;
-  const int64_t least = c.few ? 1 : 4;                     // turns of a range
-  n = n < turns / least ? n : turns / least;
+  c.chunks = 1;
+  c.chunk = 1 << 28;
+  if (c.few) {
+    // The last-level cache has 256 MB; from 192 on (217 MB: 42.6 and 38.4 us, 134 MB: 23.0 and 27.5).
+    c.bypass = units * keys * 2 * p.D >= (int64_t)192 << 20;
+    const int64_t turns = (keys + 255) / 256;
+    if (turns > 8) {
+      const int64_t n = p.Hk < 256 ? 256 / p.Hk : 1, most = p.B * turns;
+      c.shares = (int)(n < most ? n : most);
+      c.part_ml = up256(2 * c.shares * p.Hk * rows * p.D * 4);
+      c.before = c.part_ml + up256(2 * c.shares * p.Hk * rows * 8);
+      c.bytes = c.before + up256(((int64_t)p.B + 1) * 8);
+    }
+    return c;
+  }
+  const int64_t tiles = units * ((rows + 127) / 128), turns = (keys + 63) / 64;
+  int64_t n = tiles > 0 ? 512 / tiles : 1;                 // ranges that fill the chip
+  n = n < turns / 4 ? n : turns / 4;
   n = n < 1 ? 1 : n;
   const int64_t each = turns == 0 ? 1 : (turns + n - 1) / n;
-  c.chunk = (int)(each * step < 0x7FFFFF00 ? each * step : 0x7FFFFF00);
-  c.chunks = turns == 0 ? 1 : (int)((turns + each - 1) / each);
+  if (n > 1) c.chunk = (int)(each * 64);
+  c.chunks = n > 1 ? (int)((turns + each - 1) / each) : 1;
   if (c.chunks > 1) {
     const int64_t all = (int64_t)c.chunks * p.B * p.H * p.L;
-    c.part_ml = (all * p.D * 4 + 255) / 256 * 256;
-    c.bytes = c.part_ml + (all * 8 + 255) / 256 * 256;
+    c.part_ml = up256(all * p.D * 4);
+    c.bytes = c.part_ml + up256(all * 8);
   }
   return c;
+}
+
+template <class T, int D, int NQ>
+static void run_few(const CacheParams& p, bool bypass, hipStream_t st) {
+  if (bypass) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, true>), dim3(p.n_wg), dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, false>), dim3(p.n_wg), dim3(256), 0, st, p);
 }
 
 template <class T, int D>
@@ -553,10 +766,17 @@ static hipError_t run_attn(CacheParams p, const CachePlan& c, hipStream_t st) {
   const int64_t rows = (int64_t)p.G * p.L, units = (int64_t)p.B * p.Hk;
   p.chunk = c.chunk;
   p.chunks = c.chunks;
-  p.n_wg = (int)(units * p.chunks * (c.few ? 1 : (rows + 127) / 128));
-  if (!c.few) hipLaunchKernelGGL((cache_rows_kernel<T, D>), dim3(p.n_wg), dim3(256), 0, st, p);
-  else if (rows <= 16) hipLaunchKernelGGL((cache_few_kernel<T, D, 1>), dim3(p.n_wg), dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((cache_few_kernel<T, D, 2>), dim3(p.n_wg), dim3(256), 0, st, p);
+  p.shares = c.shares;
+  if (c.few) {
+    p.n_wg = (c.shares ? c.shares : p.B) * p.Hk;
+    if (rows <= 16) run_few<T, D, 1>(p, c.bypass, st);
+    else run_few<T, D, 2>(p, c.bypass, st);
+    if (p.shares)
+      hipLaunchKernelGGL((cache_few_join_kernel<T, D>), dim3((uint32_t)(units * rows)), dim3(256), 0, st, p);
+    return hipGetLastError();
+  }
+  p.n_wg = (int)(units * p.chunks * ((rows + 127) / 128));
+  hipLaunchKernelGGL((cache_rows_kernel<T, D>), dim3(p.n_wg), dim3(256), 0, st, p);
   if (p.chunks > 1)
     hipLaunchKernelGGL((cache_join_kernel<T, D>), dim3((uint32_t)(units * rows)), dim3(256), 0, st, p);
   return hipGetLastError();
