@@ -451,91 +451,190 @@ __global__ __launch_bounds__(256) void cache_few_join_kernel(const CacheParams p
   if (p.lse && t == 0) p.lse[((int64_t)ro.b * p.H + ro.h) * p.L + ro.i] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Many rows: 128 of a key head, four waves of 32, over tiles of 64 keys that are
-// turned into 16 bits once for all of them on their way to LDS: raw codes of the
-// next tile are loaded into registers while this one is worked on.
+// Many rows: 32 NW of a key head, over tiles of 64 keys that are turned into 16 bits
+// once for all of them on their way to LDS: raw codes are loaded into registers two
+// tiles ahead (values: one), and written while an earlier tile is worked on.
 //   keys: 16-byte pieces (8 channels) of the tile's 64 keys side by side, a piece
 //   and one further apart each time, so that neither way meets a bank twice;
 //   values: pieces of 8 tokens of a channel, in the order of the weights' places
 //   in the second product, channels side by side.
+// Every place that a lane reads is its own base plus a constant.
+constexpr int kKeyPiece = 64 * 8 + 8;                      // elements from a piece of the keys to the next
+template <int D>
+constexpr int kRowWaves = D / 16;
+
+// One step over tiles that every row sees whole: the scores of the next tile, the
+// weights of this one, the output of the one before, in slots of one MFMA and a share of
+// the weights' three stages (argument, exponential, rounding and sum), each a slot after
+// the one it needs; a fence closes the slot, so that the matrix pipe and the vector units work side
+// by side within a wave.  Scores and outputs alternate; operands are read two slots ahead.
+template <int D, typename Hook>
+__device__ __forceinline__ void rows_step(Hook&& hook, const u16* k, const u16* v, const bf16x8 (&qf)[D / 16],
+                                          const f32x16 (&s_cur)[2], const f32x4& a, float mc,
+                                          const bf16x8 (&p_prev)[4], f32x16 (&s_next)[2], bf16x8 (&p_cur)[4],
+                                          f32x16 (&o)[D / 32], float& sum) {
+  constexpr int NK = D / 16, ND = D / 32, NM = 2 * NK + 4 * ND, PER = 32 / NM, AHEAD = 2;
+  static_assert(2 * NK == 4 * ND && 32 % NM == 0, "slots alternate and share the weights evenly");
+  bf16x8 op[NM];
+  auto fetch = [&](int i) {
+    const int j = i >> 1;
+    if ((i & 1) == 0) op[i] = *reinterpret_cast<const bf16x8*>(k + row_chunk(j % NK) * kKeyPiece + j / NK * 256);
+    else op[i] = *reinterpret_cast<const bf16x8*>(v + (2 * (j / ND) * D + 32 * (j % ND)) * 8);
+  };
+  auto mfma = [&](int i) {
+    const int j = i >> 1;
+    if ((i & 1) == 0) s_next[j / NK] = mfma32(op[i], qf[j % NK], j % NK == 0 ? f32x16{} : s_next[j / NK]);
+    else o[j % ND] = mfma32(op[i], p_prev[j / ND], o[j % ND]);
+  };
+  float arg[32], ex[32], s0 = 0.f, s1 = 0.f;
+  auto stage_arg = [&](int i) {
+#pragma unroll
+    for (int e = i * PER; e < (i + 1) * PER; ++e) {
+      arg[e] = fmaf(s_cur[e >> 4][e & 15], a[e >> 3], -mc);
+      pin(arg[e]);
+    }
+  };
+  auto stage_exp = [&](int i) {
+#pragma unroll
+    for (int e = i * PER; e < (i + 1) * PER; ++e) {
+      ex[e] = fast_exp2(arg[e]);
+      pin(ex[e]);
+    }
+  };
+  auto stage_sum = [&](int i) {
+#pragma unroll
+    for (int e = i * PER; e < (i + 1) * PER; ++e)
+      if (e & 1) {
+        bf16x2 pr = {(__bf16)ex[e - 1], (__bf16)ex[e]};
+        pin(pr);
+        p_cur[e >> 3][(e & 7) - 1] = pr[0];
+        p_cur[e >> 3][e & 7] = pr[1];
+        s0 += ex[e - 1];
+        s1 += ex[e];
+        pin(s0);
+        pin(s1);
+      }
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(i);
+#pragma unroll
+  for (int i = 0; i < NM; ++i) {
+    if (i + AHEAD < NM) fetch(i + AHEAD);
+    mfma(i);
+    hook(i);
+    stage_arg(i);
+    if (i >= 1) stage_exp(i - 1);
+    if (i >= 2) stage_sum(i - 2);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  stage_exp(NM - 1);
+  stage_sum(NM - 2);
+  stage_sum(NM - 1);
+  sum = s0 + s1;
+}
+
+// A barrier that waits for LDS alone: loads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);                      // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 template <class T, int D>
-__global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p) {
-  constexpr int KP = 64 * 8 + 8;                           // elements from a piece of the keys to the next
-  constexpr int PER = D / 64;                              // 16-byte loads of a thread, for keys and for values
+__global__ __launch_bounds__(64 * kRowWaves<D>, D == 128 ? 1 : 2) void cache_rows_kernel(const CacheParams p) {
+  constexpr int NW = kRowWaves<D>, NR = 32 * NW, KP = kKeyPiece;
+  static_assert(64 * NW == 4 * D, "a thread has one 16-byte piece of a tile's keys and one of its values");
   __shared__ __attribute__((aligned(16))) u16 sk[2][D / 8 * KP];
   __shared__ __attribute__((aligned(16))) u16 sv[2][64 * D];
-  __shared__ __attribute__((aligned(16))) float scale[2][4];   // factors on the scores of the keys' sixteens; below 0: not there
+  __shared__ __attribute__((aligned(16))) float scale[4][4];   // factors on the scores of a tile's sixteens; below 0: not there
+  __shared__ int again;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int hw = lane >> 5, c32 = lane & 31;
-  const int n_rows = p.G * p.L, n_rt = (n_rows + 127) / 128;
-  const int lid = xcd_remap(blockIdx.x, p.n_wg);
-  const int unit = lid / (n_rt * p.chunks), range = lid / n_rt % p.chunks, rt = n_rt - 1 - lid % n_rt;
+  const int n_rows = p.G * p.L, n_rt = (n_rows + NR - 1) / NR;
+  // All units' longest row tiles come first, and the short ones fill the gaps.
+  const int around = p.n_wg / n_rt, lid = xcd_remap(blockIdx.x % around, around);
+  const int unit = lid / p.chunks, range = lid % p.chunks, rt = n_rt - 1 - blockIdx.x / around;
   const int b = unit / p.Hk, hk = unit % p.Hk;
   const Lens len(p, b);
   if (range > 0 && range * p.chunk >= len.n) return;
-  const int rw = rt * 128 + wave * 32, r = rw + c32;
-  const RowOf ro = cache_row(p, unit, r < n_rows ? r : 0);
-  const int seen = r < n_rows ? len.seen(p, ro.i) : 0;
-  // The most keys that a row of this tile, and of this wave, sees; the fewest of this wave.
-  const int last = rt * 128 + 127 < n_rows ? rt * 128 + 127 : n_rows - 1;
-  auto most_of = [&](int from, int to) {                   // rows [from, to]
+  const int r0 = rt * NR, rw = r0 + wave * 32, r = rw + c32;
+  const bool ok = r < n_rows;
+  const RowOf ro = cache_row(p, unit, ok ? r : 0);
+  const int seen = ok ? len.seen(p, ro.i) : 0;
+  // The most keys that a row of [from, to] sees.
+  auto most_of = [&](int from, int to) {
     const int i = to / p.G < len.q ? to / p.G : len.q - 1;
     return from > to || i < from / p.G ? 0 : len.seen(p, i);
   };
-  const int end = most_of(rt * 128, last);
-  const int rl = rw + 31 < n_rows ? rw + 31 : n_rows - 1;
-  const int most = most_of(rw, rl);
-  const int fewest = rw + 31 < n_rows && rl / p.G < len.q ? len.seen(p, rw / p.G) : 0;
+  const int end = most_of(r0, r0 + NR < n_rows ? r0 + NR - 1 : n_rows - 1);
+  const int most = most_of(rw, rw + 32 < n_rows ? rw + 31 : n_rows - 1);
   const int k0 = range * p.chunk, k1 = end - k0 < p.chunk ? end : k0 + p.chunk;
   const int nt = k1 > k0 ? (k1 - k0 + 63) / 64 : 0;
+  // Tiles that all rows which see anything see whole: the first row sees the fewest.  (Rows behind
+  // the last query, and behind the last row, are worked on like it and count for nothing.)
+  const int fewest = len.seen(p, r0 / p.G) - k0;
+  // They are taken in pairs.
+  int whole = fewest <= 0 ? 0 : (fewest / 64 < nt ? fewest / 64 : nt) & ~1;
+  if (T::kHalf) whole = 0;
 
   const int shift = 31 - __builtin_clz(p.c.page), mask = p.c.page - 1;
-  // Thread's piece j is of sixteen number (tid + 256 j) / D of the tile, for keys and values.
-  u32x4 rk[PER], rv[PER];
-  float ks[PER], vs[PER];
-  int live[PER], id[PER];
-  const int six0 = wave * 64 / D;
+  // This thread's piece of a tile is of sixteen number `six`, for keys and for values alike.
+  const int six = wave * 64 / D, in = tid % D;
+  // What the page table says of that sixteen in 64 tiles (a lane each) and the 64 after them.
   auto look = [&](int t) {
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int pos = k0 + t * 64 + (six0 + 256 * j / D) * 16;
-      id[j] = p.c.table[b * p.c.table_stride + ((pos < len.n - 1 ? pos : len.n - 1) >> shift)];
-    }
+    const int pos = k0 + (t + lane) * 64 + six * 16;
+    return p.c.table[b * p.c.table_stride + ((pos < len.n - 1 ? pos : len.n - 1) >> shift)];
   };
-  // What is not there is read from the pool's first page and masked.
-  auto fetch = [&](int t) {
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int pos = k0 + t * 64 + (six0 + 256 * j / D) * 16;
-      const bool there = pos < len.n && (uint32_t)id[j] < (uint32_t)p.c.pages;
-      const int64_t a = (int64_t)(there ? id[j] : 0) * p.Hk + hk;
-      const int64_t base = (a << shift) * D + (pos & mask) * D + (tid + 256 * j) % D * 16;
-      rk[j] = *reinterpret_cast<const u32x4*>(p.c.k + base);
-      rv[j] = *reinterpret_cast<const u32x4*>(p.c.v + base);
-      ks[j] = p.c.k_scale[a];
-      vs[j] = p.c.v_scale[a];
-      live[j] = there ? (len.n - pos < 16 ? len.n - pos : 16) : 0;
-    }
+  int pages, later, id_k, id_v, id_between;                // those of the tiles that rk and rv hold, and between
+  u32x4 rk, rv;
+  float ks, vs;
+  bool gone = false;                                       // a page that is not there
+  auto there = [&](int id, int pos) { return pos < len.n && (uint32_t)id < (uint32_t)p.c.pages; };
+  auto offset = [&](int id, int pos) {                     // in the pool, of this thread's piece
+    const int64_t a = (int64_t)(there(id, pos) ? id : 0) * p.Hk + hk;
+    return (a << shift) * D + (pos & mask) * D + in * 16;
   };
-  auto put = [&](int slot) {
+  auto turn_pages = [&](int t) {                           // before tile t is fetched
+    if ((t & 63) != 0 || t == 0) return;
+    pages = later;
+    later = look(t + 64);
+  };
+  auto fetch_k = [&](int t) {
+    id_v = id_between;
+    id_between = id_k;
+    id_k = __builtin_amdgcn_readlane(pages, t & 63);
+    const int pos = k0 + t * 64 + six * 16;
+    rk = *reinterpret_cast<const u32x4*>(p.c.k + offset(id_k, pos));
+    ks = p.c.k_scale[(int64_t)(there(id_k, pos) ? id_k : 0) * p.Hk + hk];
+  };
+  auto fetch_v = [&](int t, int id) {
+    const int pos = k0 + t * 64 + six * 16;
+    rv = *reinterpret_cast<const u32x4*>(p.c.v + offset(id, pos));
+    vs = p.c.v_scale[(int64_t)(there(id, pos) ? id : 0) * p.Hk + hk];
+  };
+  auto put_k = [&](int t, int id) {
+    const int pos = k0 + t * 64 + six * 16;
+    u16* k = sk[t & 1] + in % (D / 16) * 2 * KP + (six * 16 + in / (D / 16)) * 8;
+    *reinterpret_cast<typename T::x8*>(k) = decode8<T>(rk[0], rk[1], 1.f);
+    *reinterpret_cast<typename T::x8*>(k + KP) = decode8<T>(rk[2], rk[3], 1.f);
+    // At least 2^-126, so that times minus infinity it hides.  (Every lane of the wave has the same.)
+    const bool is = there(id, pos);
+    scale[t & 3][six] = is ? fmaxf(ks * p.sl2, 0x1p-126f) : -1.f;
+    gone = gone || (!is && pos < len.n);
+  };
+  // all: every token is there (or the tile is worked on again).
+  auto put_v = [&](auto all, int t, int id) {
+    const int pos = k0 + t * 64 + six * 16, live = there(id, pos) ? len.n - pos : 0;
+    float by = vs;
+    if (!all && live < 16) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int piece = tid + 256 * j, six = piece / D, in = piece % D;
-      const int key = six * 16 + in / (D / 16), c = in % (D / 16) * 2;
-      u16* k = sk[slot] + c * KP + key * 8;
-      *reinterpret_cast<typename T::x8*>(k) = decode8<T>(rk[j][0], rk[j][1], 1.f);
-      *reinterpret_cast<typename T::x8*>(k + KP) = decode8<T>(rk[j][2], rk[j][3], 1.f);
-      if (live[j] < 16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) rv[j][i] &= first_bytes(live[j] - 4 * i);
-        if (live[j] <= 0) vs[j] = 1.f;                     // no page's scale, and zeros
-      }
-      u16* v = sv[slot] + (six * 2 * D + in) * 8;
-      *reinterpret_cast<bf16x8*>(v) = decode8<BF16>(rv[j][0], rv[j][2], vs[j]);
-      *reinterpret_cast<bf16x8*>(v + D * 8) = decode8<BF16>(rv[j][1], rv[j][3], vs[j]);
-      // At least 2^-126, so that times minus infinity it hides.
-      if (in == 0) scale[slot][six] = live[j] > 0 ? fmaxf(ks[j] * p.sl2, 0x1p-126f) : -1.f;
+      for (int i = 0; i < 4; ++i) rv[i] &= first_bytes(live - 4 * i);
+      if (live <= 0) by = 1.f;                             // no page's scale, and zeros
     }
+    u16* v = sv[t & 1] + (six * 2 * D + in) * 8;
+    *reinterpret_cast<bf16x8*>(v) = decode8<BF16>(rv[0], rv[2], by);
+    *reinterpret_cast<bf16x8*>(v + D * 8) = decode8<BF16>(rv[1], rv[3], by);
   };
 
   typename T::x8 qf[D / 16];
@@ -548,41 +647,125 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
     w.b = cache_row(p, unit, w.b_ok ? x + 16 : 0);
     return w;
   };
-  if (nt > 0) {
-    look(0);
-    fetch(0);
-    look(1);
-  }
   {
     const TwoRows w = two(lane);
     load_tile<T, D>(at(p.q, p.sq, w.a), w.a_ok, at(p.q, p.sq, w.b), w.b_ok, lane, qf);
   }
   f32x16 o[D / 32];
+  float m, l;
+  const int kl = 2 * hw * KP + c32 * 8, vl = (hw * D + c32) * 8;       // this lane's places in a tile
+  auto scores = [&](int t, f32x16 (&x)[2]) {
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
-  float m = -INFINITY, l = 0.f;
-  if (nt > 0) put(0);
-  __syncthreads();
-
-  for (int t = 0; t < nt; ++t) {
-    const int slot = t & 1, key0 = k0 + t * 64;
-    if (t + 1 < nt) {
-      fetch(t + 1);
-      look(t + 2);
+    for (int h = 0; h < 2; ++h) {
+      x[h] = f32x16{};
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s)
+        x[h] = T::mfma(*reinterpret_cast<const typename T::x8*>(sk[t & 1] + kl + row_chunk(s) * KP + 256 * h), qf[s],
+                         x[h]);
     }
-    if (key0 < most) {
-      const f32x4 a4 = *reinterpret_cast<const f32x4*>(scale[slot]);
-      f32x16 x[2];
+  };
+  auto output = [&](int t, const bf16x8 (&w)[4]) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        x[h] = f32x16{};
+    for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s)
-          x[h] = T::mfma(*reinterpret_cast<const typename T::x8*>(sk[slot] + (row_chunk(s) + 2 * hw) * KP +
-                                                                  (32 * h + c32) * 8), qf[s], x[h]);
+      for (int s = 0; s < 4; ++s)
+        o[d] = mfma32(*reinterpret_cast<const bf16x8*>(sv[t & 1] + vl + (2 * s * D + 32 * d) * 8), w[s], o[d]);
+  };
+  auto rescale = [&](float by) {
+    l *= by;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] *= by;
+  };
+  auto top_of = [&](const f32x16 (&x)[2], const f32x4& a) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = vmax(top, x[h][e] * a[2 * h + (e >> 3)]);
+    return both_halves_max(top);
+  };
+
+  for (;;) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
+    m = -INFINITY;
+    l = 0.f;
+    if (nt == 0) break;
+    if (tid == 0) again = 0;
+    pages = look(0);
+    later = look(64);
+    __syncthreads();
+    id_k = id_v = id_between = 0;
+    fetch_k(0);
+    put_k(0, id_k);
+    fetch_k(1);
+    put_k(1, id_k);
+    fetch_k(2);
+    fetch_v(0, id_v);
+    int t = 0;
+    if (whole > 0) {
+      *reinterpret_cast<u32x4*>(&sv[1][tid * 16]) = u32x4{0, 0, 0, 0};     // the values before the first tile's
+      *reinterpret_cast<u32x4*>(&sv[1][tid * 16 + 8]) = u32x4{0, 0, 0, 0};
+      lds_barrier();
+      if constexpr (!T::kHalf) {
+        f32x16 s[2][2];
+        bf16x8 w[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[1][i] = bf16x8{};
+        scores(0, s[0]);
+        m = top_of(s[0], *reinterpret_cast<const f32x4*>(scale[0]));
+        bool bad = !(m < INFINITY && m > -INFINITY);
+        if (bad) m = 0.f;
+        auto step = [&](auto u) {
+          const f32x4 a = *reinterpret_cast<const f32x4*>(scale[t & 3]);
+          float sum;
+          turn_pages(t + 3);
+          rows_step<D>([&](int i) {
+            if (i == 1) put_k(t + 2, id_k);
+            if (i == 3) put_v(integral_constant<bool, true>{}, t, id_v);
+            if (i == 5) {
+              fetch_k(t + 3);
+              fetch_v(t + 1, id_v);
+            }
+          }, sk[1 - u] + kl, sv[1 - u] + vl, qf, s[u], a, m, w[1 - u], s[1 - u], w[u], o, sum);
+          // A row's sum of this tile is far above its reference: what was taken against that, this
+          // tile's weights too, moves by a power of two, exactly.
+          const float most = both_halves_max(sum);
+          if (__any(!(most <= kSumLimit))) {
+            bad = bad || !(most <= 0x1p30f);
+            const float by = most > kSumLimit ? __builtin_floorf(__builtin_amdgcn_logf(most)) : 0.f;
+            const float f = fast_exp2(-by);
+            m += by;
+            sum *= f;
+            rescale(f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) w[u][i][e] = (__bf16)((float)w[u][i][e] * f);
+          }
+          l += sum;
+          ++t;
+          lds_barrier();
+        };
+        while (t < whole) {
+          step(integral_constant<int, 0>{});
+          step(integral_constant<int, 1>{});
+        }
+        output(1, w[1]);                                   // the last tile's
+        if (bad || gone) again = 1;
       }
-      const bool gone = !(a4[0] >= 0.f && a4[1] >= 0.f && a4[2] >= 0.f && a4[3] >= 0.f);
-      if (key0 + 64 > fewest || gone) {
+    }
+    for (; t < nt; ++t) {
+      put_v(integral_constant<bool, false>{}, t, id_v);
+      fetch_v(t + 1, id_between);
+      lds_barrier();
+      const int key0 = k0 + t * 64;
+      if (key0 < most) {
+        const f32x4 a4 = *reinterpret_cast<const f32x4*>(scale[t & 3]);
+        f32x16 x[2];
+        scores(t, x);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -590,72 +773,66 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
             // Minus infinity, once times the factor.
             if (key0 + 32 * h + 8 * (e >> 2) + 4 * hw + (e & 3) >= seen || a4[2 * h + (e >> 3)] < 0.f)
               x[h][e] = a4[2 * h + (e >> 3)] < 0.f ? INFINITY : -INFINITY;
-      }
-      bf16x8 w[4], rest[4];
-      auto weigh = [&]() {
-        const float ref = m == -INFINITY ? 0.f : -m;
-        float s0 = 0.f, s1 = 0.f;
+        bf16x8 w[4], rest[4];
+        auto weigh = [&]() {
+          const float ref = m == -INFINITY ? 0.f : -m;
+          float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          u32x4 hi, lo;
+          for (int i = 0; i < 4; ++i) {
+            u32x4 hi, lo;
 #pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            const float c = fast_exp2(fmaf(x[i >> 1][(i & 1) * 8 + e], a4[i], ref));
-            const float d = fast_exp2(fmaf(x[i >> 1][(i & 1) * 8 + e + 1], a4[i], ref));
-            s0 += c;
-            s1 += d;
-            uint32_t left = 0;
-            hi[e >> 1] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
-            lo[e >> 1] = left;
+            for (int e = 0; e < 8; e += 2) {
+              const float c = fast_exp2(fmaf(x[i >> 1][(i & 1) * 8 + e], a4[i], ref));
+              const float d = fast_exp2(fmaf(x[i >> 1][(i & 1) * 8 + e + 1], a4[i], ref));
+              s0 += c;
+              s1 += d;
+              uint32_t left = 0;
+              hi[e >> 1] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
+              lo[e >> 1] = left;
+            }
+            w[i] = __builtin_bit_cast(bf16x8, hi);
+            rest[i] = __builtin_bit_cast(bf16x8, lo);
           }
-          w[i] = __builtin_bit_cast(bf16x8, hi);
-          rest[i] = __builtin_bit_cast(bf16x8, lo);
+          return s0 + s1;
+        };
+        float sum = weigh();
+        const bool need = !(both_halves_max(sum) <= kSumLimit) || (m == -INFINITY && key0 < seen);
+        if (__any(need)) {
+          const float top = top_of(x, a4);
+          const bool move = need && !(top <= m);           // NaN too: the row becomes NaN
+          const float by = move ? fast_exp2(m - top) : 1.f;
+          if (move) m = top;
+          rescale(by);
+          sum = weigh();
         }
-        return s0 + s1;
-      };
-      float sum = weigh();
-      const bool need = !(both_halves_max(sum) <= kSumLimit) || (m == -INFINITY && key0 < seen);
-      if (__any(need)) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float six = -INFINITY;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) six = vmax(six, x[i >> 1][(i & 1) * 8 + e] * a4[i]);
-          top = vmax(top, six);
-        }
-        top = both_halves_max(top);
-        const bool move = need && !(top <= m);             // NaN too: the row becomes NaN
-        const float by = move ? fast_exp2(m - top) : 1.f;
-        if (move) m = top;
-        l *= by;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[d][e] *= by;
-        sum = weigh();
+        l += sum;
+        output(t, w);
+        if (T::kHalf) output(t, rest);
       }
-      l += sum;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sv[slot] + ((2 * s + hw) * D + 32 * d + c32) * 8);
-          o[d] = mfma32(vf, w[s], o[d]);
-          if (T::kHalf) o[d] = mfma32(vf, rest[s], o[d]);
-        }
+      lds_barrier();
+      put_k(t + 2, id_k);
+      turn_pages(t + 3);
+      fetch_k(t + 3);
     }
-    if (t + 1 < nt) put(1 - slot);
+    // Scores too far above their row's first ones, or a page that is not there: once more, tile by tile.
+    lds_barrier();
+    if (whole == 0 || !again) break;
+    whole = 0;
     __syncthreads();
+  }
+  if (seen == 0) {                                         // no key, or no query
+    l = 0.f;
+    m = -INFINITY;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
   }
 
   l = both_halves_sum(l);
   const int64_t row = ((int64_t)ro.b * p.H + ro.h) * p.L + ro.i;
-  const bool ok = r < n_rows;
   if (p.chunks > 1) {
     const int64_t to = (int64_t)range * p.B * p.H * p.L + row;
     store_tile_f32<D>(o, p.part_o + to * D, ok, hw);
-    if (ok && hw == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * to) = make_float2(m, l);
+    if (ok && hw == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * to) = make_float2(l == 0.f ? -INFINITY : m, l);
     return;
   }
   const TwoRows w = two(lane);
@@ -664,52 +841,28 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const CacheParams p)
 }
 
 // Joins the ranges of a sequence's keys: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s,
-// in a fixed order.  A workgroup per row, NG groups of D / 4 threads that take every
-// NG-th range each.
+// in their order.  Ranges are few (most often two to four) and rows many, so D / 4 threads have a
+// row to themselves; bound by its bytes.
 template <class T, int D>
 __global__ __launch_bounds__(256) void cache_join_kernel(const CacheParams p) {
-  constexpr int TPR = D / 4, NG = 256 / TPR;
-  __shared__ f32x4 so[NG][TPR];
-  __shared__ float sm[NG], sl[NG];
-  const int64_t rows = (int64_t)p.B * p.H * p.L, row = blockIdx.x;
-  const int i = (int)(row % p.L), h = (int)(row / p.L % p.H), b = (int)(row / p.L / p.H);
-  const Lens len(p, b);
-  int used = (len.n + p.chunk - 1) / p.chunk;
-  used = used < 1 ? 1 : used;                              // the first range is always there
-  const int t = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+  constexpr int TPR = D / 4;
+  const int64_t rows = (int64_t)p.B * p.H * p.L, row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (row >= rows) return;
+  const int i = (int)(row % p.L), h = (int)(row / p.L % p.H), b = (int)(row / p.L / p.H), t = threadIdx.x % TPR;
+  const int n = clamp_len(p.lens[b], p.c.pages ? p.c.max_pages * p.c.page : 0);
+  const int used = n > p.chunk ? (n + p.chunk - 1) / p.chunk : 1;          // the first range is always there
   float m = -INFINITY, l = 0.f;
-  for (int s = grp; s < used; s += NG) {
-    const float x = p.part_ml[2 * (s * rows + row)];
-    m = x <= m ? m : x;
-  }
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int s = grp; s < used; s += NG) {
+  for (int s = 0; s < used; ++s) {
     const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * (s * rows + row));
     const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (s * rows + row) * D + 4 * t);
-    const float w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
-    l += w * ml.y;
+    const float top = ml.x <= m ? m : ml.x;
+    const float old = m == -INFINITY ? 0.f : fast_exp2(m - top), by = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top);
+    m = top;
+    l = l * old + by * ml.y;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] += w * v[j];
-  }
-  so[grp][t] = o;
-  if (t == 0) {
-    sm[grp] = m;
-    sl[grp] = l;
-  }
-  __syncthreads();
-  if (grp != 0) return;
-#pragma unroll
-  for (int x = 1; x < NG; ++x) m = sm[x] <= m ? m : sm[x];
-  l = 0.f;
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int x = 0; x < NG; ++x) {
-    const float w = sm[x] == -INFINITY ? 0.f : fast_exp2(sm[x] - m);
-    const f32x4 v = so[x][t];
-    l += w * sl[x];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] += w * v[j];
+    for (int j = 0; j < 4; ++j) o[j] = o[j] * old + by * v[j];
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   *reinterpret_cast<uint2*>(p.out + b * p.so.b + h * p.so.h + i * p.so.t + 4 * t) =
@@ -740,10 +893,26 @@ CachePlan plan_cache_attn(const CacheParams& p) {
     }
     return c;
   }
-  const int64_t tiles = units * ((rows + 127) / 128), turns = (keys + 63) / 64;
-  int64_t n = tiles > 0 ? 512 / tiles : 1;                 // ranges that fill the chip
-  n = n < turns / 4 ? n : turns / 4;
-  n = n < 1 ? 1 : n;
+  // Ranges of the keys, so many that the workgroups (one a CU at d 128, two at d 64) end together.
+  // A workgroup's start counts as six tiles and its sums' way through memory as eight.  Under an
+  // order the rows of a sequence that is nearly all new differ in length: the short ones fill gaps, and
+  // no more than the longest and an even share count; otherwise whole rounds do.
+  const int NR = 2 * p.D, room = p.D == 128 ? 256 : 512;
+  const int64_t tiles = units * ((rows + NR - 1) / NR), turns = (keys + 63) / 64;
+  const bool uneven = p.causal && 2 * (int64_t)p.L > keys;
+  int64_t n = 1, best = -1;
+  for (int64_t x = 1; x <= 64 && (x == 1 || turns / x >= 8); ++x) {
+    const int64_t over = 6 + (x > 1 ? 8 : 0), each = (turns + x - 1) / x + over;
+    int64_t cost = (tiles * x + room - 1) / room * each;
+    if (uneven) {
+      const int64_t share = tiles * (turns - p.L / 128 + x * over) / room + each / 4;
+      cost = share > each ? share : each;
+    }
+    if (best < 0 || cost < best) {
+      best = cost;
+      n = x;
+    }
+  }
   const int64_t each = turns == 0 ? 1 : (turns + n - 1) / n;
   if (n > 1) c.chunk = (int)(each * 64);
   c.chunks = n > 1 ? (int)((turns + each - 1) / each) : 1;
@@ -775,10 +944,11 @@ static hipError_t run_attn(CacheParams p, const CachePlan& c, hipStream_t st) {
       hipLaunchKernelGGL((cache_few_join_kernel<T, D>), dim3((uint32_t)(units * rows)), dim3(256), 0, st, p);
     return hipGetLastError();
   }
-  p.n_wg = (int)(units * p.chunks * ((rows + 127) / 128));
-  hipLaunchKernelGGL((cache_rows_kernel<T, D>), dim3(p.n_wg), dim3(256), 0, st, p);
+  p.n_wg = (int)(units * p.chunks * ((rows + 2 * D - 1) / (2 * D)));
+  hipLaunchKernelGGL((cache_rows_kernel<T, D>), dim3(p.n_wg), dim3(64 * kRowWaves<D>), 0, st, p);
   if (p.chunks > 1)
-    hipLaunchKernelGGL((cache_join_kernel<T, D>), dim3((uint32_t)(units * rows)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((cache_join_kernel<T, D>), dim3((uint32_t)((units * rows + 1024 / D - 1) / (1024 / D))), dim3(256),
+                       0, st, p);
   return hipGetLastError();
 }
 
