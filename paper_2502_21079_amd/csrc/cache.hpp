@@ -52,7 +52,7 @@ struct CachePlan {
 };
 constexpr int kFewRows = 32;
 
-CachePlan plan_cache_attn(const CacheParams& p);
+CachePlan plan_cache_attn(const CacheParams& p, bool f16);
 hipError_t launch_cache_write(CacheParams p, bool f16, hipStream_t st);
 hipError_t launch_cache_read(CacheParams p, bool f16, hipStream_t st);
 hipError_t launch_cache_attn(CacheParams p, bool f16, const CachePlan& plan, hipStream_t st);

@@ -126,7 +126,7 @@ adaspa_status adaspa_cache_read(const adaspa_cache_problem* prob, const adaspa_c
 
 size_t adaspa_cache_attn_workspace(const adaspa_cache_problem* prob) {
   if (check_cache(prob, nullptr, true, true) != ADASPA_OK) return 0;
-  const int64_t n = plan_cache_attn(params(prob, nullptr)).bytes;
+  const int64_t n = plan_cache_attn(params(prob, nullptr), prob->dtype == ADASPA_FP16).bytes;
   return n == 0 ? 16 : (size_t)n;
 }
 
@@ -140,7 +140,7 @@ adaspa_status adaspa_cache_attn(const adaspa_cache_problem* prob, const adaspa_c
   if (bad(q, rows, 16) || bad(out, rows, 16) || bad(lens, rows, 4) || bad(q_lens, false, 4) || bad(lse, false, 4))
     return ADASPA_ERR_INVALID_ARG;
   CacheParams p = params(prob, cache);
-  const CachePlan plan = plan_cache_attn(p);
+  const CachePlan plan = plan_cache_attn(p, prob->dtype == ADASPA_FP16);
   if (plan.bytes > 0 && (!workspace || workspace_bytes < (size_t)plan.bytes || ((uintptr_t)workspace & 255) != 0))
     return ADASPA_ERR_WORKSPACE;
   if (!rows) return ADASPA_OK;

@@ -460,31 +460,35 @@ __global__ __launch_bounds__(256) void cache_few_join_kernel(const CacheParams p
 //   in the second product, channels side by side.
 // Every place that a lane reads is its own base plus a constant.
 constexpr int kKeyPiece = 64 * 8 + 8;                      // elements from a piece of the keys to the next
-template <int D>
-constexpr int kRowWaves = D / 16;
+// Waves of a workgroup, 32 rows each, and workgroups of a CU.  (fp16 at d 128: its second values leave
+// registers for one wave a SIMD.)
+constexpr int row_waves(bool f16, int D) { return f16 ? 4 : D / 16; }
 
 // One step over tiles that every row sees whole: the scores of the next tile, the
 // weights of this one, the output of the one before, in slots of one MFMA and a share of
 // the weights' three stages (argument, exponential, rounding and sum), each a slot after
 // the one it needs; a fence closes the slot, so that the matrix pipe and the vector units work side
-// by side within a wave.  Scores and outputs alternate; operands are read two slots ahead.
-template <int D, typename Hook>
-__device__ __forceinline__ void rows_step(Hook&& hook, const u16* k, const u16* v, const bf16x8 (&qf)[D / 16],
+// by side within a wave.  Scores and outputs alternate (with fp16 the output takes the weights'
+// second values too); operands are read two slots ahead.  hook(i): the caller's share of slot i.
+template <class T, int D, typename Hook>
+__device__ __forceinline__ void rows_step(Hook&& hook, const u16* k, const u16* v, const typename T::x8 (&qf)[D / 16],
                                           const f32x16 (&s_cur)[2], const f32x4& a, float mc,
-                                          const bf16x8 (&p_prev)[4], f32x16 (&s_next)[2], bf16x8 (&p_cur)[4],
+                                          const bf16x8 (&p_prev)[2][4], f32x16 (&s_next)[2], bf16x8 (&p_cur)[2][4],
                                           f32x16 (&o)[D / 32], float& sum) {
   constexpr int NK = D / 16, ND = D / 32, NM = 2 * NK + 4 * ND, PER = 32 / NM, AHEAD = 2;
   static_assert(2 * NK == 4 * ND && 32 % NM == 0, "slots alternate and share the weights evenly");
-  bf16x8 op[NM];
+  u32x4 op[NM];
   auto fetch = [&](int i) {
     const int j = i >> 1;
-    if ((i & 1) == 0) op[i] = *reinterpret_cast<const bf16x8*>(k + row_chunk(j % NK) * kKeyPiece + j / NK * 256);
-    else op[i] = *reinterpret_cast<const bf16x8*>(v + (2 * (j / ND) * D + 32 * (j % ND)) * 8);
+    op[i] = *reinterpret_cast<const u32x4*>((i & 1) == 0 ? k + row_chunk(j % NK) * kKeyPiece + j / NK * 256
+                                                         : v + (2 * (j / ND) * D + 32 * (j % ND)) * 8);
   };
   auto mfma = [&](int i) {
     const int j = i >> 1;
-    if ((i & 1) == 0) s_next[j / NK] = mfma32(op[i], qf[j % NK], j % NK == 0 ? f32x16{} : s_next[j / NK]);
-    else o[j % ND] = mfma32(op[i], p_prev[j / ND], o[j % ND]);
+    if ((i & 1) == 0)
+      s_next[j / NK] = T::mfma(__builtin_bit_cast(typename T::x8, op[i]), qf[j % NK],
+                               j % NK == 0 ? f32x16{} : s_next[j / NK]);
+    else o[j % ND] = mfma32(__builtin_bit_cast(bf16x8, op[i]), p_prev[0][j / ND], o[j % ND]);
   };
   float arg[32], ex[32], s0 = 0.f, s1 = 0.f;
   auto stage_arg = [&](int i) {
@@ -505,10 +509,17 @@ __device__ __forceinline__ void rows_step(Hook&& hook, const u16* k, const u16* 
 #pragma unroll
     for (int e = i * PER; e < (i + 1) * PER; ++e)
       if (e & 1) {
-        bf16x2 pr = {(__bf16)ex[e - 1], (__bf16)ex[e]};
+        uint32_t rest = 0;
+        bf16x2 pr = __builtin_bit_cast(bf16x2, T::kHalf ? split2(ex[e - 1], ex[e], rest) : BF16::pack(ex[e - 1], ex[e]));
         pin(pr);
-        p_cur[e >> 3][(e & 7) - 1] = pr[0];
-        p_cur[e >> 3][e & 7] = pr[1];
+        p_cur[0][e >> 3][(e & 7) - 1] = pr[0];
+        p_cur[0][e >> 3][e & 7] = pr[1];
+        if constexpr (T::kHalf) {
+          bf16x2 lo = __builtin_bit_cast(bf16x2, rest);
+          pin(lo);
+          p_cur[1][e >> 3][(e & 7) - 1] = lo[0];
+          p_cur[1][e >> 3][e & 7] = lo[1];
+        }
         s0 += ex[e - 1];
         s1 += ex[e];
         pin(s0);
@@ -526,6 +537,11 @@ __device__ __forceinline__ void rows_step(Hook&& hook, const u16* k, const u16* 
     if (i >= 1) stage_exp(i - 1);
     if (i >= 2) stage_sum(i - 2);
     __builtin_amdgcn_sched_barrier(0);
+    if (T::kHalf && (i & 1)) {
+      const int j = i >> 1;
+      o[j % ND] = mfma32(__builtin_bit_cast(bf16x8, op[i]), p_prev[1][j / ND], o[j % ND]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
   stage_exp(NM - 1);
   stage_sum(NM - 2);
@@ -542,9 +558,9 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(64 * kRowWaves<D>, D == 128 ? 1 : 2) void cache_rows_kernel(const CacheParams p) {
-  constexpr int NW = kRowWaves<D>, NR = 32 * NW, KP = kKeyPiece;
-  static_assert(64 * NW == 4 * D, "a thread has one 16-byte piece of a tile's keys and one of its values");
+__global__ __launch_bounds__(64 * row_waves(T::kHalf, D), T::kHalf && D == 128 ? 1 : 2) void cache_rows_kernel(const CacheParams p) {
+  constexpr int NW = row_waves(T::kHalf, D), NR = 32 * NW, KP = kKeyPiece;
+  constexpr int PER = 4 * D / (64 * NW);                   // 16-byte pieces of a thread, of a tile's keys and of its values
   __shared__ __attribute__((aligned(16))) u16 sk[2][D / 8 * KP];
   __shared__ __attribute__((aligned(16))) u16 sv[2][64 * D];
   __shared__ __attribute__((aligned(16))) float scale[4][4];   // factors on the scores of a tile's sixteens; below 0: not there
@@ -576,19 +592,20 @@ __global__ __launch_bounds__(64 * kRowWaves<D>, D == 128 ? 1 : 2) void cache_row
   const int fewest = len.seen(p, r0 / p.G) - k0;
   // They are taken in pairs.
   int whole = fewest <= 0 ? 0 : (fewest / 64 < nt ? fewest / 64 : nt) & ~1;
-  if (T::kHalf) whole = 0;
 
   const int shift = 31 - __builtin_clz(p.c.page), mask = p.c.page - 1;
-  // This thread's piece of a tile is of sixteen number `six`, for keys and for values alike.
-  const int six = wave * 64 / D, in = tid % D;
+  // This thread's piece j of a tile, for keys and for values alike: of sixteen number six(j).
+  const int in = tid % D;
+  auto six = [&](int j) { return wave * 64 / D + j * 64 * NW / D; };
+  auto place = [&](int t, int j) { return k0 + t * 64 + six(j) * 16; };
   // What the page table says of that sixteen in 64 tiles (a lane each) and the 64 after them.
-  auto look = [&](int t) {
-    const int pos = k0 + (t + lane) * 64 + six * 16;
+  auto look = [&](int t, int j) {
+    const int pos = place(t + lane, j);
     return p.c.table[b * p.c.table_stride + ((pos < len.n - 1 ? pos : len.n - 1) >> shift)];
   };
-  int pages, later, id_k, id_v, id_between;                // those of the tiles that rk and rv hold, and between
-  u32x4 rk, rv;
-  float ks, vs;
+  int pages[PER], later[PER], id_k[PER], id_v[PER], id_between[PER];       // those of the tiles that rk and rv hold, and between
+  u32x4 rk[PER], rv[PER];
+  float ks[PER], vs[PER];
   bool gone = false;                                       // a page that is not there
   auto there = [&](int id, int pos) { return pos < len.n && (uint32_t)id < (uint32_t)p.c.pages; };
   auto offset = [&](int id, int pos) {                     // in the pool, of this thread's piece
@@ -597,44 +614,58 @@ __global__ __launch_bounds__(64 * kRowWaves<D>, D == 128 ? 1 : 2) void cache_row
   };
   auto turn_pages = [&](int t) {                           // before tile t is fetched
     if ((t & 63) != 0 || t == 0) return;
-    pages = later;
-    later = look(t + 64);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      pages[j] = later[j];
+      later[j] = look(t + 64, j);
+    }
   };
   auto fetch_k = [&](int t) {
-    id_v = id_between;
-    id_between = id_k;
-    id_k = __builtin_amdgcn_readlane(pages, t & 63);
-    const int pos = k0 + t * 64 + six * 16;
-    rk = *reinterpret_cast<const u32x4*>(p.c.k + offset(id_k, pos));
-    ks = p.c.k_scale[(int64_t)(there(id_k, pos) ? id_k : 0) * p.Hk + hk];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      id_v[j] = id_between[j];
+      id_between[j] = id_k[j];
+      id_k[j] = __builtin_amdgcn_readlane(pages[j], t & 63);
+      const int pos = place(t, j);
+      rk[j] = *reinterpret_cast<const u32x4*>(p.c.k + offset(id_k[j], pos));
+      ks[j] = p.c.k_scale[(int64_t)(there(id_k[j], pos) ? id_k[j] : 0) * p.Hk + hk];
+    }
   };
-  auto fetch_v = [&](int t, int id) {
-    const int pos = k0 + t * 64 + six * 16;
-    rv = *reinterpret_cast<const u32x4*>(p.c.v + offset(id, pos));
-    vs = p.c.v_scale[(int64_t)(there(id, pos) ? id : 0) * p.Hk + hk];
+  auto fetch_v = [&](int t, const int (&id)[PER]) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int pos = place(t, j);
+      rv[j] = *reinterpret_cast<const u32x4*>(p.c.v + offset(id[j], pos));
+      vs[j] = p.c.v_scale[(int64_t)(there(id[j], pos) ? id[j] : 0) * p.Hk + hk];
+    }
   };
-  auto put_k = [&](int t, int id) {
-    const int pos = k0 + t * 64 + six * 16;
-    u16* k = sk[t & 1] + in % (D / 16) * 2 * KP + (six * 16 + in / (D / 16)) * 8;
-    *reinterpret_cast<typename T::x8*>(k) = decode8<T>(rk[0], rk[1], 1.f);
-    *reinterpret_cast<typename T::x8*>(k + KP) = decode8<T>(rk[2], rk[3], 1.f);
-    // At least 2^-126, so that times minus infinity it hides.  (Every lane of the wave has the same.)
-    const bool is = there(id, pos);
-    scale[t & 3][six] = is ? fmaxf(ks * p.sl2, 0x1p-126f) : -1.f;
-    gone = gone || (!is && pos < len.n);
+  auto put_k = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      u16* k = sk[t & 1] + in % (D / 16) * 2 * KP + (six(j) * 16 + in / (D / 16)) * 8;
+      *reinterpret_cast<typename T::x8*>(k) = decode8<T>(rk[j][0], rk[j][1], 1.f);
+      *reinterpret_cast<typename T::x8*>(k + KP) = decode8<T>(rk[j][2], rk[j][3], 1.f);
+      // At least 2^-126, so that times minus infinity it hides.  (Every lane of the wave has the same.)
+      const bool is = there(id_k[j], place(t, j));
+      scale[t & 3][six(j)] = is ? fmaxf(ks[j] * p.sl2, 0x1p-126f) : -1.f;
+      gone = gone || (!is && place(t, j) < len.n);
+    }
   };
   // all: every token is there (or the tile is worked on again).
-  auto put_v = [&](auto all, int t, int id) {
-    const int pos = k0 + t * 64 + six * 16, live = there(id, pos) ? len.n - pos : 0;
-    float by = vs;
-    if (!all && live < 16) {
+  auto put_v = [&](auto all, int t) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) rv[i] &= first_bytes(live - 4 * i);
-      if (live <= 0) by = 1.f;                             // no page's scale, and zeros
+    for (int j = 0; j < PER; ++j) {
+      const int live = there(id_v[j], place(t, j)) ? len.n - place(t, j) : 0;
+      float by = vs[j];
+      if (!all && live < 16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rv[j][i] &= first_bytes(live - 4 * i);
+        if (live <= 0) by = 1.f;                           // no page's scale, and zeros
+      }
+      u16* v = sv[t & 1] + (six(j) * 2 * D + in) * 8;
+      *reinterpret_cast<bf16x8*>(v) = decode8<BF16>(rv[j][0], rv[j][2], by);
+      *reinterpret_cast<bf16x8*>(v + D * 8) = decode8<BF16>(rv[j][1], rv[j][3], by);
     }
-    u16* v = sv[t & 1] + (six * 2 * D + in) * 8;
-    *reinterpret_cast<bf16x8*>(v) = decode8<BF16>(rv[0], rv[2], by);
-    *reinterpret_cast<bf16x8*>(v + D * 8) = decode8<BF16>(rv[1], rv[3], by);
   };
 
   typename T::x8 qf[D / 16];
@@ -694,71 +725,77 @@ __global__ __launch_bounds__(64 * kRowWaves<D>, D == 128 ? 1 : 2) void cache_row
     l = 0.f;
     if (nt == 0) break;
     if (tid == 0) again = 0;
-    pages = look(0);
-    later = look(64);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      pages[j] = look(0, j);
+      later[j] = look(64, j);
+      id_k[j] = id_v[j] = id_between[j] = 0;
+    }
     __syncthreads();
-    id_k = id_v = id_between = 0;
     fetch_k(0);
-    put_k(0, id_k);
+    put_k(0);
     fetch_k(1);
-    put_k(1, id_k);
+    put_k(1);
     fetch_k(2);
     fetch_v(0, id_v);
     int t = 0;
     if (whole > 0) {
-      *reinterpret_cast<u32x4*>(&sv[1][tid * 16]) = u32x4{0, 0, 0, 0};     // the values before the first tile's
-      *reinterpret_cast<u32x4*>(&sv[1][tid * 16 + 8]) = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 2 * PER; ++j)                    // the values before the first tile's
+        *reinterpret_cast<u32x4*>(&sv[1][(tid + 64 * NW * j) * 8]) = u32x4{0, 0, 0, 0};
       lds_barrier();
-      if constexpr (!T::kHalf) {
-        f32x16 s[2][2];
-        bf16x8 w[2][4];
+      f32x16 s[2][2];
+      bf16x8 w[2][2][4];                                 // of two tiles: weights, and with fp16 what they leave
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[1][i] = bf16x8{};
-        scores(0, s[0]);
-        m = top_of(s[0], *reinterpret_cast<const f32x4*>(scale[0]));
-        bool bad = !(m < INFINITY && m > -INFINITY);
-        if (bad) m = 0.f;
-        auto step = [&](auto u) {
-          const f32x4 a = *reinterpret_cast<const f32x4*>(scale[t & 3]);
-          float sum;
-          turn_pages(t + 3);
-          rows_step<D>([&](int i) {
-            if (i == 1) put_k(t + 2, id_k);
-            if (i == 3) put_v(integral_constant<bool, true>{}, t, id_v);
-            if (i == 5) {
-              fetch_k(t + 3);
-              fetch_v(t + 1, id_v);
-            }
-          }, sk[1 - u] + kl, sv[1 - u] + vl, qf, s[u], a, m, w[1 - u], s[1 - u], w[u], o, sum);
-          // A row's sum of this tile is far above its reference: what was taken against that, this
-          // tile's weights too, moves by a power of two, exactly.
-          const float most = both_halves_max(sum);
-          if (__any(!(most <= kSumLimit))) {
-            bad = bad || !(most <= 0x1p30f);
-            const float by = most > kSumLimit ? __builtin_floorf(__builtin_amdgcn_logf(most)) : 0.f;
-            const float f = fast_exp2(-by);
-            m += by;
-            sum *= f;
-            rescale(f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) w[u][i][e] = (__bf16)((float)w[u][i][e] * f);
+      for (int i = 0; i < 4; ++i) w[1][0][i] = w[1][1][i] = bf16x8{};
+      scores(0, s[0]);
+      m = top_of(s[0], *reinterpret_cast<const f32x4*>(scale[0]));
+      bool bad = !(m < INFINITY && m > -INFINITY);
+      if (bad) m = 0.f;
+      auto step = [&](auto u) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(scale[t & 3]);
+        float sum;
+        turn_pages(t + 3);
+        rows_step<T, D>([&](int i) {
+          if (i == 1) put_k(t + 2);
+          if (i == 3) put_v(integral_constant<bool, true>{}, t);
+          if (i == 5) {
+            fetch_k(t + 3);
+            fetch_v(t + 1, id_v);
           }
-          l += sum;
-          ++t;
-          lds_barrier();
-        };
-        while (t < whole) {
-          step(integral_constant<int, 0>{});
-          step(integral_constant<int, 1>{});
+        }, sk[1 - u] + kl, sv[1 - u] + vl, qf, s[u], a, m, w[1 - u], s[1 - u], w[u], o, sum);
+        // A row's sum of this tile is far above its reference: what was taken against that, this
+        // tile's weights too, moves by a power of two, exactly.
+        const float most = both_halves_max(sum);
+        if (__any(!(most <= kSumLimit))) {
+          bad = bad || !(most <= 0x1p30f);
+          const float by = most > kSumLimit ? __builtin_floorf(__builtin_amdgcn_logf(most)) : 0.f;
+          const float f = fast_exp2(-by);
+          m += by;
+          sum *= f;
+          rescale(f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              w[u][0][i][e] = (__bf16)((float)w[u][0][i][e] * f);
+              if (T::kHalf) w[u][1][i][e] = (__bf16)((float)w[u][1][i][e] * f);
+            }
         }
-        output(1, w[1]);                                   // the last tile's
-        if (bad || gone) again = 1;
+        l += sum;
+        ++t;
+        lds_barrier();
+      };
+      while (t < whole) {
+        step(integral_constant<int, 0>{});
+        step(integral_constant<int, 1>{});
       }
+      output(1, w[1][0]);                                // the last tile's
+      if (T::kHalf) output(1, w[1][1]);
+      if (bad || gone) again = 1;
     }
     for (; t < nt; ++t) {
-      put_v(integral_constant<bool, false>{}, t, id_v);
+      put_v(integral_constant<bool, false>{}, t);
       fetch_v(t + 1, id_between);
       lds_barrier();
       const int key0 = k0 + t * 64;
@@ -810,7 +847,7 @@ __global__ __launch_bounds__(64 * kRowWaves<D>, D == 128 ? 1 : 2) void cache_row
         if (T::kHalf) output(t, rest);
       }
       lds_barrier();
-      put_k(t + 2, id_k);
+      put_k(t + 2);
       turn_pages(t + 3);
       fetch_k(t + 3);
     }
@@ -874,7 +911,7 @@ namespace {
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 }  // namespace
 
-CachePlan plan_cache_attn(const CacheParams& p) {
+CachePlan plan_cache_attn(const CacheParams& p, bool f16) {
   CachePlan c{};
   const int64_t units = (int64_t)p.B * p.Hk, rows = (int64_t)p.G * p.L, keys = (int64_t)p.c.max_pages * p.c.page;
   c.few = rows <= kFewRows;
@@ -897,7 +934,7 @@ CachePlan plan_cache_attn(const CacheParams& p) {
   // A workgroup's start counts as six tiles and its sums' way through memory as eight.  Under an
   // order the rows of a sequence that is nearly all new differ in length: the short ones fill gaps, and
   // no more than the longest and an even share count; otherwise whole rounds do.
-  const int NR = 2 * p.D, room = p.D == 128 ? 256 : 512;
+  const int NR = 32 * row_waves(f16, p.D), room = p.D == 128 ? 256 : 512;
   const int64_t tiles = units * ((rows + NR - 1) / NR), turns = (keys + 63) / 64;
   const bool uneven = p.causal && 2 * (int64_t)p.L > keys;
   int64_t n = 1, best = -1;
@@ -944,8 +981,9 @@ static hipError_t run_attn(CacheParams p, const CachePlan& c, hipStream_t st) {
       hipLaunchKernelGGL((cache_few_join_kernel<T, D>), dim3((uint32_t)(units * rows)), dim3(256), 0, st, p);
     return hipGetLastError();
   }
-  p.n_wg = (int)(units * p.chunks * ((rows + 2 * D - 1) / (2 * D)));
-  hipLaunchKernelGGL((cache_rows_kernel<T, D>), dim3(p.n_wg), dim3(64 * kRowWaves<D>), 0, st, p);
+  constexpr int NW = row_waves(T::kHalf, D);
+  p.n_wg = (int)(units * p.chunks * ((rows + 32 * NW - 1) / (32 * NW)));
+  hipLaunchKernelGGL((cache_rows_kernel<T, D>), dim3(p.n_wg), dim3(64 * NW), 0, st, p);
   if (p.chunks > 1)
     hipLaunchKernelGGL((cache_join_kernel<T, D>), dim3((uint32_t)((units * rows + 1024 / D - 1) / (1024 / D))), dim3(256),
                        0, st, p);
