@@ -51,10 +51,13 @@ __device__ __forceinline__ RowOf cache_row(const CacheParams& p, int unit, int r
 }
 
 // Keys and queries of sequence b.
+__device__ __forceinline__ int key_count(const CacheParams& p, int b) {
+  return p.c.pages ? clamp_len(p.lens[b], p.c.max_pages * p.c.page) : 0;
+}
 struct Lens {
   int n, q;                                              // keys; queries, the last q of the positions
   __device__ __forceinline__ Lens(const CacheParams& p, int b) {
-    n = p.c.pages ? clamp_len(__builtin_amdgcn_readfirstlane(p.lens[b]), p.c.max_pages * p.c.page) : 0;
+    n = __builtin_amdgcn_readfirstlane(key_count(p, b));
     q = p.new_lens ? clamp_len(__builtin_amdgcn_readfirstlane(p.new_lens[b]), p.L) : p.L;
   }
   // How many keys query i sees.
@@ -86,7 +89,7 @@ struct Turns {
   __device__ __forceinline__ Turns(const CacheParams& p, int tid, int wave, int lane, int w, int* place) {
     __shared__ int64_t sums[4];
     const int each = (p.B + 255) / 256, b0 = tid * each, b1 = b0 + each < p.B ? b0 + each : p.B;
-    auto turns = [&](int b) { return (clamp_len(p.lens[b], p.c.max_pages * p.c.page) + 255) / 256; };
+    auto turns = [&](int b) { return (key_count(p, b) + 255) / 256; };
     int64_t mine = 0;
     for (int b = b0; b < b1; ++b) mine += turns(b);
     int64_t upto = mine;                                   // of this wave's lanes up to this one
@@ -131,22 +134,24 @@ struct Turns {
 // neighbouring tokens, whose values of one channel lie side by side in the cache.
 // So neither operand passes through LDS, and a block's loads are 16 bytes a lane.
 //
-// Work is counted in turns, 256 keys, a block for each wave.  With p.shares, workgroup
-// (w, key head) takes an equal share of the turns of all samples in their order, whatever their
+// Work is counted in turns, 256 keys, a block for each wave.  SHARED: workgroup (w, key head)
+// takes an equal share of the turns of all samples in their order, whatever their
 // lengths; where a share ends inside a sequence, its sums go to the workspace (place 2 w for
 // what begins inside one, 2 w + 1 for what begins with one) and cache_few_join_kernel joins
-// them.  Without, a workgroup takes a sequence.
+// them.  Else a workgroup takes a sequence: up to 2,048 keys that costs less than a second launch
+// (2 key heads of 1,984 keys, d 64, us a call: 14.4 and 17.7; 4 of 4,096, d 128: 25.8 and 19.0.  A CU
+// reads 50 GB/s, so eight waves instead of four gain nothing).
 //
-// Workgroups are few (one a CU with p.shares) and every wave has one or two blocks, 16 to 32 KB, on
+// Workgroups are few (one a CU) and every wave has one or two blocks, 16 to 32 KB, on
 // their way: more of them only spread the reads over memory.  The key heads of a
 // share run side by side, since they lie side by side in a page.  BYPASS: keys and values that the
 // last-level cache could not keep until the next call are read past it.  16 sequences of up to
 // 17,664 tokens, 4 key heads of d 128 under 24, and 110,080 tokens of 24 heads, us a call: shares in
 // the order samples, key heads, turns, 512 workgroups 53 and 129; key heads side by side 51 and 128;
 // 256 workgroups 48 and 124; past the cache 46 and 113 (6.0 TB/s).
-template <class T, int D, int NQ, bool BYPASS>
-__global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_few_kernel(const CacheParams p) {
-  constexpr int NW = 4, DT = D / 16, KJ = D / 64;          // channel tiles; 16-byte pieces of a key a lane
+template <class T, int D, int NQ, bool SHARED, bool BYPASS>
+__global__ __launch_bounds__(256, D == 128 && NQ == 2 ? 1 : 2) void cache_few_kernel(const CacheParams p) {
+  constexpr int NW = 4, STEP = 64 * NW, DT = D / 16, KJ = D / 64;          // channel tiles; 16-byte pieces of a key a lane
   __shared__ __attribute__((aligned(16))) float so[NW][NQ * 16 * D];
   __shared__ float sm[NW][NQ * 16], sl[NW][NQ * 16];
   __shared__ int place[2];
@@ -156,7 +161,7 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_few_kernel(const C
   const int hk = blockIdx.x % p.Hk, w = blockIdx.x / p.Hk;
   int b = w, left = 0;                                     // sample; turns of it before this share
   int64_t turn = 0, end = 1;                               // this workgroup's share of all turns
-  if (p.shares) {
+  if constexpr (SHARED) {
     const Turns all(p, tid, wave, lane, w, place);
     if (w >= all.shares) return;
     turn = all.total * w / all.shares;
@@ -166,13 +171,13 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_few_kernel(const C
   }
   for (bool first = true;; first = false) {
     const Lens len(p, b);
-    const int turns = (len.n + 255) / 256;
-    if (p.shares && turns == 0) {                            // the next sample with keys (there is one)
+    const int turns = (len.n + STEP - 1) / STEP;
+    if (SHARED && turns == 0) {                            // the next sample with keys (there is one)
       ++b;
       continue;
     }
-    const int upto = !p.shares || turns - left <= end - turn ? turns : left + (int)(end - turn);
-    const int k0 = left * 256, k1 = upto * 256 < len.n ? upto * 256 : len.n;     // keys of this part of the share
+    const int upto = !SHARED || turns - left <= end - turn ? turns : left + (int)(end - turn);
+    const int k0 = left * STEP, k1 = upto * STEP < len.n ? upto * STEP : len.n;  // keys of this part of the share
     const int unit = b * p.Hk + hk;
 
     typename T::x8 qf[NQ][KJ][2];
@@ -208,7 +213,6 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_few_kernel(const C
     // What the table says of this wave's next 16 blocks (lane 4 i + j: sixteen j of block
     // i) and of the 16 after them, so that no load waits for another.  n > 0; behind the last
     // token the last one's page stands.
-    constexpr int STEP = 64 * NW;
     auto look = [&](int k) {
       const int pos = k + (lane >> 2) * STEP + (lane & 3) * 16;
       return p.c.table[b * p.c.table_stride + ((pos < len.n - 1 ? pos : len.n - 1) >> shift)];
@@ -361,7 +365,7 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_few_kernel(const C
     }
     __syncthreads();
     constexpr int TPR = D / 4;
-    for (int i = tid; i < n_rows * TPR; i += 256) {
+    for (int i = tid; i < n_rows * TPR; i += 64 * NW) {
       const int r = i / TPR, c = i % TPR * 4;
       float top = sm[0][r], sum = 0.f;
 #pragma unroll
@@ -375,7 +379,7 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_few_kernel(const C
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += by * y[e];
       }
-      if (left > 0 || upto < turns) {
+      if (SHARED && (left > 0 || upto < turns)) {
         const int64_t to = ((2 * w + (first && left > 0 ? 0 : 1)) * (int64_t)p.Hk + hk) * n_rows + r;
         *reinterpret_cast<f32x4*>(p.part_o + to * D + c) = v;
         if (c == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * to) = make_float2(top, sum);
@@ -389,7 +393,7 @@ __global__ __launch_bounds__(256, NQ == 1 ? 2 : 1) void cache_few_kernel(const C
       if (p.lse && c == 0) p.lse[row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
     turn += upto - left;
-    if (!p.shares || turn >= end) return;
+    if (!SHARED || turn >= end) return;
     left = 0;
     ++b;
     __syncthreads();                                         // the waves' sums have been read
@@ -886,7 +890,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheParams p) {
   const int64_t rows = (int64_t)p.B * p.H * p.L, row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
   if (row >= rows) return;
   const int i = (int)(row % p.L), h = (int)(row / p.L % p.H), b = (int)(row / p.L / p.H), t = threadIdx.x % TPR;
-  const int n = clamp_len(p.lens[b], p.c.pages ? p.c.max_pages * p.c.page : 0);
+  const int n = key_count(p, b);
   const int used = n > p.chunk ? (n + p.chunk - 1) / p.chunk : 1;          // the first range is always there
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -963,8 +967,10 @@ CachePlan plan_cache_attn(const CacheParams& p, bool f16) {
 
 template <class T, int D, int NQ>
 static void run_few(const CacheParams& p, bool bypass, hipStream_t st) {
-  if (bypass) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, true>), dim3(p.n_wg), dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, false>), dim3(p.n_wg), dim3(256), 0, st, p);
+  if (p.shares && bypass) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, true, true>), dim3(p.n_wg), dim3(256), 0, st, p);
+  else if (p.shares) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, true, false>), dim3(p.n_wg), dim3(256), 0, st, p);
+  else if (bypass) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, false, true>), dim3(p.n_wg), dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, false, false>), dim3(p.n_wg), dim3(256), 0, st, p);
 }
 
 template <class T, int D>
