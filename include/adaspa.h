@@ -546,7 +546,9 @@ adaspa_status adaspa_cache_read(const adaspa_cache_problem* prob, const adaspa_c
  *   out_i = sum_j exp(S_ij - lse_i) v_j,  lse_i = log sum_j exp(S_ij),  S_ij = scale q_i . k_j
  * The queries are their sequence's last tokens: sample b has q_lens[b] of them (NULL: len;
  * clamped to [0, len]), query i stands at lens[b] - q_lens[b] + i and, with `causal`, sees no
- * token behind that.  Rows without a token, and those from q_lens[b] on, give 0 and -inf.  lse:
+ * token behind that.  Rows without a token, and those from q_lens[b] on, give 0 and -inf.  What lies
+ * behind lens[b], on pages that are not there, or in queries from q_lens[b] on takes no part,
+ * infinities and NaN too; tokens that only the order hides from a row must be finite.  lse:
  * fp32 [B, H, len] or NULL.  The workspace is that of the prompt side's calls: scratch, 256-byte
  * aligned, of the size that the _workspace call names. */
 size_t adaspa_cache_attn_workspace(const adaspa_cache_problem* prob);

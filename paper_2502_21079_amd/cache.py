@@ -208,7 +208,8 @@ def cache_attn(q, cache: KVCache, page_table, lens, *, q_lens=None, causal: bool
     cache already; ``q_lens`` (int32 [B]) leaves sample b its first q_lens[b], the rows behind
     give 0 and an lse of -inf.  With ``causal`` query i sees the tokens up to its own place,
     without it all of the sequence's.  A row that sees no token gives 0 and -inf; tokens behind
-    lens[b], or on pages that are not in the pool, take no part, whatever is there.  ``scale``
+    lens[b], or on pages that are not in the pool, take no part, whatever is there; those that
+    only the order hides from a row must be finite, as those that it sees.  ``scale``
     defaults to 1 / sqrt(D), which values up to 0 stand for too.  ``workspace`` (at least
     :func:`cache_attn_workspace` bytes, any type) is allocated here when not given and
     needed.  Results follow the shape (the page table's width among it): how the tokens

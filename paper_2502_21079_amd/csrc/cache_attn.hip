@@ -683,7 +683,10 @@ __global__ __launch_bounds__(64 * row_waves(T::kHalf, D), T::kHalf && D == 128 ?
     return w;
   };
   {
-    const TwoRows w = two(lane);
+    TwoRows w = two(lane);
+    // What lies behind a sample's last query is not read: it may be anything.
+    w.a_ok = w.a_ok && w.a.i < len.q;
+    w.b_ok = w.b_ok && w.b.i < len.q;
     load_tile<T, D>(at(p.q, p.sq, w.a), w.a_ok, at(p.q, p.sq, w.b), w.b_ok, lane, qf);
   }
   f32x16 o[D / 32];

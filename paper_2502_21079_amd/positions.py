@@ -31,6 +31,7 @@ from .prompt import _DTYPES, _I64x3, _new, _new_strides, _steps
 __all__ = ["rotary", "rotary_bwd", "rotary_embedding", "rotary_frequencies", "rotary_magnitude"]
 
 _LAYOUTS = {"half": 0, "interleaved": 1}
+_FLOATS = {float}
 
 
 class _RotaryProblem(ctypes.Structure):
@@ -109,8 +110,7 @@ def _plan(dtype, shapes, strides, outs, freqs, layout, sections, magnitude, pos_
         raise AdaspaError(f"q and k must be [B, heads, tokens, D] and differ in heads alone, got {qs} and {ks}")
     if layout not in _LAYOUTS:
         raise AdaspaError(f"unknown layout {layout!r}: 'half' or 'interleaved'")
-    freqs = tuple(map(float, freqs))
-    sections = (len(freqs),) if sections is None else tuple(map(index, sections))
+    sections = (len(freqs),) if sections is None else sections
     if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) != len(freqs):
         raise AdaspaError(f"sections must be up to 4 numbers of pairs that add up to {len(freqs)}, got {sections}")
     if not 1 <= len(freqs) <= qs[3] // 2:
@@ -172,11 +172,12 @@ def _turn(call, q, k, freqs, layout, sections, magnitude, positions, offset, out
         offset = index(offset)
         if not -(1 << 40) < offset < 1 << 40:
             raise AdaspaError(f"offset must be below 2^40 in magnitude, got {offset}")
+    if type(freqs) is not tuple or set(map(type, freqs)) != _FLOATS:
+        freqs = tuple(map(float, freqs))              # plain numbers: a plan is kept by them
     plan = _plan(_DTYPES[q.dtype], (q.shape, None if k is None else k.shape),
                  (q.stride(), None if k is None else k.stride()),
                  (None if out is None else out.stride(), None if k_out is None else k_out.stride()),
-                 freqs if type(freqs) is tuple else tuple(freqs), layout,
-                 sections if sections is None or type(sections) is tuple else tuple(sections), float(magnitude),
+                 freqs, layout, None if sections is None else tuple(map(index, sections)), float(magnitude),
                  None if positions is None else positions.shape, None if positions is None else positions.stride())
     out = _new(q) if out is None else out
     if k is not None and k_out is None:
@@ -254,7 +255,7 @@ def rotary_embedding(q, k, freqs, *, layout: str = "half", sections=None, magnit
                      offset: Union[int, torch.Tensor] = 0):
     """What :func:`rotary` returns, differentiable (once) in q and k."""
     kw = dict(layout=layout, sections=sections, magnitude=magnitude)
-    return _RotaryEmbedding.apply(q, k, positions, offset, tuple(freqs), kw)
+    return _RotaryEmbedding.apply(q, k, positions, offset, tuple(map(float, freqs)), kw)
 
 
 def _declare(lib):

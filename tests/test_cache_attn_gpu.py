@@ -212,3 +212,89 @@ def test_sizes_of_nothing():
         out, lse = ad.cache_attn(q, cache, torch.zeros(B, 3, dtype=torch.int32, device=DEV),
                                  torch.zeros(B, dtype=torch.int32, device=DEV))
         assert out.shape == q.shape and lse.shape == q.shape[:3]
+
+
+def long_pool(B, lens, Hk, page, D, seed, max_pages):
+    """A pool made on the GPU: unit-variance keys, values with a mean, and the sequences'
+    keys and values on the CPU in 64 bits."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    pool = B * max_pages + 2
+    cache = ad.kv_cache(pool, Hk, page, D)
+    table = torch.randperm(pool, generator=g, device=DEV)[:B * max_pages].view(B, max_pages).to(torch.int32)
+    n = max(lens)
+    k = torch.randn(B, Hk, n, D, generator=g, device=DEV).to(torch.bfloat16)
+    v = (torch.randn(B, Hk, n, D, generator=g, device=DEV) + 0.5).to(torch.bfloat16)
+    ad.cache_write(k, v, cache, table, i32([0] * B), new_lens=i32(lens))
+    k, v = ad.cache_read(cache, table, i32(lens), n)
+    return cache, table, [k[b, :, :lens[b]] for b in range(B)], [v[b, :, :lens[b]] for b in range(B)]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows_over_many_tiles(D, dt, causal):
+    """Walks of more than 64 tiles (page numbers are read 64 at a time), ranges that end inside
+    a sequence, rows that fill the last tile in part."""
+    for B, H, Hk, Lq, lens, page in ((2, 3, 1, 100, [9000, 4200], 16), (1, 2, 2, 700, [5003], 128)):
+        cache, table, ks, vs = long_pool(B, lens, Hk, page, D, Lq + D, -(-max(lens) // page))
+        q = queries(B, H, Lq, D, dt, 3, "blhd")
+        out, lse = ad.cache_attn(q, cache, table, i32(lens), causal=causal)
+        ref = attn_reference(q, ks, vs, lens, causal=causal)
+        within(out, ref["out"], "out")
+        within(lse, ref["lse"], "lse")
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_late_keys_far_above_the_first(dt):
+    """Rows whose reference is set by small scores, then meet ones above it by 10, 40 and 120
+    powers of two: moved, or worked on again."""
+    for Lq in (1, 20, 90):
+        for above in (10.0, 40.0, 120.0):
+            cache, table, ks, vs = long_pool(1, [1500], 1, 64, 64, 5, 24)
+            q = queries(1, 2, Lq, 64, dt, 6)
+            q[..., 0] = 1.0
+            k = ks[0].clone()
+            k[..., 0] = 0
+            k[:, 700, 0] = above * math.log(2.0) * 8.0        # one key: the score is that over sqrt(64)
+            cache = ad.kv_cache(26, 1, 64, 64)
+            ad.cache_write(k[None], vs[0][None], cache, table, i32([0]))
+            k, v = ad.cache_read(cache, table, i32([1500]), 1500)
+            out, lse = ad.cache_attn(q, cache, table, i32([1500]), causal=False)
+            ref = attn_reference(q, [k[0]], [v[0]], [1500], causal=False)
+            within(out, ref["out"], f"out {Lq} {above}")
+            within(lse, ref["lse"], f"lse {Lq} {above}")
+
+
+def test_queries_behind_the_last_may_be_anything():
+    """Padding queries of NaN and infinity change no other row's bits."""
+    for Lq in (4, 30, 200):
+        cache, table, ks, vs = long_pool(2, [900, 700], 2, 32, 64, 7, 29)
+        q = queries(2, 4, Lq, 64, torch.bfloat16, 8)
+        n = [Lq, Lq // 2]
+        out, lse = ad.cache_attn(q, cache, table, i32([900, 700]), q_lens=i32(n))
+        q[1, :, n[1]:] = math.nan
+        q[1, :, n[1]::2] = math.inf
+        out2, lse2 = ad.cache_attn(q, cache, table, i32([900, 700]), q_lens=i32(n))
+        assert torch.equal(out, out2) and torch.equal(lse, lse2)
+        assert not out[1, :, n[1]:].any() and (lse[1, :, n[1]:] == -math.inf).all()
+
+
+def test_an_empty_pool_and_many_samples():
+    """No page at all; several hundred samples, most of them empty; a table far wider than the
+    sequences are long."""
+    cache = ad.kv_cache(0, 2, 16, 64)
+    for Lq in (1, 70):
+        q = queries(3, 4, Lq, 64, torch.bfloat16, 1)
+        out, lse = ad.cache_attn(q, cache, torch.zeros(3, 300, dtype=torch.int32, device=DEV), i32([4000, 1, 0]))
+        assert not out.any() and (lse == -math.inf).all()
+    rng = random.Random(3)
+    lens = [rng.choice([0, 0, 0, rng.randrange(90)]) for _ in range(600)]
+    cache, table, ks, vs = random_pool(ad, 600, lens, 1, 16, 64, 6, 2, spare=0)
+    wide = torch.full((600, 200), -1, dtype=torch.int32, device=DEV)
+    wide[:, :6] = table
+    for Lq, q_lens in ((1, None), (3, [rng.randrange(4) for _ in range(600)])):
+        q = queries(600, 2, Lq, 64, torch.bfloat16, 3)
+        out, lse = ad.cache_attn(q, cache, wide, i32(lens), q_lens=None if q_lens is None else i32(q_lens))
+        ref = attn_reference(q, ks, vs, lens, q_lens=q_lens)
+        within(out, ref["out"], "out")
+        within(lse, ref["lse"], "lse")

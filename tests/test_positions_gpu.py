@@ -207,3 +207,19 @@ def test_same_bits_in_a_graph_and_on_a_side_stream():
         want = ad.rotary(q, k, f, offset=off)
         torch.cuda.synchronize()
         assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+def test_frequencies_are_taken_by_value():
+    """A list, an array or a tensor of them, changed between two calls, is read anew."""
+    import numpy as np
+    q = tensor((1, 2, 20, 64), torch.bfloat16, "bhld", 23)
+    for make in (list, np.array, torch.tensor, lambda x: tuple(torch.tensor(x).unbind())):
+        f = make([1.0, 0.5, 0.25])
+        a, _ = ad.rotary(q, None, f, offset=3)
+        check(a, q, (1.0, 0.5, 0.25), "q", offset=3)
+        if isinstance(f, tuple):
+            f[1].fill_(0.125)
+        else:
+            f[1] = 0.125
+        a, _ = ad.rotary(q, None, f, offset=3)
+        check(a, q, (1.0, 0.125, 0.25), "q", offset=3)
