@@ -360,8 +360,11 @@ __global__ __launch_bounds__(256, D == 128 && NQ == 2 ? 1 : 2) void cache_few_ke
         sm[wave][r * 16 + c16] = m[r];
         sl[wave][r * 16 + c16] = l[r];
       }
+      // A row that saw nothing has zeros, also where values that others saw are no numbers.
+      const bool none = m[r] == -INFINITY;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(&so[wave][(r * 16 + c16) * D + 16 * d + 4 * g]) = o[r][d];
+      for (int d = 0; d < DT; ++d)
+        *reinterpret_cast<f32x4*>(&so[wave][(r * 16 + c16) * D + 16 * d + 4 * g]) = none ? f32x4{} : o[r][d];
     }
     __syncthreads();
     constexpr int TPR = D / 4;
@@ -864,7 +867,7 @@ __global__ __launch_bounds__(64 * row_waves(T::kHalf, D), T::kHalf && D == 128 ?
     whole = 0;
     __syncthreads();
   }
-  if (seen == 0) {                                         // no key, or no query
+  if (seen <= k0) {                                        // no key here, or no query
     l = 0.f;
     m = -INFINITY;
 #pragma unroll
@@ -945,7 +948,9 @@ CachePlan plan_cache_attn(const CacheParams& p, bool f16) {
   const int64_t tiles = units * ((rows + NR - 1) / NR), turns = (keys + 63) / 64;
   const bool uneven = p.causal && 2 * (int64_t)p.L > keys;
   int64_t n = 1, best = -1;
-  for (int64_t x = 1; x <= 64 && (x == 1 || turns / x >= 8); ++x) {
+  // (Past 2^24 rows there is nothing to gain, and the join's grid has an end.)
+  const int64_t most = (int64_t)p.B * p.H * p.L <= 1 << 24 ? 64 : 1;
+  for (int64_t x = 1; x <= most && (x == 1 || turns / x >= 8); ++x) {
     const int64_t over = 6 + (x > 1 ? 8 : 0), each = (turns + x - 1) / x + over;
     int64_t cost = (tiles * x + room - 1) / room * each;
     if (uneven) {

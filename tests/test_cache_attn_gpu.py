@@ -298,3 +298,20 @@ def test_an_empty_pool_and_many_samples():
         ref = attn_reference(q, ks, vs, lens, q_lens=q_lens)
         within(out, ref["out"], "out")
         within(lse, ref["lse"], "lse")
+
+
+def test_rows_without_a_token_are_zeros_beside_tokens_that_are_no_numbers():
+    """Padding queries, and queries that stand before the first token, where values of the
+    sequence are NaN; a row that stands before those in another range of the keys than theirs."""
+    for Lq, n in ((3, 300), (3, 5000), (40, 300), (40, 9000), (150, 9000)):
+        cache, table, ks, vs = random_pool(ad, 2, [n, 2], 2, 64, 64, -(-n // 64), Lq)
+        q = queries(2, 4, Lq, 64, torch.bfloat16, 4)
+        nq = [Lq // 2, Lq]                                # the second sample's first queries see nothing
+        for t in (5, n // 2):
+            cache.k[table[0, t // 64].long(), :, t % 64] = math.nan
+            cache.v[table[0, t // 64].long(), :, t % 64 // 16, :, t % 16] = math.nan
+        cache.v[table[1, 0].long(), :, 0, :, 1] = math.nan
+        out, lse = ad.cache_attn(q, cache, table, i32([n, 2]), q_lens=i32(nq))
+        assert not out[0, :, nq[0]:].any() and (lse[0, :, nq[0]:] == -math.inf).all()
+        assert torch.isnan(out[0, :, :nq[0]]).all()
+        assert not out[1, :, :Lq - 2].any() and (lse[1, :, :Lq - 2] == -math.inf).all()
