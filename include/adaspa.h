@@ -536,7 +536,8 @@ adaspa_status adaspa_cache_write(const adaspa_cache_problem* prob, const adaspa_
                                  const int32_t* new_lens, void* stream);
 
 /* Rows t of k and v [B, Hk, len, D] are the tokens at positions starts[b] + t (starts may be
- * NULL: t) of sequences of lens[b] tokens; rows that are no token's are zeros. */
+ * NULL: t) of sequences of lens[b] tokens; rows that are no token's are zeros.  k and v must
+ * not overlap. */
 adaspa_status adaspa_cache_read(const adaspa_cache_problem* prob, const adaspa_cache* cache,
                                 const int32_t* lens, const int32_t* starts, void* k, void* v,
                                 void* stream);

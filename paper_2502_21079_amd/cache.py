@@ -173,7 +173,7 @@ def cache_read(cache: KVCache, page_table, lens, tokens: int, *, starts=None, dt
     token at position t, or ``starts[b]`` + t (int32 [B]).  Rows that are not among the
     sequence's ``lens[b]`` tokens, or on a page that is not in the pool, are zeros.  Values are
     exact in bf16 (and in fp16 within its range).  ``k`` and ``v`` are filled where they
-    are given."""
+    are given; they must not overlap."""
     dev = cache.k.get_device()
     if dtype not in _DTYPES:
         raise AdaspaError(f"dtype must be bf16 or fp16, got {dtype}")
@@ -212,8 +212,9 @@ def cache_attn(q, cache: KVCache, page_table, lens, *, q_lens=None, causal: bool
     only the order hides from a row must be finite, as those that it sees.  ``scale``
     defaults to 1 / sqrt(D), which values up to 0 stand for too.  ``workspace`` (at least
     :func:`cache_attn_workspace` bytes, any type) is allocated here when not given and
-    needed.  Results follow the shape (the page table's width among it): how the tokens
-    are divided over the GPU does not depend on lens."""
+    needed.  The same arguments give the same bits.  How the tokens are divided over the GPU
+    follows the shapes (the page table's width among them) and, up to 32 rows a key head, all
+    of ``lens``: in another batch a sequence's results may differ in their last bits."""
     dev = _device_of(q, "q")
     pool, ref = _check_cache(cache, page_table, dev)
     _check_count(lens, "lens", q.shape[0], dev)

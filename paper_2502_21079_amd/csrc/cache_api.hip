@@ -116,6 +116,7 @@ adaspa_status adaspa_cache_read(const adaspa_cache_problem* prob, const adaspa_c
   if (st != ADASPA_OK) return st;
   const bool rows = prob->batch > 0 && prob->len > 0;
   if (bad(k, rows, 16) || bad(v, rows, 16) || bad(lens, rows, 4) || bad(starts, false, 4)) return ADASPA_ERR_INVALID_ARG;
+  if (rows && k == v) return ADASPA_ERR_INVALID_ARG;
   CacheParams p = params(prob, cache);
   p.k_out = (u16*)k;
   p.v_out = (u16*)v;

@@ -253,7 +253,9 @@ class _RotaryEmbedding(torch.autograd.Function):
 
 def rotary_embedding(q, k, freqs, *, layout: str = "half", sections=None, magnitude: float = 1.0, positions=None,
                      offset: Union[int, torch.Tensor] = 0):
-    """What :func:`rotary` returns, differentiable (once) in q and k."""
+    """What :func:`rotary` returns, differentiable (once) in q and k.  A backward pass may be
+    captured into a graph with its forward pass; as with any function of torch's, no graph of
+    the same leaves from outside the capture may be alive then."""
     kw = dict(layout=layout, sections=sections, magnitude=magnitude)
     return _RotaryEmbedding.apply(q, k, positions, offset, tuple(map(float, freqs)), kw)
 

@@ -178,3 +178,8 @@ def test_the_definitions():
     for v in (1.0, 3.3, 400.0, 5000.0):
         s.write(0, torch.full((1, 1, 64), v), torch.full((1, 1, 64), v))
     assert s.scale[0][0] == [[16.0]] and s.x[0][0][0, :, 0].tolist() == [1.0, 3.25, 384.0, 5120.0]
+
+
+def test_one_place_for_keys_and_values_is_refused(lib):
+    p, c = ctypes.byref(_prob(heads=2)), ctypes.byref(_cache())
+    assert lib.adaspa_cache_read(p, c, FAKE, None, FAKE, FAKE, None) == 1

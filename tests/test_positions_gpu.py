@@ -223,3 +223,23 @@ def test_frequencies_are_taken_by_value():
             f[1] = 0.125
         a, _ = ad.rotary(q, None, f, offset=3)
         check(a, q, (1.0, 0.125, 0.25), "q", offset=3)
+
+
+def test_a_training_pass_in_a_graph():
+    """Turned and turned back inside one capture, replayed over new values."""
+    f = ad.rotary_frequencies(64)
+    q = tensor((2, 4, 37, 64), torch.bfloat16, "bhld", 31).requires_grad_()
+    k = tensor((2, 1, 37, 64), torch.bfloat16, "bhld", 32).requires_grad_()
+    gq, gk = tensor(q.shape, torch.bfloat16, "bhld", 33), tensor(k.shape, torch.bfloat16, "bhld", 34)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a, b = ad.rotary_embedding(q, k, f, layout="interleaved", offset=5)
+        dq, dk = torch.autograd.grad((a, b), (q, k), (gq, gk))
+    for step in range(3):
+        with torch.no_grad():
+            q.mul_(0.5)
+            gk.add_(1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, x, way in ((a, q, 1), (b, k, 1), (dq, gq, -1), (dk, gk, -1)):
+            check(got.detach(), x.detach(), f, "in a graph", layout="interleaved", offset=5, way=way)
