@@ -213,7 +213,7 @@ def cache_attn(q, cache: KVCache, page_table, lens, *, q_lens=None, causal: bool
     defaults to 1 / sqrt(D), which values up to 0 stand for too.  ``workspace`` (at least
     :func:`cache_attn_workspace` bytes, any type) is allocated here when not given and
     needed.  The same arguments give the same bits.  How the tokens are divided over the GPU
-    follows the shapes (the page table's width among them) and, up to 32 rows a key head, all
+    follows the shapes (the page table's width among them) and, up to 48 rows a key head, all
     of ``lens``: in another batch a sequence's results may differ in their last bits."""
     dev = _device_of(q, "q")
     pool, ref = _check_cache(cache, page_table, dev)

@@ -50,7 +50,9 @@ struct CachePlan {
   int shares, chunk, chunks;
   int64_t part_ml, before, bytes;      // byte offsets into the workspace
 };
-constexpr int kFewRows = 32;
+// Few rows of a key head: up to kFewRows, and up to kSharedRows where the table is kSharedSteps turns
+// (256 keys each) wide or wider.  Up to kWholeSteps turns a workgroup takes a sequence.
+constexpr int kFewRows = 32, kSharedRows = 48, kWholeSteps = 8, kSharedSteps = 12;
 
 CachePlan plan_cache_attn(const CacheParams& p, bool f16);
 hipError_t launch_cache_write(CacheParams p, bool f16, hipStream_t st);

@@ -150,7 +150,7 @@ struct Turns {
 // the order samples, key heads, turns, 512 workgroups 53 and 129; key heads side by side 51 and 128;
 // 256 workgroups 48 and 124; past the cache 46 and 113 (6.0 TB/s).
 template <class T, int D, int NQ, bool SHARED, bool BYPASS>
-__global__ __launch_bounds__(256, D == 128 && NQ == 2 ? 1 : 2) void cache_few_kernel(const CacheParams p) {
+__global__ __launch_bounds__(256, NQ == 3 || (D == 128 && NQ == 2) ? 1 : 2) void cache_few_kernel(const CacheParams p) {
   constexpr int NW = 4, STEP = 64 * NW, DT = D / 16, KJ = D / 64;          // channel tiles; 16-byte pieces of a key a lane
   __shared__ __attribute__((aligned(16))) float so[NW][NQ * 16 * D];
   __shared__ float sm[NW][NQ * 16], sl[NW][NQ * 16];
@@ -924,15 +924,20 @@ int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 CachePlan plan_cache_attn(const CacheParams& p, bool f16) {
   CachePlan c{};
   const int64_t units = (int64_t)p.B * p.Hk, rows = (int64_t)p.G * p.L, keys = (int64_t)p.c.max_pages * p.c.page;
-  c.few = rows <= kFewRows;
+  const int64_t steps = (keys + 255) / 256;
+  // 33 to 48 rows too where keys are shared: 16 sequences of up to 17,664 tokens, 4 key heads of d 128
+  // under 24, eight tokens each, 124 us over tiles of 256 rows, 76 here (fp16 125 and 79, d 64 54 and 47).
+  // Not over less than 12 turns: 16 sequences of up to 2,304 tokens 28 and 35 (one of 3,000 24 and 21, 64 of
+  // up to 4,096 107 and 90), 32 of up to 1,500 tokens, each a workgroup's, 40 rows, 23 and 27.
+  // 49 to 64 rows gain nothing (60 of d 64: 20 and 20; 64 of d 128 over 100,000 tokens: 100 and 98).
+  c.few = rows <= kFewRows || (rows <= kSharedRows && steps >= kSharedSteps);
   c.chunks = 1;
   c.chunk = 1 << 28;
   if (c.few) {
     // The last-level cache has 256 MB; from 192 on (217 MB: 42.6 and 38.4 us, 134 MB: 23.0 and 27.5).
     c.bypass = units * keys * 2 * p.D >= (int64_t)192 << 20;
-    const int64_t turns = (keys + 255) / 256;
-    if (turns > 8) {
-      const int64_t n = p.Hk < 256 ? 256 / p.Hk : 1, most = p.B * turns;
+    if (steps > kWholeSteps) {
+      const int64_t n = p.Hk < 256 ? 256 / p.Hk : 1, most = p.B * steps;
       c.shares = (int)(n < most ? n : most);
       c.part_ml = up256(2 * c.shares * p.Hk * rows * p.D * 4);
       c.before = c.part_ml + up256(2 * c.shares * p.Hk * rows * 8);
@@ -974,9 +979,13 @@ CachePlan plan_cache_attn(const CacheParams& p, bool f16) {
 }
 
 template <class T, int D, int NQ>
+static void run_shared(const CacheParams& p, bool bypass, hipStream_t st) {
+  if (bypass) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, true, true>), dim3(p.n_wg), dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, true, false>), dim3(p.n_wg), dim3(256), 0, st, p);
+}
+template <class T, int D, int NQ>
 static void run_few(const CacheParams& p, bool bypass, hipStream_t st) {
-  if (p.shares && bypass) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, true, true>), dim3(p.n_wg), dim3(256), 0, st, p);
-  else if (p.shares) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, true, false>), dim3(p.n_wg), dim3(256), 0, st, p);
+  if (p.shares) run_shared<T, D, NQ>(p, bypass, st);
   else if (bypass) hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, false, true>), dim3(p.n_wg), dim3(256), 0, st, p);
   else hipLaunchKernelGGL((cache_few_kernel<T, D, NQ, false, false>), dim3(p.n_wg), dim3(256), 0, st, p);
 }
@@ -990,7 +999,8 @@ static hipError_t run_attn(CacheParams p, const CachePlan& c, hipStream_t st) {
   if (c.few) {
     p.n_wg = (c.shares ? c.shares : p.B) * p.Hk;
     if (rows <= 16) run_few<T, D, 1>(p, c.bypass, st);
-    else run_few<T, D, 2>(p, c.bypass, st);
+    else if (rows <= 32) run_few<T, D, 2>(p, c.bypass, st);
+    else run_shared<T, D, 3>(p, c.bypass, st);
     if (p.shares)
       hipLaunchKernelGGL((cache_few_join_kernel<T, D>), dim3((uint32_t)(units * rows)), dim3(256), 0, st, p);
     return hipGetLastError();

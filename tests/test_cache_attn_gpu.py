@@ -315,3 +315,11 @@ def test_rows_without_a_token_are_zeros_beside_tokens_that_are_no_numbers():
         assert not out[0, :, nq[0]:].any() and (lse[0, :, nq[0]:] == -math.inf).all()
         assert torch.isnan(out[0, :, :nq[0]]).all()
         assert not out[1, :, :Lq - 2].any() and (lse[1, :, :Lq - 2] == -math.inf).all()
+
+
+@pytest.mark.parametrize("Lq,H,Hk", [(33, 1, 1), (16, 6, 2), (17, 4, 2), (48, 2, 2), (49, 1, 1), (8, 6, 1), (12, 4, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_rows_around_48_over_long_sequences(Lq, H, Hk, D, dt):
+    for causal, q_lens in ((True, None), (False, None), (True, [Lq, 0, Lq - 5, Lq, 1])):
+        run(5, H, Hk, Lq, [3100, 300, 17, 0, 2900], 32, D, dt, causal=causal, q_lens=q_lens, seed=Lq, layout="blhd")
