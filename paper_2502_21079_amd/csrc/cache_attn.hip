@@ -467,8 +467,15 @@ __global__ __launch_bounds__(256) void cache_few_join_kernel(const CacheParams p
 //   in the second product, channels side by side.
 // Every place that a lane reads is its own base plus a constant.
 constexpr int kKeyPiece = 64 * 8 + 8;                      // elements from a piece of the keys to the next
-// Waves of a workgroup, 32 rows each, and workgroups of a CU.  (fp16 at d 128: its second values leave
-// registers for one wave a SIMD.)
+// Waves of a workgroup, 32 rows each; two waves a SIMD (fp16 at d 128 one: its second values leave no
+// more registers).  d 128: a tile's decoding and its way through LDS serve 256 rows; with four
+// waves and two workgroups a CU 2,047 tokens over 17,664 (24 heads over 4) take 456 instead of 413 us, a
+// prompt of 4,096 128 instead of 118.  At d 64 a tile has a piece of keys and of values for each of
+// 256 threads.
+// What bounds it: the matrix pipe at the clock that the card holds under it (busy 52% of the cycles, as
+// vector units issue in 45%) and, for the example, 20 us of joining four ranges: 399 us in all, 1,050
+// TFLOP/s where a product of 8,192^3 has 1,209; without ranges (4 x 16 heads, 4,096 over 16,384) 1,204.
+// fp16 at d 128 655 us: five products instead of four at half the waves.
 constexpr int row_waves(bool f16, int D) { return f16 ? 4 : D / 16; }
 
 // One step over tiles that every row sees whole: the scores of the next tile, the
