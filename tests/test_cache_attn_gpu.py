@@ -323,3 +323,21 @@ def test_rows_without_a_token_are_zeros_beside_tokens_that_are_no_numbers():
 def test_rows_around_48_over_long_sequences(Lq, H, Hk, D, dt):
     for causal, q_lens in ((True, None), (False, None), (True, [Lq, 0, Lq - 5, Lq, 1])):
         run(5, H, Hk, Lq, [3100, 300, 17, 0, 2900], 32, D, dt, causal=causal, q_lens=q_lens, seed=Lq, layout="blhd")
+
+
+def test_pages_past_4_gb():
+    """Pages all over a pool of more than 4 GB give what the same pages give side by side."""
+    page, Hk, D, width = 128, 8, 128, 25
+    pages = (1 << 32) // (page * Hk * D) + 40
+    g = torch.Generator(device=DEV).manual_seed(1)
+    n = page * width - 5
+    k, v = (torch.randn(1, Hk, n, D, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    far, near = ad.kv_cache(pages, Hk, page, D), ad.kv_cache(width, Hk, page, D)
+    spread = i32([[pages - 1 - i * (pages // width) for i in range(width)]])
+    side = torch.arange(width, dtype=torch.int32, device=DEV)[None]
+    ad.cache_write(k, v, far, spread, i32([0]))
+    ad.cache_write(k, v, near, side, i32([0]))
+    for Lq in (1, 20, 40, 60):
+        q = queries(1, Hk, Lq, D, torch.bfloat16, Lq)
+        for a, b in zip(ad.cache_attn(q, far, spread, i32([n])), ad.cache_attn(q, near, side, i32([n]))):
+            assert torch.equal(a, b) and torch.isfinite(a).all()
