@@ -142,15 +142,21 @@ struct Turns {
 // (2 key heads of 1,984 keys, d 64, us a call: 14.4 and 17.7; 4 of 4,096, d 128: 25.8 and 19.0.  A CU
 // reads 50 GB/s, so eight waves instead of four gain nothing).
 //
-// Workgroups are few (one a CU) and every wave has one or two blocks, 16 to 32 KB, on
-// their way: more of them only spread the reads over memory.  The key heads of a
+// Workgroups are few (one a CU) and every wave has one or two blocks, 16 to 32 KB, on their way: more of them only spread the reads over memory.  The key heads of a
 // share run side by side, since they lie side by side in a page.  BYPASS: keys and values that the
 // last-level cache could not keep until the next call are read past it.  16 sequences of up to
 // 17,664 tokens, 4 key heads of d 128 under 24, and 110,080 tokens of 24 heads, us a call: shares in
 // the order samples, key heads, turns, 512 workgroups 53 and 129; key heads side by side 51 and 128;
 // 256 workgroups 48 and 124; past the cache 46 and 113 (6.0 TB/s).
+//
+// Two tiles of rows, and three at d 64, have more to work on between a block's loads: two workgroups a CU,
+// whose waves hold one block each (and so fit), work on one while the other's is on its way.  The same
+// sequences, us: 18 rows 60 and 52, 48 rows of d 64 47 and 42; two of 6,000, 24 key heads, 20 rows 27.5 and
+// 29; 48 rows of d 128 75 and 95 (they do not fit), 6 rows 48 and 47.5.
+constexpr bool one_block(int D, int tiles, bool shared) { return shared && (tiles == 2 || (tiles == 3 && D == 64)); }
+
 template <class T, int D, int NQ, bool SHARED, bool BYPASS>
-__global__ __launch_bounds__(256, NQ == 3 || (D == 128 && NQ == 2) ? 1 : 2) void cache_few_kernel(const CacheParams p) {
+__global__ __launch_bounds__(256, !one_block(D, NQ, SHARED) && (NQ == 3 || (D == 128 && NQ == 2)) ? 1 : 2) void cache_few_kernel(const CacheParams p) {
   constexpr int NW = 4, STEP = 64 * NW, DT = D / 16, KJ = D / 64;          // channel tiles; 16-byte pieces of a key a lane
   __shared__ __attribute__((aligned(16))) float so[NW][NQ * 16 * D];
   __shared__ float sm[NW][NQ * 16], sl[NW][NQ * 16];
@@ -329,9 +335,19 @@ __global__ __launch_bounds__(256, NQ == 3 || (D == 128 && NQ == 2) ? 1 : 2) void
           }
         }
     };
-    Block x[2];
     int k = k0 + wave * 64;
-    if (k < k1) {
+    if (one_block(D, NQ, SHARED) && k < k1) {
+      Block x;
+      pages = look(k);
+      later = look(k + 16 * STEP);
+      for (;; k += STEP) {
+        load(x, k);
+        work(x, k);
+        if (k + STEP >= k1) break;
+      }
+    }
+    if (!one_block(D, NQ, SHARED) && k < k1) {
+      Block x[2];
       // A block's loads go out before the one before it is worked on, also where it is past the
       // range (it is not worked on): behind a branch the compiler would wait for the newest.
       pages = look(k);
@@ -944,7 +960,8 @@ CachePlan plan_cache_attn(const CacheParams& p, bool f16) {
     // The last-level cache has 256 MB; from 192 on (217 MB: 42.6 and 38.4 us, 134 MB: 23.0 and 27.5).
     c.bypass = units * keys * 2 * p.D >= (int64_t)192 << 20;
     if (steps > kWholeSteps) {
-      const int64_t n = p.Hk < 256 ? 256 / p.Hk : 1, most = p.B * steps;
+      const int64_t room = one_block(p.D, (int)(rows + 15) / 16, true) ? 512 : 256;
+      const int64_t n = p.Hk < room ? room / p.Hk : 1, most = p.B * steps;
       c.shares = (int)(n < most ? n : most);
       c.part_ml = up256(2 * c.shares * p.Hk * rows * p.D * 4);
       c.before = c.part_ml + up256(2 * c.shares * p.Hk * rows * 8);
