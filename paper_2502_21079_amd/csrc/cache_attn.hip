@@ -783,6 +783,7 @@ __global__ __launch_bounds__(64 * row_waves(T::kHalf, D), T::kHalf && D == 128 ?
       for (int i = 0; i < 4; ++i) w[1][0][i] = w[1][1][i] = bf16x8{};
       scores(0, s[0]);
       m = top_of(s[0], *reinterpret_cast<const f32x4*>(scale[0]));
+      lds_barrier();                                     // the first step writes tile 2's keys over tile 0's
       bool bad = !(m < INFINITY && m > -INFINITY);
       if (bad) m = 0.f;
       auto step = [&](auto u) {
