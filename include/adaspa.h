@@ -530,7 +530,8 @@ typedef struct {
  * finite values, values the nearest code, ties to even; infinities and NaN are kept as NaN.  A
  * page that holds tokens before lens[b] keeps the larger of its scale and the new tokens', and
  * where that grows their codes are brought to it.  What lies behind the last token stays as it
- * was.  A sample with lens[b] < 0 is left out.  No two sequences may write the same page. */
+ * was.  A sample with lens[b] < 0 is left out; one without new tokens writes nothing, whatever
+ * pages the table names for it.  No two sequences may write the same page. */
 adaspa_status adaspa_cache_write(const adaspa_cache_problem* prob, const adaspa_cache* cache,
                                  const void* k, const void* v, const int32_t* lens,
                                  const int32_t* new_lens, void* stream);

@@ -154,7 +154,8 @@ def cache_write(k, v, cache: KVCache, page_table, lens, *, new_lens=None) -> Non
     to it.  Infinities and NaN are kept as NaN.  Tokens behind the last one stay as they
     were; tokens for pages that the table does not name, or that are not in the pool, are
     dropped, and so are all of a sample with lens[b] < 0.  Pages that are written belong to
-    one sequence; the same page twice is an error of the caller's."""
+    one sequence; the same page twice is an error of the caller's.  A sample without new
+    tokens writes nothing, so the table may name another's pages for it."""
     dev = _device_of(k, "k, v")
     if v.dtype is not k.dtype or v.get_device() != dev or v.shape != k.shape:
         raise AdaspaError("k, v must share one type, shape and device")

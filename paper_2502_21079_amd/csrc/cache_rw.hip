@@ -28,7 +28,8 @@ __global__ __launch_bounds__(PAGE * 4) void cache_write_kernel(const CacheParams
   const bool values = blockIdx.y & 1;
   const int64_t start = p.lens[b];
   const int n = p.new_lens ? clamp_len(p.new_lens[b], p.L) : p.L;
-  if (start < 0) return;
+  // A sample without new tokens leaves every page alone: its last one may be another's to write.
+  if (start < 0 || n == 0) return;
   const int64_t index = start / PAGE + blockIdx.x, first = index * PAGE;
   if (first >= start + n || index >= p.c.max_pages) return;
   const int id = page_at(p.c, b, (int)index);

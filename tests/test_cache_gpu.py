@@ -218,3 +218,29 @@ def test_a_pool_that_was_not_written_here():
         assert torch.equal(k[b, :, :n].cpu().double(), ks[b]) and torch.equal(v[b, :, :n].cpu().double(), vs[b])
         assert not k[b, :, n:].any() and not v[b, :, n:].any()
     assert cache.k.dtype is E4M3
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("D", [64, 128])
+def test_idle_samples_write_nothing(page, D):
+    """Samples without new tokens, whose lengths end inside a page: it stays as it was, bit for
+    bit, also where another sequence writes it and its scale grows."""
+    Hk, T, idle = 3, 5, 200
+    cache = fresh_cache(4, Hk, page, D)
+    k, v = tokens(2, Hk, T, D, torch.bfloat16, 1), tokens(2, Hk, T, D, torch.bfloat16, 2)
+    before = [t.clone() for t in raw(cache)]
+    ad.cache_write(k, v, cache, i32([[1, 2], [3, 0]]), i32([7, page + 3]), new_lens=i32([0, -4]))
+    for t, was in zip(raw(cache), before):
+        assert torch.equal(t, was)
+    # One sequence in use among many slots that still name its page.
+    table = torch.ones(idle + 1, 1, dtype=torch.int32, device=DEV)
+    seqs, lens, new = Sequences(1, Hk, page, D), [3] * (idle + 1), [0] * (idle + 1)
+    g = torch.Generator().manual_seed(3)
+    for step, n in enumerate((3, 1, 1, 1, 1, 1, 1, 1)):
+        k, v = (torch.randn(1, Hk, T, D, generator=g).to(torch.bfloat16) * 4 ** step for _ in range(2))
+        k, v = k.to(DEV), v.to(DEV)
+        lens[idle // 2], new[idle // 2] = (2 + step if step else 0), n
+        ad.cache_write(k.expand(idle + 1, -1, -1, -1), v.expand(idle + 1, -1, -1, -1), cache, table, i32(lens),
+                       new_lens=i32(new))
+        seqs.write(0, k[0, :, :n], v[0, :, :n])
+        expect(cache, table[:1], seqs, [3 + step])
