@@ -552,7 +552,7 @@ adaspa_status adaspa_cache_read(const adaspa_cache_problem* prob, const adaspa_c
  * behind lens[b], on pages that are not there, or in queries from q_lens[b] on takes no part,
  * infinities and NaN too; tokens that only the order hides from a row must be finite.  lse:
  * fp32 [B, H, len] or NULL.  The workspace is that of the prompt side's calls: scratch, 256-byte
- * aligned, of the size that the _workspace call names. */
+ * aligned, of the size that the _workspace call names for the same problem, `causal` included. */
 size_t adaspa_cache_attn_workspace(const adaspa_cache_problem* prob);
 adaspa_status adaspa_cache_attn(const adaspa_cache_problem* prob, const adaspa_cache* cache,
                                 const void* q, const int32_t* lens, const int32_t* q_lens, void* out,

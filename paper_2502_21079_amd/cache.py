@@ -235,15 +235,16 @@ def cache_attn(q, cache: KVCache, page_table, lens, *, q_lens=None, causal: bool
     return out, lse
 
 
-def cache_attn_workspace(q_shape, cache: KVCache, max_pages: int, dtype=torch.bfloat16) -> int:
-    """Bytes of the workspace of :func:`cache_attn` for q of this shape and type and a
-    page table of this width."""
+def cache_attn_workspace(q_shape, cache: KVCache, max_pages: int, dtype=torch.bfloat16, *,
+                         causal: Optional[bool] = None) -> int:
+    """Bytes of the workspace of :func:`cache_attn` for q of this shape and type, a page
+    table of this width and this ``causal``; None: as many as serve either."""
     if dtype not in _DTYPES:
         raise AdaspaError(f"dtype must be bf16 or fp16, got {dtype}")
     shape = tuple(map(index, q_shape))
     pool = _pool(cache.k.shape, cache.v.shape, cache.k_scale.shape, cache.v_scale.shape)
-    return _plan(pool, _DTYPES[dtype], (shape[0], index(max_pages)), (index(max_pages), 1), shape, (_contiguous(shape),), None, True,
-                 0.0).need
+    return max(_plan(pool, _DTYPES[dtype], (shape[0], index(max_pages)), (index(max_pages), 1), shape, (_contiguous(shape),),
+                     None, order, 0.0).need for order in ((True, False) if causal is None else (bool(causal),)))
 
 
 def _declare(lib):

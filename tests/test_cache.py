@@ -183,3 +183,30 @@ def test_the_definitions():
 def test_one_place_for_keys_and_values_is_refused(lib):
     p, c = ctypes.byref(_prob(heads=2)), ctypes.byref(_cache())
     assert lib.adaspa_cache_read(p, c, FAKE, None, FAKE, FAKE, None) == 1
+
+
+# Shapes of q, key heads, page, table width.  The first two in bf16: ranges of the keys without an order
+# alone, with one alone.
+SIZES = [((1, 24, 4096, 128), 4, 64, 64), ((1, 24, 1500, 128), 4, 64, 40), ((1, 24, 2047, 128), 4, 64, 64), ((1, 24, 2047, 128), 4, 64, 276),
+         ((3, 6, 100, 64), 2, 16, 400), ((16, 24, 1, 128), 4, 64, 276), ((1, 2, 60, 64), 2, 16, 4)]
+
+
+@pytest.mark.parametrize("q,Hk,page,width", SIZES)
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_the_workspace_serves_the_call(lib, q, Hk, page, width, dt):
+    """What is named for an order, for none, and for either is what such calls ask for."""
+    B, H, L, D = q
+    pages = B * width
+    cache = ad.KVCache(*[torch.empty(s, device="meta") for s in
+                         ((pages, Hk, page, D), (pages, Hk, page // 16, D, 16), (pages, Hk), (pages, Hk))])
+    need = {}
+    for causal in (True, False):
+        p = _prob(batch=B, heads=H, kv_heads=Hk, len=L, head_dim=D, dtype=int(dt is torch.float16), pages=pages, page=page,
+                  max_pages=width, table_stride=width, causal=int(causal), q_stride=(H * L * D, L * D, D),
+                  out_stride=(H * L * D, L * D, D))
+        need[causal] = lib.adaspa_cache_attn_workspace(ctypes.byref(p))
+        assert need[causal] >= 16
+        assert ad.cache_attn_workspace(q, cache, width, dt, causal=causal) == need[causal]
+    assert ad.cache_attn_workspace(q, cache, width, dt) == max(need.values())
+    if dt is torch.bfloat16 and q[2] in (4096, 1500):
+        assert min(need.values()) == 16 == need[q[2] == 4096] and max(need.values()) > 16

@@ -341,3 +341,20 @@ def test_pages_past_4_gb():
         q = queries(1, Hk, Lq, D, torch.bfloat16, Lq)
         for a, b in zip(ad.cache_attn(q, far, spread, i32([n])), ad.cache_attn(q, near, side, i32([n]))):
             assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
+@pytest.mark.parametrize("causal", [True, False, None])
+def test_a_workspace_of_the_size_named(causal):
+    """Exactly as many bytes as are named, at shapes where an order and none want different
+    amounts; the bits are those of a call that allocates its own."""
+    for B, H, Hk, Lq, n, D, page in ((1, 24, 4, 4096, 4096, 128, 64), (1, 24, 4, 1500, 2500, 128, 64),
+                                     (2, 6, 2, 300, 400, 64, 16)):
+        width = -(-n // page)
+        cache, table, ks, vs = long_pool(B, [n] * B, Hk, page, D, 3, width)
+        q = queries(B, H, Lq, D, torch.bfloat16, 4)
+        ws = torch.empty(ad.cache_attn_workspace(q.shape, cache, width, causal=causal), dtype=torch.uint8, device=DEV)
+        for order in (True, False) if causal is None else (causal,):
+            ws.fill_(255)
+            got = ad.cache_attn(q, cache, table, i32([n] * B), causal=order, workspace=ws)
+            want = ad.cache_attn(q, cache, table, i32([n] * B), causal=order)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
