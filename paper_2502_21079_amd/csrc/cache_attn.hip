@@ -10,8 +10,12 @@
 // Keys enter the first product as codes, which 16 bits hold exactly, and their
 // scale is part of the factor that the scores get anyway.  Values enter the second
 // as code times scale in bf16, whose exponents hold every scale; so do the
-// weights, with fp16 inputs as two values each (the second what the first leaves),
-// so that no output type loses to their rounding.
+// weights, as two values each (the second what the first leaves, 2^-16 of a weight are
+// lost), so that no output type loses to their rounding.  The one exception is many rows
+// with bf16 inputs: one value, 2^-9 of a weight lost where the result's own rounding is as
+// much, since a second one is half as many matrix instructions again and 64 registers
+// (2,047 tokens over 17,664, 24 heads over 4 of d 128: 399 us, as two values 655; the largest
+// error against 64 bits 0.00170, in fp32 0.00166).
 #include "cache_tile.hpp"
 
 namespace adaspa {
@@ -153,6 +157,10 @@ struct Turns {
 // whose waves hold one block each (and so fit), work on one while the other's is on its way.  The same
 // sequences, us: 18 rows 60 and 52, 48 rows of d 64 47 and 42; two of 6,000, 24 key heads, 20 rows 27.5 and
 // 29; 48 rows of d 128 75 and 95 (they do not fit), 6 rows 48 and 47.5.
+//
+// Weights as two values for bf16 inputs too, us with one and with two: 16 sequences of up to 17,664
+// tokens, 6 rows 46.4 and 47.7, 18 rows 58.9 and 59.5, 48 rows 74 and 79, 48 rows of d 64 42 and 47;
+// 110,080 tokens of 24 heads 112.6 and 113.2.
 constexpr bool one_block(int D, int tiles, bool shared) { return shared && (tiles == 2 || (tiles == 3 && D == 64)); }
 
 template <class T, int D, int NQ, bool SHARED, bool BYPASS>
@@ -313,7 +321,7 @@ __global__ __launch_bounds__(256, !one_block(D, NQ, SHARED) && (NQ == 3 || (D ==
             const float c = fast_exp2(s[r][t][e] - ref), d = fast_exp2(s[r][t][e + 1] - ref);
             sum += c + d;
             uint32_t left = 0;
-            hi[t >> 1][(t & 1) * 2 + e / 2] = T::kHalf ? split2(c, d, left) : BF16::pack(c, d);
+            hi[t >> 1][(t & 1) * 2 + e / 2] = split2(c, d, left);
             lo[t >> 1][(t & 1) * 2 + e / 2] = left;
           }
         l[r] += sum;
@@ -331,7 +339,7 @@ __global__ __launch_bounds__(256, !one_block(D, NQ, SHARED) && (NQ == 3 || (D ==
 #pragma unroll
           for (int r = 0; r < NQ; ++r) {
             o[r][d] = mfma16(vf, w[r][h], o[r][d]);
-            if (T::kHalf) o[r][d] = mfma16(vf, rest[r][h], o[r][d]);
+            o[r][d] = mfma16(vf, rest[r][h], o[r][d]);
           }
         }
     };

@@ -358,3 +358,16 @@ def test_a_workspace_of_the_size_named(causal):
             got = ad.cache_attn(q, cache, table, i32([n] * B), causal=order, workspace=ws)
             want = ad.cache_attn(q, cache, table, i32([n] * B), causal=order)
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("H,Hk,Lq,lens", [(2, 2, 1, [300, 1984, 40]), (12, 2, 1, [9000, 5]), (8, 1, 3, [4000, 700]),
+                                          (6, 1, 7, [5000, 3100]), (3, 3, 9, [130, 64])])
+@pytest.mark.parametrize("D", [64, 128])
+def test_few_rows_lose_no_bits_to_their_weights(H, Hk, Lq, lens, D):
+    """bf16 with up to 48 rows a key head: weights are two bf16 values, so what remains of them is
+    2^-16, as with fp16, and the result's own rounding (2^-8) is all of its size."""
+    cache, table, ks, vs = random_pool(ad, len(lens), lens, Hk, 32, D, -(-max(lens) // 32), Lq + D)
+    q = queries(len(lens), H, Lq, D, torch.bfloat16, Lq)
+    out, lse = ad.cache_attn(q, cache, table, i32(lens))
+    want, abs_sum = (attn_reference(q, ks, [f(v) for v in vs], lens)["out"][0] for f in (lambda v: v, torch.abs))
+    within(out, (want, 2.0 ** -8 * want.abs() + (2.0 ** -16 + 2e-5) * abs_sum), "out")
