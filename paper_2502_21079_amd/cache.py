@@ -49,7 +49,8 @@ class _Cache(ctypes.Structure):
 @dataclass
 class KVCache:
     """A pool of pages.  A value is its code times its page's and head's scale, a
-    power of two."""
+    power of two.  (Magnitudes from 248 * 2^120 on, among bf16's last, are rounded to 2^128,
+    which is infinite where it is read.)"""
     k: torch.Tensor               # e4m3 [pages, Hk, page, D]
     v: torch.Tensor               # e4m3 [pages, Hk, page / 16, D, 16]: sixteen tokens of a channel side by side
     k_scale: torch.Tensor         # fp32 [pages, Hk]
@@ -173,7 +174,7 @@ def cache_read(cache: KVCache, page_table, lens, tokens: int, *, starts=None, dt
     """(k, v) [B, Hk, tokens, D] in ``dtype`` (bf16 or fp16): row t of sample b is the
     token at position t, or ``starts[b]`` + t (int32 [B]).  Rows that are not among the
     sequence's ``lens[b]`` tokens, or on a page that is not in the pool, are zeros.  Values are
-    exact in bf16 (and in fp16 within its range).  ``k`` and ``v`` are filled where they
+    exact within the type's range (in fp16 those that were rounded to 2^16 are infinite).  ``k`` and ``v`` are filled where they
     are given; they must not overlap."""
     dev = cache.k.get_device()
     if dtype not in _DTYPES:

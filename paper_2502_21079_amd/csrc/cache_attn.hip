@@ -12,10 +12,11 @@
 // as code times scale in bf16, whose exponents hold every scale; so do the
 // weights, as two values each (the second what the first leaves, 2^-16 of a weight are
 // lost), so that no output type loses to their rounding.  The one exception is many rows
-// with bf16 inputs: one value, 2^-9 of a weight lost where the result's own rounding is as
-// much, since a second one is half as many matrix instructions again and 64 registers
-// (2,047 tokens over 17,664, 24 heads over 4 of d 128: 399 us, as two values 655; the largest
-// error against 64 bits 0.00170, in fp32 0.00166).
+// with bf16 inputs: one value, which loses up to 2^-8 of a weight, as the result's own
+// rounding does, since a second one is half as many matrix instructions again and leaves
+// registers for half the waves (2,047 tokens over 17,664, 24 heads over 4 of d 128: 399 us,
+// as two values, which fp16 inputs have, 655; the largest error against 64 bits 0.00170, with
+// weights in fp32 0.00166).
 #include "cache_tile.hpp"
 
 namespace adaspa {
@@ -146,8 +147,9 @@ struct Turns {
 // (2 key heads of 1,984 keys, d 64, us a call: 14.4 and 17.7; 4 of 4,096, d 128: 25.8 and 19.0.  A CU
 // reads 50 GB/s, so eight waves instead of four gain nothing).
 //
-// Workgroups are few (one a CU) and every wave has one or two blocks, 16 to 32 KB, on their way: more of them only spread the reads over memory.  The key heads of a
-// share run side by side, since they lie side by side in a page.  BYPASS: keys and values that the
+// Workgroups are few (one a CU; two where the next paragraph says so) and every wave has one or two
+// blocks, 16 to 32 KB, on their way: more of them only spread the reads over memory.  The key heads of
+// a share run side by side, since they lie side by side in a page.  BYPASS: keys and values that the
 // last-level cache could not keep until the next call are read past it.  16 sequences of up to
 // 17,664 tokens, 4 key heads of d 128 under 24, and 110,080 tokens of 24 heads, us a call: shares in
 // the order samples, key heads, turns, 512 workgroups 53 and 129; key heads side by side 51 and 128;
@@ -155,8 +157,8 @@ struct Turns {
 //
 // Two tiles of rows, and three at d 64, have more to work on between a block's loads: two workgroups a CU,
 // whose waves hold one block each (and so fit), work on one while the other's is on its way.  The same
-// sequences, us: 18 rows 60 and 52, 48 rows of d 64 47 and 42; two of 6,000, 24 key heads, 20 rows 27.5 and
-// 29; 48 rows of d 128 75 and 95 (they do not fit), 6 rows 48 and 47.5.
+// sequences, us: 18 rows 64 and 54.5, 48 rows of d 64 52 and 47; two of 6,000, 24 key heads, 20 rows 29.5 and
+// 31; 48 rows of d 128 75 and 95 (they do not fit), 6 rows 48 and 47.5.
 //
 // Weights as two values for bf16 inputs too, us with one and with two: 16 sequences of up to 17,664
 // tokens, 6 rows 46.4 and 47.7, 18 rows 58.9 and 59.5, 48 rows 74 and 79, 48 rows of d 64 42 and 47;
@@ -499,7 +501,9 @@ constexpr int kKeyPiece = 64 * 8 + 8;                      // elements from a pi
 // What bounds it: the matrix pipe at the clock that the card holds under it (busy 52% of the cycles, as
 // vector units issue in 45%) and, for the example, 20 us of joining four ranges: 399 us in all, 1,050
 // TFLOP/s where a product of 8,192^3 has 1,209; without ranges (4 x 16 heads, 4,096 over 16,384) 1,204.
-// fp16 at d 128 655 us: five products instead of four at half the waves.
+// fp16 at d 128 655 us: six matrix instructions instead of four, and one wave a SIMD instead of two.
+// d 64: 4,096 tokens of 24 heads over 4 74 us, 700 TFLOP/s: half the matrix instructions for a weight's
+// same vector work (vector units issuing in 47% of the cycles, the matrix pipe busy in 28%).
 constexpr int row_waves(bool f16, int D) { return f16 ? 4 : D / 16; }
 
 // One step over tiles that every row sees whole: the scores of the next tile, the
@@ -958,9 +962,9 @@ CachePlan plan_cache_attn(const CacheParams& p, bool f16) {
   const int64_t units = (int64_t)p.B * p.Hk, rows = (int64_t)p.G * p.L, keys = (int64_t)p.c.max_pages * p.c.page;
   const int64_t steps = (keys + 255) / 256;
   // 33 to 48 rows too where keys are shared: 16 sequences of up to 17,664 tokens, 4 key heads of d 128
-  // under 24, eight tokens each, 124 us over tiles of 256 rows, 76 here (fp16 125 and 79, d 64 54 and 47).
+  // under 24, eight tokens each, 124 us over tiles of 256 rows, 79 here (fp16 125 and 79, d 64 54 and 47).
   // Not over less than 12 turns: 16 sequences of up to 2,304 tokens 28 and 35 (one of 3,000 24 and 21, 64 of
-  // up to 4,096 107 and 90), 32 of up to 1,500 tokens, each a workgroup's, 40 rows, 23 and 27.
+  // up to 4,096 107 and 96), 32 of up to 1,500 tokens, each a workgroup's, 40 rows, 23 and 27.
   // 49 to 64 rows gain nothing (60 of d 64: 20 and 20; 64 of d 128 over 100,000 tokens: 100 and 98).
   c.few = rows <= kFewRows || (rows <= kSharedRows && steps >= kSharedSteps);
   c.chunks = 1;
